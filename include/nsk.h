@@ -467,6 +467,99 @@ int nsk_gru_seq_bwd(int dtype, int T, int N, int H, const void *saved, const voi
                     void *dgi, void *dgh, void *dh_scratch, void *stream);
 
 /* ---------------------------------------------------------------------------------------------------------------
+ * Sequence models without a step-by-step product: layer norm, the gated linear recurrence, AdamW with 8-bit moments.
+ * What the GRU above computes one step after the other, a recurrence that is linear in its state computes for all steps
+ * at once; stacks of such layers want a normalisation that needs no batch (lengths differ, and a token comes alone when
+ * a model is served), and a large embedding table wants an optimizer state of two bytes a weight instead of eight.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Layer norm over the last axis of [rows, C], with the residual add in front of it:
+ *   s = x + residual (x without one), rounded to `dtype`;  mean and var over a row of s, biased;  invstd = 1/sqrt(var + eps);
+ *   y = (s - mean) * invstd * gamma + beta.
+ * gamma, beta: float [C], each may be NULL (ones, zeros). */
+typedef struct {
+    long long rows;
+    int C;
+    int dtype;   /* of x, residual, sum, y, dy, dsum, dx */
+    float eps;   /* above 0; not read by the backward pass */
+} nsk_layernorm_desc_t;
+/* Bytes of workspace of nsk_layernorm_bwd; 0 for an invalid descriptor.  Host only. */
+size_t nsk_layernorm_bwd_workspace_bytes(const nsk_layernorm_desc_t *desc);
+/* residual: NULL or [rows, C]; sum: NULL or [rows, C], receives s (a backward pass and the next residual add read it), only
+ * with a residual; it may be the buffer of `residual`, or of x.  save_mean, save_invstd: NULL or float [rows]. */
+int nsk_layernorm_fwd(const nsk_layernorm_desc_t *desc, const void *x, const void *residual, const float *gamma,
+                      const float *beta, void *sum, void *y, float *save_mean, float *save_invstd, void *stream);
+/* s: what was normalised (x, or `sum`).  With gh = dy * gamma and xh = (s - mean) * invstd, means over a row:
+ *   dx = invstd * (gh - mean(gh) - xh * mean(gh * xh)) + dsum   (the gradient of x, and of the residual)
+ *   dgamma (+)= sum over rows of dy * xh,  dbeta (+)= sum over rows of dy   (float [C], each may be NULL).
+ * dsum: NULL, or [rows, C], the gradient that reaches s past the normalisation; dx may be the buffer of dsum.
+ * Fixed order of summation. */
+int nsk_layernorm_bwd(const nsk_layernorm_desc_t *desc, const void *s, const void *dy, const void *dsum,
+                      const float *gamma, const float *save_mean, const float *save_invstd, void *dx, float *dgamma,
+                      float *dbeta, int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gated linear recurrence.  gi: [T,N,3H], one product of the layer's input, gates in the order (f, c, o); bias: float [3H]
+ * or NULL.  For every sequence n and channel, steps t < lengths[n] (NULL: all T):
+ *   f = sigmoid(gi_f + b_f),  c = gi_c + b_c,  o = sigmoid(gi_o + b_o),  h_t = f * h_{t-1} + (1 - f) * c,  y_t = o * h_t.
+ * In later steps h stays, y and the gradients are zero and gi, dy are not used, whatever they hold.  A length below 0 counts as
+ * 0, one above T as T.  States are float throughout.
+ * Rows of 3H (gi, dgi) and H (y, dy) elements are contiguous; strides say where they begin: element (t, n, 0) lies at
+ * t * gi_t + n * gi_n.  Both strides of a pair 0: dense [T,N,..].  [N,T,..] is gi_n = T * gi_t.  Rows must not overlap, and
+ * the rows of one step or those of one sequence have to lie together (no row of another one between them). */
+typedef struct {
+    int T, N, H;
+    int dtype;               /* of gi, y, dy, dgi */
+    long long gi_t, gi_n;    /* of gi and dgi */
+    long long y_t, y_n;      /* of y and dy */
+} nsk_glr_desc_t;
+/* Steps between two states that the forward pass leaves for the backward pass. */
+#define NSK_GLR_STRETCH 16
+/* Bytes of `saved`: float [ceil(T / NSK_GLR_STRETCH)][N][H], the states that enter the steps 0, 16, 32, ...; 0 for an invalid
+ * descriptor.  Host only. */
+size_t nsk_glr_saved_bytes(const nsk_glr_desc_t *desc);
+/* Workspace of a pass (NSK_PASS_FWD, NSK_PASS_DGRAD); may be 0.  Host only. */
+size_t nsk_glr_workspace_bytes(const nsk_glr_desc_t *desc, int pass);
+/* h0: float [N,H], NULL: zeros.  y: NULL if only the last state is wanted; h_last: NULL or float [N,H], the state after the
+ * last step; one of the two at least.  saved: NULL where no backward pass follows. */
+int nsk_glr_fwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0,
+                void *y, float *h_last, float *saved, void *workspace, size_t workspace_bytes, void *stream);
+/* dy: NULL (no gradient of y), dh_last: NULL or float [N,H]; one of the two at least.  dgi: as gi; its column sums are the
+ * bias gradients.  dh0: NULL or float [N,H]. */
+int nsk_glr_bwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *saved,
+                const void *dy, const float *dh_last, void *dgi, float *dh0, void *workspace, size_t workspace_bytes,
+                void *stream);
+/* One token for each of N sequences whose states lie in a table, state: float [S,H], updated in place.  gi: [N,3H], y: [N,H]
+ * (NULL: not wanted).  slots: int [N], the row of the table that holds sequence n's state, no row twice; NULL: row n.  A slot
+ * outside [0,S) is an idle place of the batch: y is zero there and no state changes. */
+int nsk_glr_step(int dtype, int N, int H, int S, const void *gi, const float *bias, const int *slots, float *state,
+                 void *y, void *stream);
+
+/* AdamW on `count` tensors as nsk_adamw_step_multi, with the moments in 8 bits: m, and r = sqrt(v), are e4m3 values (one sign, four
+ * exponent, three mantissa bits, largest 448) times a power of two for every NSK_ADAMW8_BLOCK elements.  A record's state is n
+ * bytes m, n bytes r and ceil(n / NSK_ADAMW8_BLOCK) floats each in scale_m and scale_r (4-byte aligned); all zeros at the start.
+ *   g = grad_scale * grad;  m <- beta1*m + (1-beta1)*g;  r <- sqrt(beta2*r*r + (1-beta2)*g*g);
+ *   w <- w*(1 - lr*weight_decay) - lr * (m/(1-beta1^step)) / (r/sqrt(1-beta2^step) + eps);  grad <- 0;  w_lp <- bf16 of w.
+ * w takes m and r as computed; held are then m / scale and r / scale, scale the power of two (2^-126 at least) for which the
+ * block's largest magnitude lies in (224, 448], rounded at random with the exact value as the mean: r moves by less than a
+ * thousandth in a step and would stand still if rounded to nearest.  An r above zero is never held as zero, so that no weight is
+ * divided by eps alone.  Infinite or NaN moments become NaN and do not enter the scale: they stay with their element.
+ * The random bits are a function of `seed`, the tensor's place in `params` and the element's in the tensor; a caller takes
+ * another seed for every step.  With mix(x): x ^= x >> 16, x *= 0x243F6A89, x ^= x >> 15, x *= 0xB7E15163, x ^= x >> 16 on 32
+ * bits, element i of tensor k has u = mix(i * 0x9E3779B9 + (i >> 32) * 0x85A308D3 + mix(seed + k * 0x9E3779B9)); a magnitude is
+ * rounded up where the part below its last place is at least 1 - (u & 0xffff) / 65536 of a place (m), (u >> 16) for r. */
+#define NSK_ADAMW8_BLOCK 256
+typedef struct {
+    float *w, *grad;
+    void *m, *r;
+    float *scale_m, *scale_r;
+    void *w_lp;              /* NULL, or n bf16 elements */
+    size_t n;
+    float weight_decay;
+} nsk_param8_t;
+int nsk_adamw8_step_multi(int count, const nsk_param8_t *params, int step, unsigned seed, float lr, float beta1, float beta2,
+                          float eps, const float *grad_scale, void *stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
  * Device memory pool and cache (section "Caching and Pooling"): what hands out the raw pointers every entry point
  * above takes, for callers that have no allocator of their own.  Host code; no entry point above uses it.
  *

@@ -59,6 +59,18 @@ class nsk_param_t(ctypes.Structure):
                 ("w_lp", ctypes.c_void_p), ("n", ctypes.c_size_t), ("weight_decay", ctypes.c_float)]
 
 
+class nsk_layernorm_desc_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong), ("C", ctypes.c_int), ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class nsk_glr_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("T", "N", "H", "dtype")] + [(n, ctypes.c_longlong) for n in ("gi_t", "gi_n", "y_t", "y_n")]
+
+
+class nsk_param8_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "grad", "m", "r", "scale_m", "scale_r", "w_lp")] + [("n", ctypes.c_size_t), ("weight_decay", ctypes.c_float)]
+
+
 class NskError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -216,6 +228,25 @@ def lib() -> ctypes.CDLL:
         L.nsk_gru_seq_bwd.restype = ci
         L.nsk_gru_seq_bwd.argtypes = [ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp]
         vpp, szp = ctypes.POINTER(vp), ctypes.POINTER(sz)
+        ld, gd = ctypes.POINTER(nsk_layernorm_desc_t), ctypes.POINTER(nsk_glr_desc_t)
+        L.nsk_layernorm_bwd_workspace_bytes.restype = sz
+        L.nsk_layernorm_bwd_workspace_bytes.argtypes = [ld]
+        L.nsk_layernorm_fwd.restype = ci
+        L.nsk_layernorm_fwd.argtypes = [ld] + [vp] * 9
+        L.nsk_layernorm_bwd.restype = ci
+        L.nsk_layernorm_bwd.argtypes = [ld] + [vp] * 9 + [ci, vp, sz, vp]
+        L.nsk_glr_saved_bytes.restype = sz
+        L.nsk_glr_saved_bytes.argtypes = [gd]
+        L.nsk_glr_workspace_bytes.restype = sz
+        L.nsk_glr_workspace_bytes.argtypes = [gd, ci]
+        L.nsk_glr_fwd.restype = ci
+        L.nsk_glr_fwd.argtypes = [gd] + [vp] * 7 + [vp, sz, vp]
+        L.nsk_glr_bwd.restype = ci
+        L.nsk_glr_bwd.argtypes = [gd] + [vp] * 8 + [vp, sz, vp]
+        L.nsk_glr_step.restype = ci
+        L.nsk_glr_step.argtypes = [ci, ci, ci, ci] + [vp] * 6
+        L.nsk_adamw8_step_multi.restype = ci
+        L.nsk_adamw8_step_multi.argtypes = [ci, ctypes.POINTER(nsk_param8_t), ci, ctypes.c_uint] + [ctypes.c_float] * 4 + [vp, vp]
         L.nsk_pool_create.restype = ci
         L.nsk_pool_create.argtypes = [ci, vpp]
         L.nsk_pool_get.restype = ci
@@ -256,9 +287,13 @@ EXPORTS = ("nsk_version", "nsk_test_hooks_reload", "nsk_status_string", "nsk_las
            "nsk_sgd_momentum_step", "nsk_adamw_step", "nsk_sgd_momentum_step_multi", "nsk_adamw_step_multi", "nsk_sumsq_accumulate", "nsk_clip_scale", "nsk_clip_scale_multi",
            "nsk_embedding_fwd", "nsk_embedding_bwd", "nsk_gru_gates_fwd", "nsk_gru_gates_bwd",
            "nsk_gru_step_supported", "nsk_gru_step_fwd", "nsk_gru_step_bwd", "nsk_gru_seq_blocks", "nsk_gru_seq_fwd", "nsk_gru_seq_bwd",
+           "nsk_layernorm_bwd_workspace_bytes", "nsk_layernorm_fwd", "nsk_layernorm_bwd", "nsk_glr_saved_bytes", "nsk_glr_workspace_bytes",
+           "nsk_glr_fwd", "nsk_glr_bwd", "nsk_glr_step", "nsk_adamw8_step_multi",
            "nsk_pool_create", "nsk_pool_get", "nsk_pool_put", "nsk_pool_cached", "nsk_pool_stats", "nsk_pool_destroy")
 NSK_POOL_DEVICE, NSK_POOL_HOST = 0, 1
 NSK_SUMSQ_PARTIALS = 256
+NSK_GLR_STRETCH = 16
+NSK_ADAMW8_BLOCK = 256
 
 
 def __getattr__(name):  # raw entry points under their C names: binding.nsk_conv2d_fwd(...)
@@ -956,6 +991,186 @@ def gru_seq_bwd(saved, h, dh_top, w_hh_t, dgi, dgh, dh_scratch):
     T, N, H = h.shape[0] - 1, h.shape[1], h.shape[2]
     _check(lib().nsk_gru_seq_bwd(_dtype_code(h), int(T), int(N), int(H), _ptr(saved), _ptr(h), _ptr(dh_top), _ptr(w_hh_t),
                                  _ptr(dgi), _ptr(dgh), _ptr(dh_scratch), _stream()), "nsk_gru_seq_bwd")
+
+
+# ------------------------------------------------------------------------------------ sequence models
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _layernorm_call(rows, C, dtype, eps):
+    ref = ctypes.byref(nsk_layernorm_desc_t(rows, C, dtype, eps))
+    return ref, lib().nsk_layernorm_bwd_workspace_bytes(ref)
+
+
+def _floats(t, *shape):
+    """t, a float32 tensor of that shape, or None."""
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape):
+        raise ValueError(f"a float32 tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def _like(t, ref):
+    """t, of ref's type and shape, or None."""
+    if t is not None and (t.dtype != ref.dtype or t.shape != ref.shape):
+        raise ValueError(f"a {ref.dtype} tensor of shape {tuple(ref.shape)} is wanted, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, residual=None, out=None, sum_out=None, save_mean=None, save_invstd=None, save=True):
+    """y = layer norm of s = x + residual over the last axis.  Returns (y, s, mean, invstd): s is x where there is no residual; with
+    save=False (nothing follows that needs them) the buffers that are not given are not made, and None comes back for them."""
+    C = int(x.shape[-1])
+    rows = x.numel() // C if C else 0
+    d, _ = _layernorm_call(rows, C, _dtype_code(x), float(eps))
+    _floats(gamma, C), _floats(beta, C), _like(residual, x), _like(out, x), _like(sum_out, x), _floats(save_mean, rows), _floats(save_invstd, rows)
+    if out is None:
+        out = torch.empty_like(x)
+    if save:
+        if sum_out is None and residual is not None:
+            sum_out = torch.empty_like(x)
+        if save_mean is None:
+            save_mean = torch.empty((rows,), dtype=torch.float32, device=x.device)
+        if save_invstd is None:
+            save_invstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    _check(lib().nsk_layernorm_fwd(d, _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(sum_out), _ptr(out), _ptr(save_mean), _ptr(save_invstd),
+                                   _stream()), "nsk_layernorm_fwd")
+    return out, x if residual is None else sum_out, save_mean, save_invstd
+
+
+def layernorm_bwd(dy, s, gamma, save_mean, save_invstd, dsum=None, dx=None, dgamma=None, dbeta=None, accumulate=False, want_affine=True,
+                  ws: Optional[Workspace] = None):
+    """s: what layernorm_fwd returned as such.  Returns (dx, dgamma, dbeta); dx includes dsum, the gradient that reaches s past the normalisation.
+    want_affine=False: no gradients of gamma and beta but into buffers that are given."""
+    C = int(s.shape[-1])
+    rows = s.numel() // C if C else 0
+    d, need = _layernorm_call(rows, C, _dtype_code(s), 1e-5)
+    _like(dy, s), _floats(gamma, C), _floats(save_mean, rows), _floats(save_invstd, rows), _like(dsum, s), _like(dx, s), _floats(dgamma, C), _floats(dbeta, C)
+    if dx is None:
+        dx = torch.empty_like(s)
+    if want_affine:
+        assert not accumulate or (dgamma is not None and dbeta is not None)
+        if dgamma is None:
+            dgamma = torch.empty((C,), dtype=torch.float32, device=s.device)
+        if dbeta is None:
+            dbeta = torch.empty((C,), dtype=torch.float32, device=s.device)
+    ws = ws or Workspace(s.device)
+    wp, wb = ws.get(need if dgamma is not None or dbeta is not None else 0)
+    _check(lib().nsk_layernorm_bwd(d, _ptr(s), _ptr(dy), _ptr(dsum), _ptr(gamma), _ptr(save_mean), _ptr(save_invstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                   int(bool(accumulate)), wp, wb, _stream()), "nsk_layernorm_bwd")
+    return dx, dgamma, dbeta
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _glr_call(T, N, H, dtype, gi_t, gi_n, y_t, y_n, which):
+    ref = ctypes.byref(nsk_glr_desc_t(T, N, H, dtype, gi_t, gi_n, y_t, y_n))
+    return ref, lib().nsk_glr_workspace_bytes(ref, which)
+
+
+def _rows_ptr(t: Optional[torch.Tensor], strides=None):
+    """Pointer of a [T,N,width] tensor whose rows are contiguous and begin where its strides (and `strides`, if given) say."""
+    if t is None:
+        return None
+    st, n = t.stride(), t.shape
+    if (not t.is_cuda or (n[2] > 1 and st[2] != 1) or any(n[k] > 1 and (st[k] < n[2] or (strides is not None and st[k] != strides[k])) for k in (0, 1))):
+        raise ValueError("rows of a sequence tensor have to be contiguous, and lie as those of the tensor that it belongs to")
+    return t.data_ptr()
+
+
+def _glr_dims(gi):
+    T, N, width = gi.shape
+    if width % 3:
+        raise ValueError(f"gi holds three gates a channel: [T, N, 3 * H], got {tuple(gi.shape)}")
+    return int(T), int(N), int(width) // 3
+
+
+def _lengths_ptr(lengths, N):
+    if lengths is not None and (lengths.dtype != torch.int32 or tuple(lengths.shape) != (N,)):
+        raise ValueError(f"lengths: int32 [{N}], got {lengths.dtype} {tuple(lengths.shape)}")
+    return _ptr(lengths)
+
+
+def glr_fwd(gi, bias=None, h0=None, lengths=None, y=None, h_last=None, saved=None, want_y=True, save=True, ws: Optional[Workspace] = None):
+    """All steps of the gated linear recurrence.  gi [T,N,3H], time-major, or a transposed view of [N,T,3H]; a y that is not given lies as
+    gi does.  Returns (y, h_last, saved): saved is what glr_bwd reads, None with save=False; y is None with want_y=False."""
+    T, N, H = _glr_dims(gi)
+    dev = gi.device
+    if y is None and want_y:
+        y = torch.empty((T, N, H), dtype=gi.dtype, device=dev) if gi.stride(0) >= gi.stride(1) else torch.empty((N, T, H), dtype=gi.dtype, device=dev).transpose(0, 1)
+    if y is not None and (y.dtype != gi.dtype or tuple(y.shape) != (T, N, H)):
+        raise ValueError(f"y: {gi.dtype} of shape {(T, N, H)}, got {y.dtype} {tuple(y.shape)}")
+    if h_last is None:
+        h_last = torch.empty((N, H), dtype=torch.float32, device=dev)
+    if saved is None and save:
+        saved = torch.empty((-(-T // NSK_GLR_STRETCH), N, H), dtype=torch.float32, device=dev)
+    _floats(bias, 3 * H), _floats(h0, N, H), _floats(h_last, N, H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H)
+    d, need = _glr_call(T, N, H, _dtype_code(gi), *gi.stride()[:2], *((0, 0) if y is None else y.stride()[:2]), NSK_PASS_FWD)
+    ws = ws or Workspace(dev)
+    wp, wb = ws.get(need)
+    _check(lib().nsk_glr_fwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(h0), _rows_ptr(y), _ptr(h_last), _ptr(saved), wp, wb, _stream()),
+           "nsk_glr_fwd")
+    return y, h_last, saved
+
+
+def glr_bwd(gi, saved, bias=None, dy=None, dh_last=None, lengths=None, dgi=None, dh0=None, want_dh0=True, ws: Optional[Workspace] = None):
+    """Gradients of glr_fwd: (dgi, dh0).  dgi lies as gi does."""
+    T, N, H = _glr_dims(gi)
+    dev = gi.device
+    if dgi is None:
+        dgi = torch.empty_strided(gi.shape, gi.stride(), dtype=gi.dtype, device=dev)
+    if dh0 is None and want_dh0:
+        dh0 = torch.empty((N, H), dtype=torch.float32, device=dev)
+    _like(dgi, gi), _floats(bias, 3 * H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H), _floats(dh_last, N, H), _floats(dh0, N, H)
+    if dy is not None and (dy.dtype != gi.dtype or tuple(dy.shape) != (T, N, H)):
+        raise ValueError(f"dy: {gi.dtype} of shape {(T, N, H)}, got {dy.dtype} {tuple(dy.shape)}")
+    d, need = _glr_call(T, N, H, _dtype_code(gi), *gi.stride()[:2], *((0, 0) if dy is None else dy.stride()[:2]), NSK_PASS_DGRAD)
+    ws = ws or Workspace(dev)
+    wp, wb = ws.get(need)
+    _check(lib().nsk_glr_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(dy), _ptr(dh_last), _rows_ptr(dgi, gi.stride()),
+                             _ptr(dh0), wp, wb, _stream()), "nsk_glr_bwd")
+    return dgi, dh0
+
+
+def glr_step(gi, state, bias=None, slots=None, y=None, want_y=True):
+    """One token for each of N sequences: gi [N,3H]; state float [S,H], updated in place; slots: int32 [N] rows of state, or None for the first N."""
+    N, H = int(gi.shape[0]), int(gi.shape[1]) // 3
+    if tuple(gi.shape) != (N, 3 * H):
+        raise ValueError(f"gi holds three gates a channel: [N, 3 * H], got {tuple(gi.shape)}")
+    S = int(state.shape[0])
+    _floats(state, S, H), _floats(bias, 3 * H)
+    if y is None and want_y:
+        y = torch.empty((N, H), dtype=gi.dtype, device=gi.device)
+    if y is not None and (y.dtype != gi.dtype or tuple(y.shape) != (N, H)):
+        raise ValueError(f"y: {gi.dtype} of shape {(N, H)}, got {y.dtype} {tuple(y.shape)}")
+    _check(lib().nsk_glr_step(_dtype_code(gi), N, H, S, _ptr(gi), _ptr(bias), _lengths_ptr(slots, N), _ptr(state), _ptr(y), _stream()), "nsk_glr_step")
+    return y
+
+
+def adamw8_state(n: int, device="cuda:0"):
+    """(m, r, scale_m, scale_r) of n weights before the first step of adamw8_step_multi."""
+    blocks = -(-n // NSK_ADAMW8_BLOCK)
+    held = lambda: torch.zeros((n,), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+    return held(), held(), torch.zeros((blocks,), dtype=torch.float32, device=device), torch.zeros((blocks,), dtype=torch.float32, device=device)
+
+
+def param8_table(records):
+    """records: iterable of (w, grad, m, r, scale_m, scale_r, w_lp or None, weight_decay) -> ctypes array of nsk_param8_t (keep the tensors
+    alive while it is in use)."""
+    records = list(records)
+    tab = (nsk_param8_t * len(records))()
+    for i, (w, g, m, r, sm, sr, lp, wd) in enumerate(records):
+        n = w.numel()
+        blocks = -(-n // NSK_ADAMW8_BLOCK)
+        assert all(t.dtype == torch.float32 and t.numel() == n for t in (w, g))
+        assert all(t.dtype == torch.float8_e4m3fn and t.numel() == n for t in (m, r))
+        assert all(t.dtype == torch.float32 and t.numel() == blocks for t in (sm, sr))
+        assert lp is None or (lp.dtype == torch.bfloat16 and lp.numel() == n)
+        tab[i] = nsk_param8_t(_ptr(w), _ptr(g), _ptr(m), _ptr(r), _ptr(sm), _ptr(sr), _ptr(lp), n, float(wd))
+    return tab
+
+
+def adamw8_step_multi(tab, step, seed, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None):
+    """In place on the tensors of param8_table; seed: a number below 2^32, another one for every step."""
+    _check(lib().nsk_adamw8_step_multi(len(tab), tab, int(step), int(seed), float(lr), float(beta1), float(beta2), float(eps), _ptr(grad_scale), _stream()),
+           "nsk_adamw8_step_multi")
 
 
 # ------------------------------------------------------------------------------------ memory pool
