@@ -2,7 +2,7 @@
 //   s = x + residual,  y = (s - mean) * invstd * gamma + beta
 //   gh = dy * gamma, xh = (s - mean) * invstd:  dx = invstd * (gh - mean(gh) - xh * mean(gh * xh)) + dsum,
 //   dgamma = sum over rows of dy * xh,  dbeta = sum over rows of dy
-// Bound by memory: a row is read once and stays in the registers of the lanes that share it (8 to 1024 of them), so that the variance is the mean square of
+// Bound by memory: a row is read once and stays in the registers of the lanes that share it (2 to 1024 of them), so that the variance is the mean square of
 // the differences from the mean itself, and the backward pass sums dy * xh and dy for the weights on the way.
 #include "nsk_internal.h"
 
@@ -17,35 +17,30 @@ template <typename T> struct Vec {
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
-// Sum over groups of LANES neighbouring lanes, in all of them.
-template <int LANES> __device__ inline float lanes_sum(float v)
+// The value of lane ^ O.
+template <int O> __device__ inline float other(float v)
 {
-    auto moved = [](float x, auto ctl) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctl)::value, 0xf, 0xf, true));
-    };
-    static_assert(LANES >= 8 && LANES <= 64, "a row of the register file at most");
-    v += moved(v, std::integral_constant<int, 0xb1>{});         // quad_perm 1,0,3,2
-    v += moved(v, std::integral_constant<int, 0x4e>{});         // quad_perm 2,3,0,1
-    v += moved(v, std::integral_constant<int, 0x141>{});        // row_half_mirror: the other four of eight
-    if constexpr (LANES >= 16) v += moved(v, std::integral_constant<int, 0x140>{});      // row_mirror: the other eight
-    if constexpr (LANES >= 32) {
-        const unsigned u = __builtin_bit_cast(unsigned, v);
-        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-        v = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    if constexpr (O == 1) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)u, 0xb1, 0xf, 0xf, true));      // quad_perm 1,0,3,2
+    else if constexpr (O < 16) return lane_xor<O>(v);
+    else {
+        // (of the two results of a swap with itself, each lane has its own value and the other's)
+        const auto r = O == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return __builtin_bit_cast(float, (unsigned)((threadIdx.x & O) ? r[0] : r[1]));
     }
-    if constexpr (LANES >= 64) {
-        const unsigned u = __builtin_bit_cast(unsigned, v);
-        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-        v = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
-    }
-    return v;
+}
+// Sum over the lanes whose numbers differ in bits FROM .. TO / 2, in all of them.
+template <int FROM, int TO> __device__ inline float lanes_sum(float v)
+{
+    if constexpr (FROM < TO) return lanes_sum<FROM * 2, TO>(v + other<FROM>(v));
+    else return v;
 }
 // Sums of M values over the LANES lanes that share a row.  Rows of several wavefronts exchange them through LDS, in two buffers that take turns: a wavefront
 // writes one again only after a barrier that all reach behind their reads of it.
 template <int LANES, int M> __device__ inline void row_sum(float (&v)[M], float (&part)[2][M][16], int &turn)
 {
 #pragma unroll
-    for (int m = 0; m < M; ++m) v[m] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[m]);
+    for (int m = 0; m < M; ++m) v[m] = lanes_sum<1, (LANES < 64 ? LANES : 64)>(v[m]);
     if constexpr (LANES > 64) {
         const int wave = threadIdx.x >> 6;
 #pragma unroll
@@ -71,22 +66,33 @@ template <typename T, int LANES, int K> struct Share {
     __device__ bool has(int k) const { return k * LANES + at < vectors; }
     __device__ bool has_tail() const { return at < tail; }
     __device__ bool valid(int i) const { return i < K * V ? has(i / V) : has_tail(); }
-    // Zeros (`none`) where the lane has nothing.
-    template <typename U> __device__ void load(const U *row, float (&v)[SIZE], float none = 0.f) const
+    // A lane's part as it lies in memory, zeros where it has none; a later row's is fetched while one is worked on.
+    struct Raw {
+        vec v[K];
+        T tail;
+    };
+    __device__ void fetch(const T *row, Raw &r) const
     {
-        typedef U uvec __attribute__((ext_vector_type(V), aligned(sizeof(U))));
+#pragma unroll
+        for (int k = 0; k < K; ++k) r.v[k] = has(k) ? *(const vec *)(row + (k * LANES + at) * V) : vec{};
+        r.tail = has_tail() ? row[vectors * V + at] : (T)0.f;
+    }
+    static __device__ void unpack(const Raw &r, float (&v)[SIZE])
+    {
+#pragma unroll
+        for (int i = 0; i < K * V; ++i) v[i] = (float)r.v[i / V][i % V];
+        v[K * V] = (float)r.tail;
+    }
+    __device__ void load(const float *row, float (&v)[SIZE]) const
+    {
+        typedef float fvec __attribute__((ext_vector_type(V), aligned(4)));
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (has(k)) {
-                const uvec u = *(const uvec *)(row + (k * LANES + at) * V);
+            const fvec u = has(k) ? *(const fvec *)(row + (k * LANES + at) * V) : fvec{};
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[k * V + e] = (float)u[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[k * V + e] = none;
-            }
+            for (int e = 0; e < V; ++e) v[k * V + e] = u[e];
         }
-        v[K * V] = has_tail() ? (float)row[vectors * V + at] : none;
+        v[K * V] = has_tail() ? row[vectors * V + at] : 0.f;
     }
     template <typename U> __device__ void store(U *row, const float (&v)[SIZE]) const
     {
@@ -127,10 +133,13 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void layernorm_fwd_kerne
         if (row >= rows) break;         // (rows of several wavefronts: one a block, none left for any)
         const size_t at = (size_t)row * C;
         float v[S::SIZE], t[1] = {0.f};
-        s.load(x + at, v);
+        typename S::Raw raw, more;
+        s.fetch(x + at, raw);
+        if (residual) s.fetch(residual + at, more);
+        S::unpack(raw, v);
         if (residual) {
             float w[S::SIZE];
-            s.load(residual + at, w);
+            S::unpack(more, w);
 #pragma unroll
             for (int i = 0; i < S::SIZE; ++i) v[i] = (float)(T)(v[i] + w[i]);
             if (sum) s.store(sum + at, v);
@@ -176,17 +185,29 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void layernorm_bwd_kerne
 #pragma unroll
     for (int i = 0; i < S::SIZE; ++i) dg[i] = db[i] = 0.f;
     const float over = 1.f / (float)C;
-    for (long long r0 = (long long)blockIdx.x * ROWS; r0 < rows; r0 += (long long)gridDim.x * ROWS) {
-        const long long row = r0 + threadIdx.x / LANES;
-        if (row >= rows) break;
+    const long long step = (long long)gridDim.x * ROWS;
+    typename S::Raw rs{}, rd{}, ru{};
+    float mean = 0.f, invstd = 0.f;
+    auto fetch = [&](long long row) {
         const size_t at = (size_t)row * C;
-        const float mean = save_mean[row], invstd = save_invstd[row];
-        float v[S::SIZE], d[S::SIZE], t[2] = {0.f, 0.f};
-        s.load(sum + at, v, mean);      // (xh is 0 where the lane has nothing)
-        s.load(dy + at, d);
+        mean = save_mean[row];
+        invstd = save_invstd[row];
+        s.fetch(sum + at, rs);
+        s.fetch(dy + at, rd);
+        if (dsum) s.fetch(dsum + at, ru);
+    };
+    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / LANES;
+    if (row < rows) fetch(row);
+    for (; row < rows; row += step) {       // (rows of several wavefronts: one a block, the same for all)
+        float v[S::SIZE], d[S::SIZE], u[S::SIZE], t[2] = {0.f, 0.f};
+        S::unpack(rs, v);
+        S::unpack(rd, d);
+        S::unpack(ru, u);
+        const float m = mean, inv = invstd;
+        if (row + step < rows) fetch(row + step);
 #pragma unroll
         for (int i = 0; i < S::SIZE; ++i) {
-            v[i] = (v[i] - mean) * invstd;
+            v[i] = (v[i] - m) * inv;        // (where the lane has nothing: anything, and d is 0)
             if (PARAMS) {
                 dg[i] += d[i] * v[i];
                 db[i] += d[i];
@@ -198,25 +219,28 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void layernorm_bwd_kerne
         row_sum<LANES>(t, part, turn);
         const float a = t[0] * over, b = t[1] * over;
 #pragma unroll
-        for (int i = 0; i < S::SIZE; ++i) v[i] = invstd * (d[i] - a - v[i] * b);
-        if (dsum) {
-            s.load(dsum + at, d);
+        for (int i = 0; i < S::SIZE; ++i) v[i] = inv * (d[i] - a - v[i] * b);
+        if (dsum)
 #pragma unroll
-            for (int i = 0; i < S::SIZE; ++i) v[i] += d[i];
-        }
-        s.store(dx + at, v);
+            for (int i = 0; i < S::SIZE; ++i) v[i] += u[i];
+        s.store(dx + (size_t)row * C, v);
     }
     if constexpr (PARAMS) {
         float *const p = partial + (size_t)blockIdx.x * C, *const q = p + (size_t)gridDim.x * C;
         if constexpr (ROWS > 1) {
-            // lanes of the block's other rows with the same columns: added up in LDS, row by row
+            // lanes of the block's other rows with the same columns: within a wavefront first, then wavefront by wavefront in LDS
+#pragma unroll
+            for (int i = 0; i < S::SIZE; ++i) {
+                dg[i] = lanes_sum<LANES, 64>(dg[i]);
+                db[i] = lanes_sum<LANES, 64>(db[i]);
+            }
             extern __shared__ float sums[];     // [2][C]
-            for (int turn2 = 0; turn2 < ROWS; ++turn2) {
+            for (int w = 0; w < 4; ++w) {
                 __syncthreads();
-                if ((int)threadIdx.x / LANES == turn2) {
+                if ((int)threadIdx.x >> 6 == w && (threadIdx.x & 63) < LANES) {
                     auto add = [&](int c, int i) {
-                        sums[c] = turn2 ? sums[c] + dg[i] : dg[i];
-                        sums[C + c] = turn2 ? sums[C + c] + db[i] : db[i];
+                        sums[c] = w ? sums[c] + dg[i] : dg[i];
+                        sums[C + c] = w ? sums[C + c] + db[i] : db[i];
                     };
 #pragma unroll
                     for (int i = 0; i < K * S::V; ++i)
@@ -300,6 +324,7 @@ __global__ __launch_bounds__(256) void layernorm_dparam_wide_kernel(const T *__r
     const int c = blockIdx.y * 256 + threadIdx.x;
     if (c >= C) return;
     float a = 0.f, b = 0.f;
+#pragma unroll 4
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const float d = (float)dy[(size_t)r * C + c];
         a += d * (((float)s[(size_t)r * C + c] - save_mean[r]) * save_invstd[r]);
@@ -319,6 +344,7 @@ __global__ __launch_bounds__(1024) void layernorm_dparam_final_kernel(const floa
     if (!out) return;
     double t = 0.0;
     if (c < C)
+#pragma unroll 8
         for (int k = k0; k < shares; k += 32) t += (double)partial[((size_t)blockIdx.y * shares + k) * C + c];
     part[k0][column] = t;
     __syncthreads();
@@ -335,21 +361,25 @@ struct Plan {
 Plan plan_of(const nsk_layernorm_desc_t &d)
 {
     const int v = d.dtype == NSK_BF16 ? 8 : 4, vectors = d.C / v;
-    for (int lanes = 8; lanes <= 64; lanes *= 2)
+    // (an element behind the last vector has a lane of its own: there are 7 of them at most)
+    for (int lanes = d.C % v ? 8 : 2; lanes <= 64; lanes *= 2)
         if (vectors <= lanes) return {lanes, 1};
     if (vectors <= 128) return {64, 2};
-    if (vectors <= 256) return {64, 4};
+    if (vectors <= 256) return {256, 1};
     if (vectors <= 512) return {256, 2};
-    if (vectors <= 1024) return {256, 4};
+    if (vectors <= 1024) return {1024, 1};
     if (vectors <= 2048) return {1024, 2};
     return {0, 0};
 }
+// The pass that makes dx also makes the sums for gamma and beta, unless their registers would not fit (16384 bf16 columns, 2048 rows: 147 us with spilled ones,
+// 31 for dx alone).
+constexpr bool on_the_way(Plan p) { return p.lanes > 0 && !(p.lanes == 1024 && p.k == 2); }
 int rows_a_block(const Plan &p) { return p.lanes == 0 || p.lanes >= 256 ? 1 : 256 / p.lanes; }
 // Blocks of the backward pass, each with sums of its own.
 int shares_of(const nsk_layernorm_desc_t &d)
 {
     const Plan p = plan_of(d);
-    const long long blocks = (d.rows + 4 * rows_a_block(p) - 1) / (4 * rows_a_block(p)), most = p.lanes == 1024 ? 256 : 512;
+    const long long blocks = (d.rows + rows_a_block(p) - 1) / rows_a_block(p), most = p.lanes == 1024 || p.lanes == 0 ? 256 : 512;
     return (int)(blocks < most ? blocks : most);
 }
 
@@ -366,7 +396,7 @@ template <typename F> void with(const Plan &p, F &&f)
 {
 #define NSK_CASE(L, N)                                                                   \
     if (p.lanes == L && p.k == N) f(std::integral_constant<int, L>{}, std::integral_constant<int, N>{});
-    NSK_CASE(8, 1) NSK_CASE(16, 1) NSK_CASE(32, 1) NSK_CASE(64, 1) NSK_CASE(64, 2) NSK_CASE(64, 4) NSK_CASE(256, 2) NSK_CASE(256, 4) NSK_CASE(1024, 2)
+    NSK_CASE(2, 1) NSK_CASE(4, 1) NSK_CASE(8, 1) NSK_CASE(16, 1) NSK_CASE(32, 1) NSK_CASE(64, 1) NSK_CASE(64, 2) NSK_CASE(256, 1) NSK_CASE(256, 2) NSK_CASE(1024, 1) NSK_CASE(1024, 2)
 #undef NSK_CASE
 }
 
@@ -430,18 +460,18 @@ int nsk_layernorm_bwd(const nsk_layernorm_desc_t *desc, const void *s, const voi
     float *const partial = (float *)workspace;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        if (p.lanes == 0) {
-            if (params)
-                hipLaunchKernelGGL(layernorm_dparam_wide_kernel<T>, dim3((unsigned)shares, (unsigned)ceil_div(C, 256)), dim3(256), 0, st, (const T *)s, (const T *)dy, save_mean, save_invstd,
-                                   partial, desc->rows, C);
+        if (params && !on_the_way(p))
+            hipLaunchKernelGGL(layernorm_dparam_wide_kernel<T>, dim3((unsigned)shares, (unsigned)ceil_div(C, 256)), dim3(256), 0, st, (const T *)s, (const T *)dy, save_mean, save_invstd,
+                               partial, desc->rows, C);
+        if (p.lanes == 0)
             hipLaunchKernelGGL(layernorm_dx_wide_kernel<T>, dim3((unsigned)(desc->rows < 512 ? desc->rows : 512)), dim3(1024), 0, st, (const T *)s, (const T *)dy, (const T *)dsum, gamma,
                                save_mean, save_invstd, (T *)dx, desc->rows, C);
-        }
         with(p, [&](auto lanes, auto k) {
             constexpr int L = decltype(lanes)::value, N = decltype(k)::value;
             const dim3 block(L > 256 ? L : 256);
-            if (params)
-                hipLaunchKernelGGL((layernorm_bwd_kernel<T, L, N, true>), grid, block, L < 256 ? 2 * C * sizeof(float) : 0, st, (const T *)s, (const T *)dy, (const T *)dsum, gamma, save_mean,
+            constexpr bool ON_THE_WAY = on_the_way({L, N});
+            if (params && ON_THE_WAY)
+                hipLaunchKernelGGL((layernorm_bwd_kernel<T, L, N, ON_THE_WAY>), grid, block, L < 256 ? 2 * C * sizeof(float) : 0, st, (const T *)s, (const T *)dy, (const T *)dsum, gamma, save_mean,
                                    save_invstd, (T *)dx, partial, desc->rows, C);
             else
                 hipLaunchKernelGGL((layernorm_bwd_kernel<T, L, N, false>), grid, block, 0, st, (const T *)s, (const T *)dy, (const T *)dsum, gamma, save_mean, save_invstd, (T *)dx, partial,
