@@ -1001,18 +1001,25 @@ def _layernorm_call(rows, C, dtype, eps):
     return ref, lib().nsk_layernorm_bwd_workspace_bytes(ref)
 
 
+# (What a call makes and checks costs more than it does itself where it is small: sizes go to torch.empty as numbers, 0.8 us less than as a tuple, and
+# what was not given is not checked.)
+
 def _floats(t, *shape):
-    """t, a float32 tensor of that shape, or None."""
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape):
+    """t, if it is given: a float32 tensor of that shape."""
+    if t is not None and (t.dtype is not torch.float32 or t.shape != shape):
         raise ValueError(f"a float32 tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)}")
-    return t
 
 
 def _like(t, ref):
-    """t, of ref's type and shape, or None."""
-    if t is not None and (t.dtype != ref.dtype or t.shape != ref.shape):
+    """t, if it is given: of ref's type and shape."""
+    if t is not None and (t.dtype is not ref.dtype or t.shape != ref.shape):
         raise ValueError(f"a {ref.dtype} tensor of shape {tuple(ref.shape)} is wanted, got {t.dtype} {tuple(t.shape)}")
-    return t
+
+
+def _rows_of(t, ref, *shape):
+    """t, if it is given: of ref's type and that shape."""
+    if t is not None and (t.dtype is not ref.dtype or t.shape != shape):
+        raise ValueError(f"a {ref.dtype} tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)}")
 
 
 def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, residual=None, out=None, sum_out=None, save_mean=None, save_invstd=None, save=True):
@@ -1021,16 +1028,21 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, residual=None, out=None, s
     C = int(x.shape[-1])
     rows = x.numel() // C if C else 0
     d, _ = _layernorm_call(rows, C, _dtype_code(x), float(eps))
-    _floats(gamma, C), _floats(beta, C), _like(residual, x), _like(out, x), _like(sum_out, x), _floats(save_mean, rows), _floats(save_invstd, rows)
+    _floats(gamma, C), _floats(beta, C), _like(residual, x), _like(sum_out, x)
     if out is None:
         out = torch.empty_like(x)
-    if save:
-        if sum_out is None and residual is not None:
-            sum_out = torch.empty_like(x)
-        if save_mean is None:
-            save_mean = torch.empty((rows,), dtype=torch.float32, device=x.device)
-        if save_invstd is None:
-            save_invstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    else:
+        _like(out, x)
+    if save and sum_out is None and residual is not None:
+        sum_out = torch.empty_like(x)
+    if save_mean is not None:
+        _floats(save_mean, rows)
+    elif save:
+        save_mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if save_invstd is not None:
+        _floats(save_invstd, rows)
+    elif save:
+        save_invstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(lib().nsk_layernorm_fwd(d, _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(sum_out), _ptr(out), _ptr(save_mean), _ptr(save_invstd),
                                    _stream()), "nsk_layernorm_fwd")
     return out, x if residual is None else sum_out, save_mean, save_invstd
@@ -1043,15 +1055,20 @@ def layernorm_bwd(dy, s, gamma, save_mean, save_invstd, dsum=None, dx=None, dgam
     C = int(s.shape[-1])
     rows = s.numel() // C if C else 0
     d, need = _layernorm_call(rows, C, _dtype_code(s), 1e-5)
-    _like(dy, s), _floats(gamma, C), _floats(save_mean, rows), _floats(save_invstd, rows), _like(dsum, s), _like(dx, s), _floats(dgamma, C), _floats(dbeta, C)
+    _like(dy, s), _floats(gamma, C), _floats(save_mean, rows), _floats(save_invstd, rows), _like(dsum, s)
+    assert not accumulate or not want_affine or (dgamma is not None and dbeta is not None)
     if dx is None:
         dx = torch.empty_like(s)
-    if want_affine:
-        assert not accumulate or (dgamma is not None and dbeta is not None)
-        if dgamma is None:
-            dgamma = torch.empty((C,), dtype=torch.float32, device=s.device)
-        if dbeta is None:
-            dbeta = torch.empty((C,), dtype=torch.float32, device=s.device)
+    else:
+        _like(dx, s)
+    if dgamma is not None:
+        _floats(dgamma, C)
+    elif want_affine:
+        dgamma = torch.empty(C, dtype=torch.float32, device=s.device)
+    if dbeta is not None:
+        _floats(dbeta, C)
+    elif want_affine:
+        dbeta = torch.empty(C, dtype=torch.float32, device=s.device)
     ws = ws or Workspace(s.device)
     wp, wb = ws.get(need if dgamma is not None or dbeta is not None else 0)
     _check(lib().nsk_layernorm_bwd(d, _ptr(s), _ptr(dy), _ptr(dsum), _ptr(gamma), _ptr(save_mean), _ptr(save_invstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
@@ -1065,13 +1082,15 @@ def _glr_call(T, N, H, dtype, gi_t, gi_n, y_t, y_n, which):
     return ref, lib().nsk_glr_workspace_bytes(ref, which)
 
 
-def _rows_ptr(t: Optional[torch.Tensor], strides=None):
-    """Pointer of a [T,N,width] tensor whose rows are contiguous and begin where its strides (and `strides`, if given) say."""
+def _rows_ptr(t: Optional[torch.Tensor], like=None):
+    """Pointer of a [T,N,width] tensor whose rows are contiguous and do not overlap; `like`: one whose rows lie as its own have to."""
     if t is None:
         return None
-    st, n = t.stride(), t.shape
-    if (not t.is_cuda or (n[2] > 1 and st[2] != 1) or any(n[k] > 1 and (st[k] < n[2] or (strides is not None and st[k] != strides[k])) for k in (0, 1))):
-        raise ValueError("rows of a sequence tensor have to be contiguous, and lie as those of the tensor that it belongs to")
+    (T, N, width), (st, sn, one) = t.shape, t.stride()
+    if not t.is_cuda or (one != 1 and width > 1) or (T > 1 and st < width) or (N > 1 and sn < width):
+        raise ValueError("rows of a sequence tensor have to be contiguous, on the GPU, and must not overlap")
+    if like is not None and ((T > 1 and st != like.stride(0)) or (N > 1 and sn != like.stride(1))):
+        raise ValueError("rows of a gradient have to lie as those of its tensor")
     return t.data_ptr()
 
 
@@ -1079,11 +1098,11 @@ def _glr_dims(gi):
     T, N, width = gi.shape
     if width % 3:
         raise ValueError(f"gi holds three gates a channel: [T, N, 3 * H], got {tuple(gi.shape)}")
-    return int(T), int(N), int(width) // 3
+    return T, N, width // 3
 
 
 def _lengths_ptr(lengths, N):
-    if lengths is not None and (lengths.dtype != torch.int32 or tuple(lengths.shape) != (N,)):
+    if lengths is not None and (lengths.dtype is not torch.int32 or lengths.shape != (N,)):
         raise ValueError(f"lengths: int32 [{N}], got {lengths.dtype} {tuple(lengths.shape)}")
     return _ptr(lengths)
 
@@ -1092,17 +1111,23 @@ def glr_fwd(gi, bias=None, h0=None, lengths=None, y=None, h_last=None, saved=Non
     """All steps of the gated linear recurrence.  gi [T,N,3H], time-major, or a transposed view of [N,T,3H]; a y that is not given lies as
     gi does.  Returns (y, h_last, saved): saved is what glr_bwd reads, None with save=False; y is None with want_y=False."""
     T, N, H = _glr_dims(gi)
-    dev = gi.device
+    dev, (gt, gn, _) = gi.device, gi.stride()
     if y is None and want_y:
-        y = torch.empty((T, N, H), dtype=gi.dtype, device=dev) if gi.stride(0) >= gi.stride(1) else torch.empty((N, T, H), dtype=gi.dtype, device=dev).transpose(0, 1)
-    if y is not None and (y.dtype != gi.dtype or tuple(y.shape) != (T, N, H)):
-        raise ValueError(f"y: {gi.dtype} of shape {(T, N, H)}, got {y.dtype} {tuple(y.shape)}")
+        y = torch.empty(T, N, H, dtype=gi.dtype, device=dev) if gt >= gn else torch.empty(N, T, H, dtype=gi.dtype, device=dev).transpose(0, 1)
+    else:
+        _rows_of(y, gi, T, N, H)
     if h_last is None:
-        h_last = torch.empty((N, H), dtype=torch.float32, device=dev)
-    if saved is None and save:
-        saved = torch.empty((-(-T // NSK_GLR_STRETCH), N, H), dtype=torch.float32, device=dev)
-    _floats(bias, 3 * H), _floats(h0, N, H), _floats(h_last, N, H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H)
-    d, need = _glr_call(T, N, H, _dtype_code(gi), *gi.stride()[:2], *((0, 0) if y is None else y.stride()[:2]), NSK_PASS_FWD)
+        h_last = torch.empty(N, H, dtype=torch.float32, device=dev)
+    else:
+        _floats(h_last, N, H)
+    stretches = -(-T // NSK_GLR_STRETCH)
+    if saved is not None:
+        _floats(saved, stretches, N, H)
+    elif save:
+        saved = torch.empty(stretches, N, H, dtype=torch.float32, device=dev)
+    _floats(bias, 3 * H), _floats(h0, N, H)
+    yt, yn, _ = (0, 0, 1) if y is None else y.stride()
+    d, need = _glr_call(T, N, H, _dtype_code(gi), gt, gn, yt, yn, NSK_PASS_FWD)
     ws = ws or Workspace(dev)
     wp, wb = ws.get(need)
     _check(lib().nsk_glr_fwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(h0), _rows_ptr(y), _ptr(h_last), _ptr(saved), wp, wb, _stream()),
@@ -1116,30 +1141,34 @@ def glr_bwd(gi, saved, bias=None, dy=None, dh_last=None, lengths=None, dgi=None,
     dev = gi.device
     if dgi is None:
         dgi = torch.empty_strided(gi.shape, gi.stride(), dtype=gi.dtype, device=dev)
-    if dh0 is None and want_dh0:
-        dh0 = torch.empty((N, H), dtype=torch.float32, device=dev)
-    _like(dgi, gi), _floats(bias, 3 * H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H), _floats(dh_last, N, H), _floats(dh0, N, H)
-    if dy is not None and (dy.dtype != gi.dtype or tuple(dy.shape) != (T, N, H)):
-        raise ValueError(f"dy: {gi.dtype} of shape {(T, N, H)}, got {dy.dtype} {tuple(dy.shape)}")
-    d, need = _glr_call(T, N, H, _dtype_code(gi), *gi.stride()[:2], *((0, 0) if dy is None else dy.stride()[:2]), NSK_PASS_DGRAD)
+    else:
+        _like(dgi, gi)
+    if dh0 is not None:
+        _floats(dh0, N, H)
+    elif want_dh0:
+        dh0 = torch.empty(N, H, dtype=torch.float32, device=dev)
+    _floats(bias, 3 * H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H), _floats(dh_last, N, H), _rows_of(dy, gi, T, N, H)
+    gt, gn, _ = gi.stride()
+    yt, yn, _ = (0, 0, 1) if dy is None else dy.stride()
+    d, need = _glr_call(T, N, H, _dtype_code(gi), gt, gn, yt, yn, NSK_PASS_DGRAD)
     ws = ws or Workspace(dev)
     wp, wb = ws.get(need)
-    _check(lib().nsk_glr_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(dy), _ptr(dh_last), _rows_ptr(dgi, gi.stride()),
+    _check(lib().nsk_glr_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(dy), _ptr(dh_last), _rows_ptr(dgi, gi),
                              _ptr(dh0), wp, wb, _stream()), "nsk_glr_bwd")
     return dgi, dh0
 
 
 def glr_step(gi, state, bias=None, slots=None, y=None, want_y=True):
     """One token for each of N sequences: gi [N,3H]; state float [S,H], updated in place; slots: int32 [N] rows of state, or None for the first N."""
-    N, H = int(gi.shape[0]), int(gi.shape[1]) // 3
-    if tuple(gi.shape) != (N, 3 * H):
+    N, width = gi.shape
+    H, S = width // 3, state.shape[0]
+    if width % 3:
         raise ValueError(f"gi holds three gates a channel: [N, 3 * H], got {tuple(gi.shape)}")
-    S = int(state.shape[0])
-    _floats(state, S, H), _floats(bias, 3 * H)
-    if y is None and want_y:
-        y = torch.empty((N, H), dtype=gi.dtype, device=gi.device)
-    if y is not None and (y.dtype != gi.dtype or tuple(y.shape) != (N, H)):
-        raise ValueError(f"y: {gi.dtype} of shape {(N, H)}, got {y.dtype} {tuple(y.shape)}")
+    _floats(state, S, H), _floats(bias, width)
+    if y is not None:
+        _rows_of(y, gi, N, H)
+    elif want_y:
+        y = torch.empty(N, H, dtype=gi.dtype, device=gi.device)
     _check(lib().nsk_glr_step(_dtype_code(gi), N, H, S, _ptr(gi), _ptr(bias), _lengths_ptr(slots, N), _ptr(state), _ptr(y), _stream()), "nsk_glr_step")
     return y
 
