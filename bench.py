@@ -78,6 +78,9 @@ def parse():
     ap.add_argument("--gru", action="store_true",
                     help="time the recurrent workload instead: embedding + GRU(256) + output layer, batch 50, sequence "
                          "length 200, vocabulary 32768, 2 classes, forward + backward through time + clipped AdamW")
+    ap.add_argument("--linear-recurrence", action="store_true",
+                    help="time the classifier with gated linear recurrences on the same batches instead (2 blocks of 256 units, "
+                         "AdamW with 8-bit moments), and its tokens one by one")
     ap.add_argument("--layers", action="store_true", help="per-layer convolution table instead of the step benchmark")
     ap.add_argument("--grouped", action="store_true", help="table of grouped / depthwise convolution layers")
     return ap.parse_args()
@@ -402,6 +405,64 @@ def gru_bench(a):
                                  "hip_graph": graph is not None}, "loss": float(m.loss.item())}))
 
 
+def linear_recurrence_bench(a):
+    """The classifier of linear_recurrent.py on the recurrent workload's batches (200 steps of 50 sequences, vocabulary 32768, width 256, 2 classes), two blocks:
+    forward, backward, gradient clip and AdamW with 8-bit moments; then one token for each of the 50 sequences (latency of a step).  Prints one JSON line."""
+    import numpy as np
+    import torch
+    import nsk_inputs as gen
+    from paper_2409_11600_amd.linear_recurrent import GpuLinearRecurrentClassifier, TokenStream
+
+    T, N, E, H, V, K, L = 200, 50, 256, 256, 32768, 2, 2
+    dtype = "f32"
+    tokens = ((gen.uniform(77, 0, (T, N)) * V).astype(np.int32)) % V
+    labels = ((gen.uniform(77, 1, (N,)) * K).astype(np.int32)) % K
+    p = {"table": gen.normal(77, 2, (V, E)), "gamma": np.ones(H), "beta": np.zeros(H), "w_cls": gen.normal(77, 3, (K, H)) / np.sqrt(H), "b_cls": np.zeros(K)}
+    for k in range(L):
+        p |= {f"gamma{k}": np.ones(E), f"beta{k}": np.zeros(E), f"w_in{k}": gen.normal(77, 10 + k, (3 * H, E)) / np.sqrt(E),
+              f"b_in{k}": np.concatenate((1 + 2 * gen.normal(77, 20 + k, (H,)), np.zeros(2 * H)))}
+    p["w_out0"] = gen.normal(77, 30, (E, H)) / np.sqrt(H)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        m = GpuLinearRecurrentClassifier(tokens, labels, p, dtype=dtype)
+        for _ in range(max(a.warmup, 2)):
+            m.step()
+        stream.synchronize()
+        graph = None
+        if not a.no_graph:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                m.forward()
+                m.backward()
+        steps = max(a.steps, 20)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            if graph is not None:
+                graph.replay()
+                m.update()
+            else:
+                m.step()
+        torch.cuda.synchronize()
+        t1 = time.perf_counter()
+        # tokens one by one: a step of all 50 sequences, waited for each time
+        serve, one = TokenStream(m, N), torch.from_numpy(tokens[0]).cuda()
+        for _ in range(10):
+            serve.step(one)
+        torch.cuda.synchronize()
+        t2 = time.perf_counter()
+        for _ in range(100):
+            serve.step(one)
+            stream.synchronize()
+        t3 = time.perf_counter()
+    ms = (t1 - t0) * 1e3 / steps
+    print(json.dumps({"metric": "linear-recurrence classifier training step (embedding + 2 blocks of layer norm, product and recurrence + output layer, clipped 8-bit AdamW)",
+                      "value": N * steps / (t1 - t0), "unit": "sequences/s", "n_gpus": 1, "steps": steps, "warmup": a.warmup,
+                      "ms_per_step": ms, "higher_is_better": True, "dtype": dtype, "data": "synthetic",
+                      "config": {"workload": f"tokens [{T}, {N}], vocabulary {V}, width {E}, {L} blocks of {H} units, {K} classes", "hip_graph": graph is not None},
+                      "token_step_us": (t3 - t2) * 1e4, "loss": float(m.loss.item())}))
+
+
 def main():
     a = parse()
     if a.gpus != 1:
@@ -424,6 +485,9 @@ def main():
         return
     if a.gru:
         gru_bench(a)
+        return
+    if a.linear_recurrence:
+        linear_recurrence_bench(a)
         return
     if a.grouped:
         grouped_table()

@@ -138,3 +138,44 @@ def adamw8_step(w, grad, m, r, scale_m, scale_r, step, seed, index, lr, beta1, b
     qm, qr = held(mn, sm, (bits & np.uint64(0xFFFF)).astype(np.float64)), held(rn, sr, (bits >> np.uint64(16)).astype(np.float64))
     qr = np.where((rn > 0) & (qr < 2.0 ** -9), 2.0 ** -9, qr)
     return wn, qm, qr, sm, sr, mn, rn
+
+
+# ----------------------------------------------------------------------------- the classifier made of them
+
+def classifier_step(tokens, labels, p, lengths=None, eps=1e-5):
+    """Loss, logits, final states of each block and gradients of the classifier in paper_2409_11600_amd/linear_recurrent.py, whose parameter names these are."""
+    from . import gru, train
+    T, N = tokens.shape
+    L = sum(1 for k in p if k.startswith("w_in"))
+    rows = lambda a: a.reshape(T * N, -1)
+    s, u, gi, y, states, norms = [], [], [], [], [], []
+    stream = gru.embedding_fwd(tokens.reshape(-1), p["table"])
+    for k in range(L):
+        s.append(stream)
+        un, mean, invstd = layernorm_fwd(stream, p[f"gamma{k}"], p[f"beta{k}"], eps)
+        u.append(un)
+        norms.append((mean, invstd))
+        gi.append((un @ _f64(p[f"w_in{k}"]).T).reshape(T, N, -1))
+        yk, st = glr_fwd(gi[k], p[f"b_in{k}"], None, lengths)
+        y.append(yk)
+        states.append(st)
+        if k < L - 1:
+            stream = stream + rows(yk) @ _f64(p[f"w_out{k}"]).T
+    z, zm, zi = layernorm_fwd(states[-1][-1], p["gamma"], p["beta"], eps)
+    logits = train.linear_fwd(z, p["w_cls"], p["b_cls"])
+    loss, _ = train.softmax_xent_fwd(logits, labels)
+    dlogits = train.softmax_xent_bwd(logits, labels)
+    g = {}
+    g["w_cls"], g["b_cls"] = train.linear_wgrad(z, dlogits)
+    dh, g["gamma"], g["beta"] = layernorm_bwd(train.linear_dgrad(dlogits, p["w_cls"]), states[-1][-1], p["gamma"], zm, zi)
+    ds = None
+    for k in reversed(range(L)):
+        dy = None
+        if k < L - 1:
+            g[f"w_out{k}"] = ds.T @ rows(y[k])
+            dy = (ds @ _f64(p[f"w_out{k}"])).reshape(T, N, -1)
+        dgi, _ = glr_bwd(gi[k], p[f"b_in{k}"], states[k], dy, dh if k == L - 1 else None, lengths)
+        g[f"w_in{k}"], g[f"b_in{k}"] = rows(dgi).T @ u[k], dgi.sum(axis=(0, 1))
+        ds, g[f"gamma{k}"], g[f"beta{k}"] = layernorm_bwd(rows(dgi) @ _f64(p[f"w_in{k}"]), s[k], p[f"gamma{k}"], *norms[k], dsum=ds)
+    g["table"] = gru.embedding_bwd(tokens.reshape(-1), ds, p["table"].shape[0])
+    return loss, logits, [st[-1] for st in states], g

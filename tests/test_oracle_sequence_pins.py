@@ -126,3 +126,18 @@ def test_optimizer_step_of_both_precisions():
     b = S.adamw8_step(w, g, first[1], first[2], first[3], first[4], 2, 10, 0, 1e-3, 0.9, 0.999, 1e-8, 1e-2, 0.5, real=np.float64)
     assert np.abs(a[0] - b[0]).max() <= 1e-6 and np.array_equal(a[3], b[3]) and np.array_equal(a[4], b[4])
     assert np.mean(a[1] != b[1]) <= 0.01 and np.mean(a[2] != b[2]) <= 0.01
+
+
+def test_classifier_gradients_against_differences():
+    T, N, E, H, V, K, L = 4, 3, 5, 4, 7, 2, 2
+    r = rng(31)
+    tokens, labels, lengths = r.integers(0, V, (T, N)), r.integers(0, K, N), np.array([4, 1, 3])
+    p = {"table": r.normal(size=(V, E)), "gamma": 1 + 0.1 * r.normal(size=H), "beta": 0.1 * r.normal(size=H), "w_cls": r.normal(size=(K, H)), "b_cls": r.normal(size=K)}
+    for k in range(L):
+        p |= {f"gamma{k}": 1 + 0.1 * r.normal(size=E), f"beta{k}": 0.1 * r.normal(size=E), f"w_in{k}": r.normal(size=(3 * H, E)), f"b_in{k}": r.normal(size=3 * H)}
+    p["w_out0"] = r.normal(size=(E, H))
+    _, _, _, g = S.classifier_step(tokens, labels, p, lengths)
+    assert set(g) == set(p)
+    for name in p:
+        d = differences(lambda a: float(S.classifier_step(tokens, labels, {**p, name: a}, lengths)[0]), p[name], 1e-5)
+        assert np.abs(d - g[name]).max() <= 1e-6 * (1 + np.abs(g[name]).max()), name
