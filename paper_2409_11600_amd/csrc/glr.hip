@@ -29,30 +29,113 @@ __device__ inline float sigmoid(float a)
 }
 
 // How the work is laid out.  A lane has one channel of one sequence, a wavefront 64 of them (a tile) and a stretch of 16 steps, whose values it keeps in registers:
-// they are read once.  A stretch by itself takes a state h to A h + B; the wavefronts of a block take consecutive stretches, exchange (A, B) through LDS,
-// and each then goes through its steps again from the state that enters them.  A block goes on like this to the end of its segment.  Where tiles are few
-// and steps many, the steps are shared out to several segments; a launch before the main one finds (A, B) of each.
+// they are read once.  A stretch by itself takes a state h to A h + B; the wavefronts of a block take consecutive stretches (a segment) and exchange (A, B)
+// through LDS.  Where a tile has several segments, a block leaves its segment's (A, B) in memory, finds the state that enters it from what the blocks before it
+// left, leaves the state that leaves it, and then goes through its steps again, which are still in its registers.
+// The state behind a segment is A h + B with the h in front of it, whichever block computes that, so the results do not depend on how far the others are.
+// Waiting ends: blocks take numbers from a counter as they begin, and a block waits only for smaller numbers, whose blocks have begun and leave (A, B) before
+// they wait themselves.
 constexpr int kStretch = NSK_GLR_STRETCH;
 constexpr int kMostWaves = 16;
 struct Sizes {
     int T, N, H;
     int stretches;          // of the whole sequence
-    int per;                // of a segment
-    int segments;
+    int segments;           // of `waves` stretches
     unsigned tiles;
-    int together;           // neighbouring tiles on one XCD (place)
+    int groups;             // parts of the tiles that have counters of their own: 1 or 8
     int flat;               // tiles go on across sequences (1), or each sequence has tiles of its own (0)
     long long gi_t, gi_n, y_t, y_n;
 };
-// Blocks are handed to the eight XCDs in turn.  Where rows are not whole cache lines, neighbouring tiles share those at their ends and are given to the same XCD
-// (T=777, N=33, bf16 200 channels, us forward / backward: 23 / 29, otherwise 25 / 33); where they are, it costs a little (T=4096, N=4, fp32 256 channels: 22.4 / 33.8
-// and 21.0 / 30.1).
-__device__ inline void place(const Sizes &z, unsigned &tile, unsigned &segment)
+typedef unsigned long long u64;
+// What blocks leave for each other, all ones where nothing is yet: (A, B) and the state behind every segment of every tile.
+struct Exchange {
+    unsigned *counters;     // one in 16 words is used
+    u64 *ab;                // [segment][tile][64]
+    unsigned *behind;       // [segment][tile][64]
+};
+constexpr int kCounterWords = 8 * 16;
+size_t exchange_words(const Sizes &z) { return kCounterWords + (size_t)z.segments * z.tiles * 64 * 3; }
+Exchange exchange_at(void *workspace, const Sizes &z)
 {
-    const unsigned g = blockIdx.x, n = gridDim.x, x = g % 8, each = n / 8, more = n % 8;
-    const unsigned at = z.together ? x * each + (x < more ? x : more) + g / 8 : g;
-    segment = at / z.tiles;
-    tile = at - segment * z.tiles;
+    unsigned *const w = (unsigned *)workspace;
+    return {w, (u64 *)(w + kCounterWords), w + kCounterWords + (size_t)z.segments * z.tiles * 64 * 2};
+}
+__global__ __launch_bounds__(256) void glr_unset_kernel(unsigned *__restrict__ w, size_t words)
+{
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) w[i] = i < kCounterWords ? 0u : ~0u;
+}
+template <typename U> __device__ inline U seen(const U *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename U> __device__ inline void leave(U *p, U v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline unsigned bits(float v) { return __builtin_bit_cast(unsigned, v); }
+__device__ inline float value(unsigned v) { return __builtin_bit_cast(float, v); }
+constexpr unsigned kNaN = 0x7fc00000u;      // (in place of a NaN of all ones)
+
+// The tile of this block and which of its segments (in the order in which they wait for each other); false: there is nothing left for it.
+// Blocks are handed to the eight XCDs in turn.  With eight groups, neighbouring tiles, which share the cache lines at their ends if rows are not whole ones,
+// and all segments of a tile are on one XCD.
+__device__ inline bool place(const Sizes &z, const Exchange &x, unsigned &tile, int &segment)
+{
+    const unsigned group = z.groups == 8 ? blockIdx.x % 8 : 0, g = z.groups;
+    const unsigned each = z.tiles / g, more = z.tiles % g, count = each + (group < more), first = group * each + (group < more ? group : more);
+    unsigned number = z.groups == 8 ? blockIdx.x / 8 : blockIdx.x;
+    if (z.segments > 1) {
+        __shared__ unsigned taken;
+        if (threadIdx.x == 0) taken = __hip_atomic_fetch_add(x.counters + group * 16, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        number = __builtin_amdgcn_readfirstlane(taken);
+    }
+    if (count == 0 || number / count >= (unsigned)z.segments) return false;
+    segment = (int)(number / count);
+    tile = first + number % count;
+    return true;
+}
+
+// The state that enters a segment; called by one wavefront.  v0 enters the first one; A, B: this segment's.
+__device__ inline float entering(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B)
+{
+    if (z.segments == 1) return v0;
+    const int lane = threadIdx.x & 63;
+    const size_t step = (size_t)z.tiles * 64, at = (size_t)tile * 64 + lane;
+    const bool last = segment == z.segments - 1;
+    if (segment > 0 && !last) {
+        const u64 ab = (u64)bits(B) << 32 | bits(A);
+        leave(x.ab + segment * step + at, ab == ~0ull ? (u64)kNaN << 32 | kNaN : ab);
+    }
+    // back to the nearest segment whose state is there, over those whose (A, B) are, four at a time
+    float v = v0;
+    int j = segment - 1;
+    for (bool found = false; j >= 0 && !found;) {
+        unsigned behind[4];
+        u64 ab[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const size_t k = (size_t)(j - i > 0 ? j - i : 0) * step + at;
+            behind[i] = seen(x.behind + k);
+            ab[i] = seen(x.ab + k);
+        }
+        bool wait = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (found || wait || j < 0) continue;
+            if (!__builtin_amdgcn_ballot_w64(behind[i] == ~0u)) {
+                v = value(behind[i]);
+                found = true;
+            } else if (j > 0 && !__builtin_amdgcn_ballot_w64(ab[i] == ~0ull)) --j;
+            else wait = true;
+        }
+        if (wait) __builtin_amdgcn_s_sleep(2);
+    }
+    // and on from there
+#pragma unroll 4
+    for (int k = j + 1; k < segment; ++k) {
+        const u64 ab = seen(x.ab + k * step + at);
+        v = fmaf(value((unsigned)ab), v, value((unsigned)(ab >> 32)));
+    }
+    if (!last) {
+        const unsigned behind = bits(fmaf(A, v, B));
+        leave(x.behind + segment * step + at, behind == ~0u ? kNaN : behind);
+    }
+    return v;
 }
 // The channel of this lane.
 struct Lane {
@@ -193,255 +276,162 @@ __device__ inline void fold(const float (&f)[kStretch], const float (&x)[kStretc
     }
 }
 
-// (A, B) of a segment into ab[segment][2][N * H].
-template <typename T>
-__global__ __launch_bounds__(1024) void glr_fwd_fold_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, float *__restrict__ ab)
+// (A, B) of a block's stretches through LDS; the value that enters this wavefront's stretch, and the one that leaves the block's last.
+__device__ inline float join(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B, float &leaves)
 {
-    __shared__ float part[kMostWaves][2][64];
+    __shared__ float part[kMostWaves][2][64], enters[64];
     const int lane = threadIdx.x & 63, wave = wave_of_block(), waves = blockDim.x >> 6;
-    unsigned tile, segment;
-    place(z, tile, segment);
-    long long gi0, y0;
-    const Lane l = lane_of<T>(z, tile, gi0, y0);
-    const int len = steps_of(lengths, l, z.T);
-    const Bias b = bias_of(bias, z, l);
-    const int begin = segment * z.per;
-    float A = 1.f, B = 0.f;
-    // a wavefront takes a run of the segment's stretches, the runs are joined once
-    const int each = (z.per + waves - 1) / waves, first = begin + wave * each, most = begin + z.per < z.stretches ? begin + z.per : z.stretches;
-    const int last = first + each < most ? first + each : most;
-    for (int s = first; s < last; ++s) {
-        const int t0 = s * kStretch;
-        if (!any(t0 < len)) break;
-        float f[kStretch], x[kStretch], p, q;
-        load_gates<T, false>(gi + gi0 + t0 * z.gi_t, z, l, b, t0, f, x, f);
-        if (any(t0 + kStretch > len)) leave_state(len - t0, f, x);
-        apply_gates<false>(f, x, f);
-        fold(f, x, p, q);
-        A *= p;
-        B = p * B + q;
-    }
     part[wave][0][lane] = A;
     part[wave][1][lane] = B;
-    __syncthreads();
-    if (wave == 0 && l.there) {
-        for (int w = 1; w < waves; ++w) {
-            A *= part[w][0][lane];
-            B = part[w][0][lane] * B + part[w][1][lane];
+    lds_barrier();
+    if (z.segments > 1) {
+        if (wave == 0) {
+            A = 1.f;
+            B = 0.f;
+            for (int w = 0; w < waves; ++w) {
+                A *= part[w][0][lane];
+                B = fmaf(part[w][0][lane], B, part[w][1][lane]);
+            }
+            v0 = entering(z, x, tile, segment, v0, A, B);
+            enters[lane] = v0;
+            leaves = fmaf(A, v0, B);
         }
-        const long long all = (long long)z.N * z.H;
-        ab[(2LL * segment) * all + l.q] = A;
-        ab[(2LL * segment + 1) * all + l.q] = B;
+        lds_barrier();
+        v0 = enters[lane];
     }
+    float mine = v0;
+    for (int w = 0; w < waves; ++w) {
+        if (w == wave) mine = v0;
+        v0 = fmaf(part[w][0][lane], v0, part[w][1][lane]);
+    }
+    if (z.segments == 1) leaves = v0;
+    return mine;
 }
 
 template <typename T>
-__global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
-                                                      const float *__restrict__ h0, const float *__restrict__ ab, T *__restrict__ y, float *__restrict__ h_last,
-                                                      float *__restrict__ saved)
+__global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
+                                                       const float *__restrict__ h0, T *__restrict__ y, float *__restrict__ h_last, float *__restrict__ saved)
 {
-    __shared__ float part[2][kMostWaves][2][64];
-    const int lane = threadIdx.x & 63, wave = wave_of_block(), waves = blockDim.x >> 6;
-    unsigned tile, segment;
-    place(z, tile, segment);
+    unsigned tile;
+    int segment;
+    if (!place(z, ex, tile, segment)) return;
     long long gi0, y0;
     const Lane l = lane_of<T>(z, tile, gi0, y0);
     const long long all = (long long)z.N * z.H;
     const int len = steps_of(lengths, l, z.T);
     const Bias b = bias_of(bias, z, l);
-    const int begin = segment * z.per, end = begin + z.per < z.stretches ? begin + z.per : z.stretches;
-    float carry = h0 ? h0[l.q] : 0.f;
-    for (int s = 0; s < (int)segment; ++s) carry = ab[2LL * s * all + l.q] * carry + ab[(2LL * s + 1) * all + l.q];
-    for (int k = begin, turn = 0; k < end; k += waves, turn ^= 1) {
-        const int s = k + wave, t0 = s * kStretch;
-        float f[kStretch], x[kStretch], o[kStretch], A = 1.f, B = 0.f;
-        const bool some = s < end && any(t0 < len), ends = any(t0 + kStretch > len);
-        if (some) {
-            load_gates<T, true>(gi + gi0 + t0 * z.gi_t, z, l, b, t0, f, x, o);
-            if (ends) leave_state(len - t0, f, x);
-            apply_gates<true>(f, x, o);
-            fold(f, x, A, B);
-        }
-        part[turn][wave][0][lane] = A;
-        part[turn][wave][1][lane] = B;
-        // (a wavefront writes a buffer again only after the barrier of the next turn, which all pass behind their reads of this one)
-        lds_barrier();
-        float h = carry;
-        for (int w = 0; w < waves; ++w) {
-            if (w == wave) h = carry;
-            carry = part[turn][w][0][lane] * carry + part[turn][w][1][lane];
-        }
-        if (s >= end) continue;
-        if (saved && l.there) saved[s * all + l.q] = h;
-        if (!y) continue;
-        T *out = y + y0 + t0 * z.y_t;
-        if (some) {
-            Rows<T> rows{out, z.T - t0};
-#pragma unroll
-            for (int i = 0; i < kStretch; ++i) {
-                h = f[i] * h + x[i];
-                store<T>(o[i] * h, rows.at(), l.y, 0);
-                rows.move(z.y_t);
-            }
-        }
-        if (ends) store_zeros(out, z.y_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.y, 0, 1);
+    const int wave = wave_of_block(), s = segment * (int)(blockDim.x >> 6) + wave, t0 = s * kStretch;
+    float f[kStretch], x[kStretch], o[kStretch], A = 1.f, B = 0.f, leaves;
+    const bool mine = s < z.stretches, some = mine && any(t0 < len), ends = any(t0 + kStretch > len);
+    if (some) {
+        load_gates<T, true>(gi + gi0 + t0 * z.gi_t, z, l, b, t0, f, x, o);
+        if (ends) leave_state(len - t0, f, x);
+        apply_gates<true>(f, x, o);
+        fold(f, x, A, B);
     }
-    if (h_last && end == z.stretches && wave == 0 && l.there) h_last[l.q] = carry;
+    float h = join(z, ex, tile, segment, h0 ? h0[l.q] : 0.f, A, B, leaves);
+    if (h_last && segment == z.segments - 1 && wave == 0 && l.there) h_last[l.q] = leaves;
+    if (!mine) return;
+    if (saved && l.there) saved[s * all + l.q] = h;
+    if (!y) return;
+    T *out = y + y0 + t0 * z.y_t;
+    if (some) {
+        Rows<T> rows{out, z.T - t0};
+#pragma unroll
+        for (int i = 0; i < kStretch; ++i) {
+            h = f[i] * h + x[i];
+            store<T>(o[i] * h, rows.at(), l.y, 0);
+            rows.move(z.y_t);
+        }
+    }
+    if (ends) store_zeros(out, z.y_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.y, 0, 1);
 }
 
 // Backwards a stretch takes E, the gradient of the state that leaves it, to A E + B.  What a step needs for that: f, u = dy o, and with the states, which
 // come from the saved one, k = 1 - f and d = (h_{t-1} - c) f (1 - f).  The gradient of the gate o depends on nothing later.
 template <typename T>
-__global__ __launch_bounds__(1024) void glr_bwd_fold_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
-                                                           const T *__restrict__ dy, float *__restrict__ ab)
+__global__ __launch_bounds__(1024) void glr_bwd_kernel(Sizes z, Exchange ex, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
+                                                       const float *__restrict__ saved, const T *__restrict__ dy, const float *__restrict__ dh_last, T *__restrict__ dgi,
+                                                       float *__restrict__ dh0)
 {
-    __shared__ float part[kMostWaves][2][64];
-    const int lane = threadIdx.x & 63, wave = wave_of_block(), waves = blockDim.x >> 6;
-    unsigned tile, segment;
-    place(z, tile, segment);
-    long long gi0, y0;
-    const Lane l = lane_of<T>(z, tile, gi0, y0);
-    const int len = steps_of(lengths, l, z.T);
-    const Bias b = bias_of(bias, z, l);
-    const unsigned gate = (unsigned)z.H * (unsigned)sizeof(T);
-    const int begin = ++segment * z.per;       // (nothing comes before the first)
-    float A = 1.f, B = 0.f;
-    const int each = (z.per + waves - 1) / waves, first = begin + wave * each, most = begin + z.per < z.stretches ? begin + z.per : z.stretches;
-    const int last = first + each < most ? first + each : most;
-    for (int s = last - 1; s >= first; --s) {
-        const int t0 = s * kStretch;
-        if (!any(t0 < len)) continue;
-        float f[kStretch], o[kStretch], up[kStretch];
-        Rows<const T> in{gi + gi0 + t0 * z.gi_t, z.T - t0}, above{dy + y0 + t0 * z.y_t, dy ? z.T - t0 : 0};
-#pragma unroll
-        for (int i = 0; i < kStretch; ++i) {
-            const __amdgpu_buffer_rsrc_t r = in.at();
-            f[i] = load<T>(r, l.gi, 0);
-            o[i] = load<T>(r, l.gi, 2 * gate);
-            up[i] = load<T>(above.at(), l.y, 0);
-            in.move(z.gi_t);
-            above.move(z.y_t);
-        }
-#pragma unroll
-        for (int i = kStretch - 1; i >= 0; --i) {
-            const bool live = t0 + i < len;
-            const float g = live ? sigmoid(f[i] + b.f) : 1.f, u = live ? up[i] * sigmoid(o[i] + b.o) : 0.f;
-            B = g * (B + u);
-            A *= g;
-        }
-    }
-    part[wave][0][lane] = A;
-    part[wave][1][lane] = B;
-    __syncthreads();
-    if (wave == 0 && l.there) {
-        A = 1.f;
-        B = 0.f;
-        for (int w = waves - 1; w >= 0; --w) {
-            A *= part[w][0][lane];
-            B = part[w][0][lane] * B + part[w][1][lane];
-        }
-        const long long all = (long long)z.N * z.H;
-        ab[(2LL * segment) * all + l.q] = A;
-        ab[(2LL * segment + 1) * all + l.q] = B;
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(1024) void glr_bwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
-                                                      const float *__restrict__ saved, const T *__restrict__ dy, const float *__restrict__ dh_last,
-                                                      const float *__restrict__ ab, T *__restrict__ dgi, float *__restrict__ dh0)
-{
-    __shared__ float part[2][kMostWaves][2][64];
-    const int lane = threadIdx.x & 63, wave = wave_of_block(), waves = blockDim.x >> 6;
-    unsigned tile, segment;
-    place(z, tile, segment);
+    unsigned tile;
+    int segment;
+    if (!place(z, ex, tile, segment)) return;
     long long gi0, y0;
     const Lane l = lane_of<T>(z, tile, gi0, y0);
     const long long all = (long long)z.N * z.H;
     const int len = steps_of(lengths, l, z.T);
     const Bias b = bias_of(bias, z, l);
     const unsigned gate = (unsigned)z.H * (unsigned)sizeof(T);
-    const int begin = segment * z.per, end = begin + z.per < z.stretches ? begin + z.per : z.stretches;
-    float carry = dh_last ? dh_last[l.q] : 0.f;
-    for (int s = z.segments - 1; s > (int)segment; --s) carry = ab[2LL * s * all + l.q] * carry + ab[(2LL * s + 1) * all + l.q];
-    for (int k = end, turn = 0; k > begin; k -= waves, turn ^= 1) {
-        const int s = k - 1 - wave, t0 = s * kStretch;       // wavefront 0 has the last stretch
-        const bool mine = s >= begin, some = mine && any(t0 < len), ends = any(t0 + kStretch > len);
-        float f[kStretch], keep[kStretch], u[kStretch], d[kStretch], A = 1.f, B = 0.f;
-        const long long at = gi0 + t0 * z.gi_t;
-        if (some) {
-            // (arguments of f and o, c and dy are in f, keep, d and u until their step)
-            float h = saved[s * all + l.q];
-            Rows<const T> in{gi + at, z.T - t0}, above{dy + y0 + t0 * z.y_t, dy ? z.T - t0 : 0};
+    // segments and, in a block, wavefronts go from the end to the front
+    const int wave = wave_of_block(), waves = blockDim.x >> 6, s = (z.segments - segment) * waves - 1 - wave, t0 = s * kStretch;
+    const bool mine = s < z.stretches, some = mine && any(t0 < len), ends = any(t0 + kStretch > len);
+    float f[kStretch], keep[kStretch], u[kStretch], d[kStretch], q[kStretch], A = 1.f, B = 0.f, leaves;
+    const long long at = gi0 + t0 * z.gi_t;
+    if (some) {
+        // (arguments of f and o, c and dy are in f, keep, d and u until their step)
+        float h = saved[s * all + l.q];
+        Rows<const T> in{gi + at, z.T - t0}, above{dy + y0 + t0 * z.y_t, dy ? z.T - t0 : 0};
+#pragma unroll
+        for (int i = 0; i < kStretch; ++i) {
+            const __amdgpu_buffer_rsrc_t r = in.at();
+            f[i] = load<T>(r, l.gi, 0);
+            d[i] = load<T>(r, l.gi, gate);
+            keep[i] = load<T>(r, l.gi, 2 * gate);
+            u[i] = load<T>(above.at(), l.y, 0);
+            in.move(z.gi_t);
+            above.move(z.y_t);
+        }
+#pragma unroll
+        for (int i = 0; i < kStretch; ++i) {
+            f[i] += b.f;
+            d[i] += b.c;
+            keep[i] += b.o;
+        }
+        if (ends) {
+            leave_state(len - t0, f, d);
 #pragma unroll
             for (int i = 0; i < kStretch; ++i) {
-                const __amdgpu_buffer_rsrc_t r = in.at();
-                f[i] = load<T>(r, l.gi, 0);
-                d[i] = load<T>(r, l.gi, gate);
-                keep[i] = load<T>(r, l.gi, 2 * gate);
-                u[i] = load<T>(above.at(), l.y, 0);
-                in.move(z.gi_t);
-                above.move(z.y_t);
-            }
-#pragma unroll
-            for (int i = 0; i < kStretch; ++i) {
-                f[i] += b.f;
-                d[i] += b.c;
-                keep[i] += b.o;
-            }
-            if (ends) {
-                leave_state(len - t0, f, d);
-#pragma unroll
-                for (int i = 0; i < kStretch; ++i) {
-                    keep[i] = t0 + i < len ? keep[i] : 0.f;
-                    u[i] = t0 + i < len ? u[i] : 0.f;
-                }
-            }
-            Rows<T> out{dgi + at, z.T - t0};
-#pragma unroll
-            for (int i = 0; i < kStretch; ++i) {
-                const float c = d[i];
-                float o, shut, s, rest;
-                sigmoid2(keep[i], o, shut);
-                sigmoid2(f[i], s, rest);
-                f[i] = s;
-                keep[i] = rest;
-                d[i] = (h - c) * (s * rest);
-                h = s * h + rest * c;
-                u[i] *= o;
-                store<T>(u[i] * shut * h, out.at(), l.gi, 2 * gate);
-                out.move(z.gi_t);
-            }
-#pragma unroll
-            for (int i = kStretch - 1; i >= 0; --i) {
-                A *= f[i];
-                B = f[i] * (B + u[i]);
+                keep[i] = t0 + i < len ? keep[i] : 0.f;
+                u[i] = t0 + i < len ? u[i] : 0.f;
             }
         }
-        part[turn][wave][0][lane] = A;
-        part[turn][wave][1][lane] = B;
-        lds_barrier();
-        float E = carry;
-        for (int w = 0; w < waves; ++w) {
-            if (w == wave) E = carry;
-            carry = part[turn][w][0][lane] * carry + part[turn][w][1][lane];
-        }
-        if (!mine) continue;
-        if (some) {
-            Rows<T> out{dgi + at + (kStretch - 1) * z.gi_t, z.T - t0 - (kStretch - 1)};
 #pragma unroll
-            for (int i = kStretch - 1; i >= 0; --i) {
-                const __amdgpu_buffer_rsrc_t r = out.at();
-                const float G = E + u[i];
-                store<T>(G * d[i], r, l.gi, 0);
-                store<T>(G * keep[i], r, l.gi, gate);
-                E = f[i] * G;
-                out.move(-z.gi_t, -1);
-            }
+        for (int i = 0; i < kStretch; ++i) {
+            const float c = d[i];
+            float o, shut, s, rest;
+            sigmoid2(keep[i], o, shut);
+            sigmoid2(f[i], s, rest);
+            f[i] = s;
+            keep[i] = rest;
+            d[i] = (h - c) * (s * rest);
+            h = s * h + rest * c;
+            u[i] *= o;
+            q[i] = u[i] * shut * h;     // (stored at the end: the loads that look for other blocks' values would wait for it)
         }
-        if (ends) store_zeros(dgi + at, z.gi_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.gi, gate, 3);
+#pragma unroll
+        for (int i = kStretch - 1; i >= 0; --i) {
+            A *= f[i];
+            B = f[i] * (B + u[i]);
+        }
     }
-    if (dh0 && begin == 0 && wave == 0 && l.there) dh0[l.q] = carry;
+    float E = join(z, ex, tile, segment, dh_last ? dh_last[l.q] : 0.f, A, B, leaves);
+    if (dh0 && segment == z.segments - 1 && wave == 0 && l.there) dh0[l.q] = leaves;
+    if (!mine) return;
+    if (some) {
+        Rows<T> out{dgi + at + (kStretch - 1) * z.gi_t, z.T - t0 - (kStretch - 1)};
+#pragma unroll
+        for (int i = kStretch - 1; i >= 0; --i) {
+            const __amdgpu_buffer_rsrc_t r = out.at();
+            const float G = E + u[i];
+            store<T>(G * d[i], r, l.gi, 0);
+            store<T>(G * keep[i], r, l.gi, gate);
+            store<T>(q[i], r, l.gi, 2 * gate);
+            E = f[i] * G;
+            out.move(-z.gi_t, -1);
+        }
+    }
+    if (ends) store_zeros(dgi + at, z.gi_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.gi, gate, 3);
 }
 
 template <typename T>
@@ -488,41 +478,37 @@ int check(const nsk_glr_desc_t *desc, nsk_glr_desc_t &d)
     return NSK_OK;
 }
 
-// Tiles, wavefronts of a block and segments of a call.
+// Tiles, segments and wavefronts of a call.
 struct Plan {
     Sizes z;
     int waves;
+    unsigned blocks;
 };
 Plan plan_of(const nsk_glr_desc_t &d)
 {
     Plan p{};
     const long long es = d.dtype == NSK_BF16 ? 2 : 4;
-    p.z = {d.T, d.N, d.H, ceil_div(d.T, kStretch), 0, 1, 0, 0, 0, d.gi_t, d.gi_n, d.y_t, d.y_n};
-    p.z.together = d.H * es % 128 != 0 || (d.gi_t | d.gi_n) * es % 128 != 0;
+    p.z = {d.T, d.N, d.H, ceil_div(d.T, kStretch), 1, 0, 1, 0, d.gi_t, d.gi_n, d.y_t, d.y_n};
     // a tile reaches over 63 / H + 1 further sequences, whose offsets have to fit 30 bits (those of a single sequence do)
     const long long over = d.H < 64 ? 63 / d.H + 1 : 1, stride = d.gi_n > d.y_n ? d.gi_n : d.y_n;
     p.z.flat = stride < (1LL << 30) && (over * stride + d.H) * es < (1LL << 30);
     const long long tiles = p.z.flat ? ((long long)d.N * d.H + 63) / 64 : (long long)d.N * ((d.H + 63) / 64);
     p.z.tiles = (unsigned)tiles;
-    // One round of 16 wavefronts takes a compute unit about 5 us, 0.31 a stretch.  With a block for every unit or more, blocks go through all steps of their tile;
-    // with fewer, the launch before the main one costs about 6 us and 0.6 of the main one's work, but all units share the work: 6 + 1.6 * 0.31 / 256 * tiles * stretches
-    // against 0.31 * stretches.  (us forward / backward, whole / shared out: T=65536, N=1, bf16 512 channels 1514 / 2126 and 92 / 147; T=4096, N=4, fp32 256 channels
-    // 80 / 119 and 21 / 30; T=200, N=50, fp32 256 channels 9.2 / 14.6 and 12.6 / 18.8.)
-    const bool share = tiles < 160 && (long long)p.z.stretches * (160 - tiles) > 3072;
-    // Wavefronts: as many as there are stretches for a block that has a unit to itself (T=200, N=50, fp32 256 channels, 13 / 8 of them: 9.2 and 10.2 us forward); fewer
-    // where several blocks share a unit, whose barriers then come at different times (T=200, N=512, bf16 768 channels, 4 / 8 / 13 of them: 77, 77, 100 us forward, 129, 133,
-    // 150 backward; T=2048, N=32, bf16 768 channels, 4 / 8 / 16: 122, 111, 117 and 194, 187, 183).
-    const int most = share ? 8 : tiles <= 256 ? kMostWaves : tiles < 1024 ? 8 : 4;
-    p.waves = p.z.stretches < most ? p.z.stretches : most;
-    const int rounds = ceil_div(p.z.stretches, p.waves);
-    long long want = share ? (512 + tiles - 1) / tiles : 1;
-    if (want > rounds) want = rounds;
-    // (two blocks a compute unit, what the backward pass has room for: more come in a second turn)
-    p.z.per = ceil_div(rounds, (int)want) * p.waves;
-    p.z.segments = ceil_div(p.z.stretches, p.z.per);
+    p.z.groups = tiles >= 64 ? 8 : 1;
+    const int most = 8;
+    p.z.segments = p.z.stretches <= kMostWaves && tiles <= 256 ? 1 : ceil_div(p.z.stretches, most);
+    p.waves = ceil_div(p.z.stretches, p.z.segments);
+    p.z.segments = ceil_div(p.z.stretches, p.waves);
+    p.blocks = p.z.groups == 8 ? 8 * (unsigned)ceil_div((int)tiles, 8) * (unsigned)p.z.segments : (unsigned)tiles * (unsigned)p.z.segments;
     return p;
 }
-size_t workspace_of(const Plan &p) { return p.z.segments > 1 ? (size_t)p.z.segments * 2 * p.z.N * p.z.H * sizeof(float) : 0; }
+size_t workspace_of(const Plan &p) { return p.z.segments > 1 ? exchange_words(p.z) * sizeof(unsigned) : 0; }
+// Puts the marks where blocks will look for each other's values.
+void unset(const Plan &p, void *workspace, hipStream_t st)
+{
+    const size_t words = exchange_words(p.z), blocks = (words + 1023) / 1024;
+    if (p.z.segments > 1) hipLaunchKernelGGL(glr_unset_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, (unsigned *)workspace, words);
+}
 
 }  // namespace
 }  // namespace nsk
@@ -554,13 +540,13 @@ int nsk_glr_fwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, c
         return NSK_ERR_ALIGNMENT;
     const Plan p = plan_of(d);
     if (p.z.segments > 1 && (!workspace || workspace_bytes < workspace_of(p))) return NSK_ERR_WORKSPACE;
-    const dim3 grid(p.z.tiles * (unsigned)p.z.segments), block((unsigned)p.waves * 64);
+    const dim3 grid(p.blocks), block((unsigned)p.waves * 64);
     hipStream_t st = (hipStream_t)stream;
-    float *ab = (float *)workspace;
+    const Exchange ex = exchange_at(workspace, p.z);
+    unset(p, workspace, st);
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        if (p.z.segments > 1) hipLaunchKernelGGL(glr_fwd_fold_kernel<T>, dim3(p.z.tiles * (unsigned)(p.z.segments - 1)), block, 0, st, p.z, (const T *)gi, bias, lengths, ab);
-        hipLaunchKernelGGL(glr_fwd_kernel<T>, grid, block, 0, st, p.z, (const T *)gi, bias, lengths, h0, ab, (T *)y, h_last, saved);
+        hipLaunchKernelGGL(glr_fwd_kernel<T>, grid, block, 0, st, p.z, ex, (const T *)gi, bias, lengths, h0, (T *)y, h_last, saved);
     };
     if (d.dtype == NSK_BF16) launch(bf16_t{});
     else launch(float{});
@@ -578,13 +564,13 @@ int nsk_glr_bwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, c
         return NSK_ERR_ALIGNMENT;
     const Plan p = plan_of(d);
     if (p.z.segments > 1 && (!workspace || workspace_bytes < workspace_of(p))) return NSK_ERR_WORKSPACE;
-    const dim3 grid(p.z.tiles * (unsigned)p.z.segments), block((unsigned)p.waves * 64);
+    const dim3 grid(p.blocks), block((unsigned)p.waves * 64);
     hipStream_t st = (hipStream_t)stream;
-    float *ab = (float *)workspace;
+    const Exchange ex = exchange_at(workspace, p.z);
+    unset(p, workspace, st);
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        if (p.z.segments > 1) hipLaunchKernelGGL(glr_bwd_fold_kernel<T>, dim3(p.z.tiles * (unsigned)(p.z.segments - 1)), block, 0, st, p.z, (const T *)gi, bias, lengths, (const T *)dy, ab);
-        hipLaunchKernelGGL(glr_bwd_kernel<T>, grid, block, 0, st, p.z, (const T *)gi, bias, lengths, saved, (const T *)dy, dh_last, ab, (T *)dgi, dh0);
+        hipLaunchKernelGGL(glr_bwd_kernel<T>, grid, block, 0, st, p.z, ex, (const T *)gi, bias, lengths, saved, (const T *)dy, dh_last, (T *)dgi, dh0);
     };
     if (d.dtype == NSK_BF16) launch(bf16_t{});
     else launch(float{});
