@@ -517,7 +517,8 @@ typedef struct {
 /* Bytes of `saved`: float [ceil(T / NSK_GLR_STRETCH)][N][H], the states that enter the steps 0, 16, 32, ...; 0 for an invalid
  * descriptor.  Host only. */
 size_t nsk_glr_saved_bytes(const nsk_glr_desc_t *desc);
-/* Workspace of a pass (NSK_PASS_FWD, NSK_PASS_DGRAD); may be 0.  Host only. */
+/* Workspace of a pass (NSK_PASS_FWD, NSK_PASS_DGRAD); 0 where a block has all steps of its channels.  Blocks that share a sequence hand states on through
+ * it: a call has it to itself while it runs; what it held before does not matter.  Host only. */
 size_t nsk_glr_workspace_bytes(const nsk_glr_desc_t *desc, int pass);
 /* h0: float [N,H], NULL: zeros.  y: NULL if only the last state is wanted; h_last: NULL or float [N,H], the state after the
  * last step; one of the two at least.  saved: NULL where no backward pass follows. */

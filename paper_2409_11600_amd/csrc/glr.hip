@@ -42,7 +42,7 @@ struct Sizes {
     int stretches;          // of the whole sequence
     int segments;           // of `waves` stretches
     unsigned tiles;
-    int groups;             // parts of the tiles that have counters of their own: 1 or 8
+    int groups;             // parts of the tiles that have counters of their own
     int flat;               // tiles go on across sequences (1), or each sequence has tiles of its own (0)
     long long gi_t, gi_n, y_t, y_n;
 };
@@ -53,7 +53,7 @@ struct Exchange {
     u64 *ab;                // [segment][tile][64]
     unsigned *behind;       // [segment][tile][64]
 };
-constexpr int kCounterWords = 8 * 16;
+constexpr int kMostGroups = 32, kCounterWords = kMostGroups * 16;
 size_t exchange_words(const Sizes &z) { return kCounterWords + (size_t)z.segments * z.tiles * 64 * 3; }
 Exchange exchange_at(void *workspace, const Sizes &z)
 {
@@ -71,13 +71,14 @@ __device__ inline float value(unsigned v) { return __builtin_bit_cast(float, v);
 constexpr unsigned kNaN = 0x7fc00000u;      // (in place of a NaN of all ones)
 
 // The tile of this block and which of its segments (in the order in which they wait for each other); false: there is nothing left for it.
-// Blocks are handed to the eight XCDs in turn.  With eight groups, neighbouring tiles, which share the cache lines at their ends if rows are not whole ones,
-// and all segments of a tile are on one XCD.
+// Blocks are handed to the eight XCDs in turn: with 8 or 32 groups, all segments of a tile are on one XCD, and so are most neighbouring tiles, which share the cache
+// lines at their ends where rows are not whole ones.  (us forward / backward, 1 / 8 / 32 groups, T=2048, N=32, bf16 768 channels, 6144 blocks of 4 wavefronts: 165 / 176,
+// 89 / 143, 86 / 142: a counter gives out a number in 12 ns; ragged T=777, N=33, fp32 201 channels: 25 / 43, 19 / 37, 20 / 42.)
 __device__ inline bool place(const Sizes &z, const Exchange &x, unsigned &tile, int &segment)
 {
-    const unsigned group = z.groups == 8 ? blockIdx.x % 8 : 0, g = z.groups;
+    const unsigned g = z.groups, group = blockIdx.x % g;
     const unsigned each = z.tiles / g, more = z.tiles % g, count = each + (group < more), first = group * each + (group < more ? group : more);
-    unsigned number = z.groups == 8 ? blockIdx.x / 8 : blockIdx.x;
+    unsigned number = blockIdx.x / g;
     if (z.segments > 1) {
         __shared__ unsigned taken;
         if (threadIdx.x == 0) taken = __hip_atomic_fetch_add(x.counters + group * 16, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -494,12 +495,17 @@ Plan plan_of(const nsk_glr_desc_t &d)
     p.z.flat = stride < (1LL << 30) && (over * stride + d.H) * es < (1LL << 30);
     const long long tiles = p.z.flat ? ((long long)d.N * d.H + 63) / 64 : (long long)d.N * ((d.H + 63) / 64);
     p.z.tiles = (unsigned)tiles;
-    p.z.groups = tiles >= 64 ? 8 : 1;
-    const int most = 8;
-    p.z.segments = p.z.stretches <= kMostWaves && tiles <= 256 ? 1 : ceil_div(p.z.stretches, most);
+    p.z.groups = tiles >= 256 ? kMostGroups : tiles >= 8 ? 8 : 1;
+    // Small blocks where there are many: theirs fill the compute units evenly and wait at different times.  Large ones where tiles are few: fewer segments have to
+    // find each other.  (us forward / backward with 4 / 8 / 16 wavefronts: T=2048, N=32, bf16 768 channels 86 / 142, 89 / 157, 111 / 171; T=65536, N=1, bf16 512 channels
+    // 122 / 154, 84 / 128, 85 / 127; the same with 64 channels 78 / 80, 44 / 47, 29 / 32.)  One segment and no exchange where a block can take all stretches: up to 8 always (T=128,
+    // N=256, bf16 1280 channels, one / two segments: 79 / 137, 84 / 138), up to 16 while every block has a compute unit to itself (T=200, N=50, fp32 256 channels: 11.0 / 14.9,
+    // 14.0 / 17.1; T=200, N=512, bf16 768 channels, 4 segments of 4 stretches otherwise: 86 / 140, as one 99 / 150).
+    const int most = tiles > 256 ? 4 : tiles >= 8 ? 8 : kMostWaves;
+    p.z.segments = p.z.stretches <= 8 || (p.z.stretches <= kMostWaves && tiles <= 256) ? 1 : ceil_div(p.z.stretches, most);
     p.waves = ceil_div(p.z.stretches, p.z.segments);
     p.z.segments = ceil_div(p.z.stretches, p.waves);
-    p.blocks = p.z.groups == 8 ? 8 * (unsigned)ceil_div((int)tiles, 8) * (unsigned)p.z.segments : (unsigned)tiles * (unsigned)p.z.segments;
+    p.blocks = (unsigned)(p.z.groups * ((tiles + p.z.groups - 1) / p.z.groups) * p.z.segments);
     return p;
 }
 size_t workspace_of(const Plan &p) { return p.z.segments > 1 ? exchange_words(p.z) * sizeof(unsigned) : 0; }

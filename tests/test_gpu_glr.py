@@ -263,6 +263,52 @@ def test_tokens_one_by_one_are_the_sequence():
     in_bound(host(y), wy, ey + U * np.abs(wy), "y")
 
 
+LONG = [(300, 1, 64), (2100, 3, 24), (4000, 20, 40), (20000, 1, 1), (700, 90, 200)]      # several segments: one tile, two, 13, one, 282
+
+
+@pytest.mark.parametrize("T,N,H", LONG)
+def test_long_sequences_give_the_same_bits_every_time(T, N, H):
+    """Whatever the blocks find of each other's values, and whatever runs beside them: two streams at once, each with scratch of its own."""
+    gi, dy, bias, h0, dh_last, lengths = make(37, T, N, H, "bf16", True)
+
+    def run(ws):
+        y, h, saved = B.glr_fwd(gi, bias, h0=h0, lengths=lengths, ws=ws)
+        return (y, h, saved, *B.glr_bwd(gi, saved, bias, dy=dy, dh_last=dh_last, lengths=lengths, ws=ws))
+
+    want = run(B.Workspace("cuda:0"))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    spaces = [B.Workspace("cuda:0") for _ in streams]
+    for _ in range(6):
+        for stream, ws in zip(streams, spaces):
+            with torch.cuda.stream(stream):
+                got.append(run(ws))
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("T,N,H", LONG)
+def test_long_sequences_that_hold_the_mark_of_nothing(T, N, H):
+    """Values whose bits are all ones, a NaN, which is also what the scratch memory holds where no block has left anything yet: the NaN goes on, in its channel alone."""
+    gi, dy, bias, h0, dh_last, _ = make(41, T, N, H, "f32", False)
+    want = B.glr_fwd(gi, bias, h0=h0)
+    want += B.glr_bwd(gi, want[2], bias, dy=dy, dh_last=dh_last)
+    for where in (slice(0, H), slice(H, 2 * H), slice(2 * H, 3 * H)):
+        bad, bad_dy = gi.clone(), dy.clone()
+        at = T // 2
+        bad[at, 0, where][0:1].view(torch.int32).fill_(-1)
+        bad_dy[at, 0, 0:1].view(torch.int32).fill_(-1)
+        y, h, saved = B.glr_fwd(bad, bias, h0=h0)
+        dgi, dh0 = B.glr_bwd(bad, saved, bias, dy=bad_dy, dh_last=dh_last)
+        torch.cuda.synchronize()
+        assert dh0[0, 0].isnan() and y[at, 0, 0].isnan()
+        keep = torch.ones((N, H), dtype=torch.bool, device="cuda:0")
+        keep[0, 0] = False
+        assert torch.equal(y[:, keep], want[0][:, keep]) and torch.equal(h[keep], want[1][keep]) and torch.equal(dh0[keep], want[4][keep])
+        assert torch.equal(dgi[..., :H][:, keep], want[3][..., :H][:, keep]) and torch.equal(dgi[..., 2 * H:][:, keep], want[3][..., 2 * H:][:, keep])
+
+
 def test_offsets_beyond_32_bits():
     """Rows whose offsets, in elements and in bytes, pass 2^31 and 2^32: the last sequences of a batch-major tensor of 2^31 + elements against the same alone."""
     H, T = 128, 700
