@@ -213,8 +213,8 @@ __device__ inline Bias bias_of(const float *bias, const Sizes &z, const Lane &l)
     return {bias[l.c], bias[z.H + (long long)l.c], bias[2LL * z.H + l.c]};
 }
 
-// Loads of a stretch: gates f and c into f and x, o if asked for, biases added.
-template <typename T, bool WITH_O>
+// Loads of a stretch: gates f, c and o into f, x and o, biases added.
+template <typename T>
 __device__ inline void load_gates(const T *gi, const Sizes &z, const Lane &l, const Bias &b, int t0, float (&f)[kStretch], float (&x)[kStretch], float (&o)[kStretch])
 {
     const unsigned gate = (unsigned)z.H * (unsigned)sizeof(T);
@@ -224,14 +224,14 @@ __device__ inline void load_gates(const T *gi, const Sizes &z, const Lane &l, co
         const __amdgpu_buffer_rsrc_t r = in.at();
         f[i] = load<T>(r, l.gi, 0);
         x[i] = load<T>(r, l.gi, gate);
-        if (WITH_O) o[i] = load<T>(r, l.gi, 2 * gate);
+        o[i] = load<T>(r, l.gi, 2 * gate);
         in.move(z.gi_t);
     }
 #pragma unroll
     for (int i = 0; i < kStretch; ++i) {
         f[i] += b.f;
         x[i] += b.c;
-        if (WITH_O) o[i] += b.o;
+        o[i] += b.o;
     }
 }
 // Steps from `live` on leave the state: f = sigmoid(inf) = 1, (1 - f) c = 0.
@@ -244,7 +244,7 @@ __device__ inline void leave_state(int live, float (&f)[kStretch], float (&x)[kS
     }
 }
 // Arguments into f, x = (1 - f) c and o.
-template <bool WITH_O> __device__ inline void apply_gates(float (&f)[kStretch], float (&x)[kStretch], float (&o)[kStretch])
+__device__ inline void apply_gates(float (&f)[kStretch], float (&x)[kStretch], float (&o)[kStretch])
 {
 #pragma unroll
     for (int i = 0; i < kStretch; ++i) {
@@ -252,7 +252,7 @@ template <bool WITH_O> __device__ inline void apply_gates(float (&f)[kStretch], 
         sigmoid2(f[i], s, keep);
         x[i] *= keep;
         f[i] = s;
-        if (WITH_O) o[i] = sigmoid(o[i]);
+        o[i] = sigmoid(o[i]);
     }
 }
 // Zeros into the steps of a stretch that a lane's sequence does not have, behind what went there before.
@@ -309,6 +309,10 @@ __device__ inline float join(const Sizes &z, const Exchange &x, unsigned tile, i
     return mine;
 }
 
+// Bound by memory where tiles are many (3 + 1 elements and 1/4 byte a step and channel): bf16, T=2048, N=32, 768 channels 86 us, 4.8 TB/s of what a copy reaches 5.1 of;
+// the vector unit, with four transcendental of some 25 instructions a step, is half busy.  By the hand-over where tiles are few: bf16, T=65536, N=1, 512 channels
+// 85 us (3.3 TB/s; wavefronts wait two thirds of their time, a tile gets on by a segment in 0.16 us); and by one chain of loads, gates and stores where a call is short: fp32, T=200,
+// N=50, 256 channels 11 us for 42 MB.  (Wider look-backs, 8 or 16 segments at a time or 4 by each wavefront, cost more in traffic than they gave: 92, 97, 118 us for the long one.)
 template <typename T>
 __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
                                                        const float *__restrict__ h0, T *__restrict__ y, float *__restrict__ h_last, float *__restrict__ saved)
@@ -325,9 +329,9 @@ __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, con
     float f[kStretch], x[kStretch], o[kStretch], A = 1.f, B = 0.f, leaves;
     const bool mine = s < z.stretches, some = mine && any(t0 < len), ends = any(t0 + kStretch > len);
     if (some) {
-        load_gates<T, true>(gi + gi0 + t0 * z.gi_t, z, l, b, t0, f, x, o);
+        load_gates<T>(gi + gi0 + t0 * z.gi_t, z, l, b, t0, f, x, o);
         if (ends) leave_state(len - t0, f, x);
-        apply_gates<true>(f, x, o);
+        apply_gates(f, x, o);
         fold(f, x, A, B);
     }
     float h = join(z, ex, tile, segment, h0 ? h0[l.q] : 0.f, A, B, leaves);
@@ -348,6 +352,7 @@ __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, con
     if (ends) store_zeros(out, z.y_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.y, 0, 1);
 }
 
+// bf16, T=2048, N=32, 768 channels 142 us, 5.1 TB/s; fp32 with lengths and odd rows, T=777, N=33, 201 channels 36 us; T=200, N=50, fp32 256 channels 14.9 us.
 // Backwards a stretch takes E, the gradient of the state that leaves it, to A E + B.  What a step needs for that: f, u = dy o, and with the states, which
 // come from the saved one, k = 1 - f and d = (h_{t-1} - c) f (1 - f).  The gradient of the gate o depends on nothing later.
 template <typename T>
@@ -475,7 +480,8 @@ int check(const nsk_glr_desc_t *desc, nsk_glr_desc_t &d)
     if (d.T <= 0 || d.N <= 0 || d.H <= 0 || d.H > (1 << 26) || (d.dtype != NSK_F32 && d.dtype != NSK_BF16)) return NSK_ERR_BAD_DESC;
     if ((long long)d.N * d.H > (1LL << 60) / d.T) return NSK_ERR_BAD_DESC;
     if (!rows_apart(d.T, d.N, 3LL * d.H, d.gi_t, d.gi_n) || !rows_apart(d.T, d.N, d.H, d.y_t, d.y_n)) return NSK_ERR_BAD_DESC;
-    if ((long long)d.N * ((d.H + 63) / 64) > 0x7fffffff) return NSK_ERR_UNSUPPORTED;
+    // (a launch has fewer than 2^32 threads: one a channel and stretch at most)
+    if (d.T > 1 << 30 || (long long)d.N * ((d.H + 63) / 64) > (3LL << 30) / ((d.T + kStretch - 1) / kStretch + kMostWaves) / 64) return NSK_ERR_UNSUPPORTED;
     return NSK_OK;
 }
 
@@ -589,7 +595,7 @@ int nsk_glr_step(int dtype, int N, int H, int S, const void *gi, const float *bi
     if (!gi || !state) return NSK_ERR_NULL;
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(slots) || unaligned16(state) || unaligned16(y)) return NSK_ERR_ALIGNMENT;
     const unsigned tiles = (unsigned)ceil_div(H, 64);
-    if ((long long)tiles * N > 0x7fffffff) return NSK_ERR_UNSUPPORTED;
+    if ((long long)tiles * N >= 1 << 26) return NSK_ERR_UNSUPPORTED;        // (2^32 threads)
     const dim3 grid(tiles * (unsigned)N);
     if (dtype == NSK_BF16)
         hipLaunchKernelGGL(glr_step_kernel<bf16_t>, grid, dim3(64), 0, (hipStream_t)stream, H, S, (const bf16_t *)gi, bias, slots, state, (bf16_t *)y, tiles);

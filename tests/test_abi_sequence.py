@@ -23,6 +23,7 @@ def test_layer_norm_refusals():
         assert L.nsk_layernorm_bwd_workspace_bytes(desc(**bad)) == 0
         assert L.nsk_layernorm_fwd(desc(**bad), *fwd) == B.NSK_ERR_BAD_DESC
         assert L.nsk_layernorm_bwd(desc(**bad), *bwd) == B.NSK_ERR_BAD_DESC
+    assert L.nsk_layernorm_fwd(desc(C=(1 << 24) + 1), *fwd) == B.NSK_ERR_UNSUPPORTED and L.nsk_layernorm_bwd(desc(C=(1 << 24) + 1), *bwd) == B.NSK_ERR_UNSUPPORTED
     for eps in (0.0, -1.0, float("nan")):
         assert L.nsk_layernorm_fwd(desc(eps=eps), *fwd) == B.NSK_ERR_BAD_DESC
     assert L.nsk_layernorm_fwd(None, *fwd) == B.NSK_ERR_NULL and L.nsk_layernorm_bwd(None, *bwd) == B.NSK_ERR_NULL
@@ -52,6 +53,9 @@ def test_recurrence_refusals():
         assert L.nsk_glr_saved_bytes(desc(**bad)) == 0 and L.nsk_glr_workspace_bytes(desc(**bad), B.NSK_PASS_FWD) == 0, bad
         assert L.nsk_glr_fwd(desc(**bad), *fwd) == B.NSK_ERR_BAD_DESC, bad
         assert L.nsk_glr_bwd(desc(**bad), *bwd) == B.NSK_ERR_BAD_DESC, bad
+    for much in (dict(T=(1 << 30) + 1), dict(T=1 << 20, N=1 << 14, H=64), dict(T=1, N=1 << 26, H=1)):       # more threads than a launch has
+        assert L.nsk_glr_fwd(desc(**much), *fwd) == B.NSK_ERR_UNSUPPORTED and L.nsk_glr_bwd(desc(**much), *bwd) == B.NSK_ERR_UNSUPPORTED, much
+        assert L.nsk_glr_workspace_bytes(desc(**much), B.NSK_PASS_FWD) == 0
     assert L.nsk_glr_saved_bytes(desc()) == 3 * 3 * 8 * 4
     assert L.nsk_glr_saved_bytes(desc(gi_t=24, gi_n=960, y_t=8, y_n=320)) == 3 * 3 * 8 * 4      # batch-major
     assert L.nsk_glr_saved_bytes(desc(T=1, gi_t=1, gi_n=24)) == 3 * 8 * 4                        # the stride of a single step says nothing
@@ -79,6 +83,7 @@ def test_token_refusals():
     args = [P] * 5 + [None]
     for sizes in ((B.NSK_F32, 0, 8, 4), (B.NSK_F32, 2, 0, 4), (B.NSK_F32, 2, 8, 0), (3, 2, 8, 4), (B.NSK_BF16, -1, 8, 4)):
         assert L.nsk_glr_step(*sizes, *args) == B.NSK_ERR_BAD_DESC
+    assert L.nsk_glr_step(B.NSK_F32, 1 << 26, 8, 4, *args) == B.NSK_ERR_UNSUPPORTED
     for k in (0, 3):                     # gi, state
         assert L.nsk_glr_step(B.NSK_F32, 2, 8, 4, *replaced(args, k, None)) == B.NSK_ERR_NULL
     for k in range(5):
