@@ -60,9 +60,11 @@ Exchange exchange_at(void *workspace, const Sizes &z)
     unsigned *const w = (unsigned *)workspace;
     return {w, (u64 *)(w + kCounterWords), w + kCounterWords + (size_t)z.segments * z.tiles * 64 * 2};
 }
-__global__ __launch_bounds__(256) void glr_unset_kernel(unsigned *__restrict__ w, size_t words)
+// (vectors of four words; the counters are whole ones)
+__global__ __launch_bounds__(256) void glr_unset_kernel(unsigned *__restrict__ w, size_t vectors)
 {
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) w[i] = i < kCounterWords ? 0u : ~0u;
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < vectors; i += (size_t)gridDim.x * 256) ((u32x4 *)w)[i] = u32x4(i < kCounterWords / 4 ? 0u : ~0u);
 }
 template <typename U> __device__ inline U seen(const U *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <typename U> __device__ inline void leave(U *p, U v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -518,8 +520,9 @@ size_t workspace_of(const Plan &p) { return p.z.segments > 1 ? exchange_words(p.
 // Puts the marks where blocks will look for each other's values.
 void unset(const Plan &p, void *workspace, hipStream_t st)
 {
-    const size_t words = exchange_words(p.z), blocks = (words + 1023) / 1024;
-    if (p.z.segments > 1) hipLaunchKernelGGL(glr_unset_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, (unsigned *)workspace, words);
+    if (p.z.segments == 1) return;
+    const size_t vectors = exchange_words(p.z) / 4, blocks = (vectors + 255) / 256;
+    hipLaunchKernelGGL(glr_unset_kernel, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, st, (unsigned *)workspace, vectors);
 }
 
 }  // namespace
