@@ -504,12 +504,14 @@ Plan plan_of(const nsk_glr_desc_t &d)
     const long long tiles = p.z.flat ? ((long long)d.N * d.H + 63) / 64 : (long long)d.N * ((d.H + 63) / 64);
     p.z.tiles = (unsigned)tiles;
     p.z.groups = tiles >= 256 ? kMostGroups : tiles >= 8 ? 8 : 1;
-    // Small blocks where there are many: theirs fill the compute units evenly and wait at different times.  Large ones where tiles are few: fewer segments have to
-    // find each other.  (us forward / backward with 4 / 8 / 16 wavefronts: T=2048, N=32, bf16 768 channels 86 / 142, 89 / 157, 111 / 171; T=65536, N=1, bf16 512 channels
-    // 122 / 154, 84 / 128, 85 / 127; the same with 64 channels 78 / 80, 44 / 47, 29 / 32.)  One segment and no exchange where a block can take all stretches: up to 8 always (T=128,
-    // N=256, bf16 1280 channels, one / two segments: 79 / 137, 84 / 138), up to 16 while every block has a compute unit to itself (T=200, N=50, fp32 256 channels: 11.0 / 14.9,
-    // 14.0 / 17.1; T=200, N=512, bf16 768 channels, 4 segments of 4 stretches otherwise: 86 / 140, as one 99 / 150).
-    const int most = tiles > 256 ? 4 : tiles >= 8 ? 8 : kMostWaves;
+    // Small blocks where there are many: they fill the compute units evenly and wait at different times; no more places than stretches, an idle wavefront holds registers.
+    // Large ones where tiles are few: fewer segments have to find each other.  us forward / backward with 2 / 4 / 8 / 16 wavefronts: T=200, N=1024, bf16 768 channels (12288 tiles) 156 / 250,
+    // 165 / 274, 183 / 315; T=2048, N=32, bf16 768 channels (384) 104 / 154, 86 / 142, 89 / 157, 111 / 171; T=65536, N=1, bf16 512 channels (8) 246 / 243, 122 / 154, 84 / 128, 85 / 127; the same with
+    // 64 channels (one) 78 / 80 with 4, 44 / 47, 29 / 32.  T=130 (9 stretches), N=512, bf16 768 channels, 2 / 3 of them: 113 / 173, 101 / 169.
+    // One segment and no exchange where a block can take all stretches: up to 8 always (T=128, N=256, bf16 1280 channels, one / two segments: 79 / 137, 84 / 138), up to 16
+    // while every block has a compute unit to itself (T=200, N=50, fp32 256 channels: 11.0 / 14.9, 14.0 / 17.1).
+    const int few = p.z.stretches % 6 == 3 ? 3 : 2;
+    const int most = tiles >= 1024 ? few : tiles > 256 ? 4 : tiles >= 8 ? 8 : kMostWaves;
     p.z.segments = p.z.stretches <= 8 || (p.z.stretches <= kMostWaves && tiles <= 256) ? 1 : ceil_div(p.z.stretches, most);
     p.waves = ceil_div(p.z.stretches, p.z.segments);
     p.z.segments = ceil_div(p.z.stretches, p.waves);
