@@ -140,6 +140,28 @@ def test_tiny_and_huge_gradients():
     assert (r[np.isfinite(r)] > 0).all()
 
 
+def test_a_tensor_beyond_32_bits():
+    """More than 2^32 elements: the last ones move, and are held, as their indexes say; the others, without a gradient, stay."""
+    end = 700
+    n = (1 << 32) + end
+    w, g = torch.zeros(n, device="cuda:0"), torch.zeros(n, device="cuda:0")
+    state = B.adamw8_state(n)
+    r = np.random.default_rng(8)
+    w0, g0 = r.normal(size=end).astype(np.float32), r.normal(size=end).astype(np.float32)
+    w[-end:], g[-end:] = torch.from_numpy(w0).cuda(), torch.from_numpy(g0).cuda()
+    B.adamw8_step_multi(B.param8_table([(w, g, *state, None, 0.0)]), 1, 77, **HYPER)
+    torch.cuda.synchronize()
+    i = np.arange(n - end, n, dtype=np.uint64)          # (the last 700 begin a block: 2^32 is whole blocks)
+    u = S.mix(i * np.uint64(0x9E3779B9) + (i >> np.uint64(32)) * np.uint64(0x85A308D3) + S.mix(77))
+    zero, scales = np.zeros(end), np.zeros(3)
+    _, _, _, sm, sr, mn, rn = S.adamw8_step(w0, g0, zero, zero, scales, scales, 1, 0, 0, weight_decay=0.0, **HYPER)
+    want_m = S.held(mn, sm, (u & np.uint64(0xFFFF)).astype(np.float64))
+    want_r = S.held(rn, sr, (u >> np.uint64(16)).astype(np.float64))
+    want_r = np.where((rn > 0) & (want_r < 2.0 ** -9), 2.0 ** -9, want_r)
+    assert np.array_equal(values(state[0][-end:]), want_m) and np.array_equal(values(state[1][-end:]), want_r)
+    assert np.array_equal(state[2][-3:].cpu().numpy(), sm) and not w[:-end].any() and not state[1][:-end].view(torch.uint8).any()
+
+
 def test_rounding_has_the_right_mean():
     """Held moments, averaged over seeds, are the moments: the mean of K roundings is off by less than 6 / (2 sqrt K) of a place (its standard deviation is half a
     place at most)."""

@@ -158,6 +158,22 @@ def test_infinities_and_nan_stay_in_their_rows(C):
         assert y[3].isnan().any() and y[7].isnan().all()
 
 
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements, 2^32 bytes: the last rows against the same alone."""
+    C = 1000
+    rows = (1 << 31) // C + 40
+    x = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda:0")
+    x[:8].normal_()
+    x[-8:].normal_()
+    gamma, beta = torch.randn(C, device="cuda:0"), torch.randn(C, device="cuda:0")
+    y, _, mean, invstd = B.layernorm_fwd(x, gamma, beta)
+    dx, _, _ = B.layernorm_bwd(y, x, gamma, mean, invstd)
+    for part in (slice(0, 8), slice(rows - 8, rows)):
+        y2, _, m2, i2 = B.layernorm_fwd(x[part].clone(), gamma, beta)
+        dx2, _, _ = B.layernorm_bwd(y2, x[part].clone(), gamma, m2, i2)
+        assert torch.equal(y[part], y2) and torch.equal(mean[part], m2) and torch.equal(invstd[part], i2) and torch.equal(dx[part], dx2)
+
+
 def test_no_affine_part():
     x, _, dy, _, gamma, _ = make(1, 33, 100, "f32")
     one, zero = torch.ones_like(gamma), torch.zeros_like(gamma)
