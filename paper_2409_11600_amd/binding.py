@@ -1002,7 +1002,7 @@ def _layernorm_call(rows, C, dtype, eps):
 
 
 # (What a call makes and checks costs more than it does itself where it is small: sizes go to torch.empty as numbers, 0.8 us less than as a tuple, and
-# what was not given is not checked.)
+# what was made here is not checked.)
 
 def _floats(t, *shape):
     """t, if it is given: a float32 tensor of that shape."""
@@ -1032,19 +1032,19 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, residual=None, out=None, s
     if out is None:
         out = torch.empty_like(x)
     else:
-        _like(out, x)
+        _like(out, x), _ptr(out)
     if save and sum_out is None and residual is not None:
         sum_out = torch.empty_like(x)
     if save_mean is not None:
-        _floats(save_mean, rows)
+        _floats(save_mean, rows), _ptr(save_mean)
     elif save:
         save_mean = torch.empty(rows, dtype=torch.float32, device=x.device)
     if save_invstd is not None:
-        _floats(save_invstd, rows)
+        _floats(save_invstd, rows), _ptr(save_invstd)
     elif save:
         save_invstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _check(lib().nsk_layernorm_fwd(d, _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(sum_out), _ptr(out), _ptr(save_mean), _ptr(save_invstd),
-                                   _stream()), "nsk_layernorm_fwd")
+    _check(lib().nsk_layernorm_fwd(d, _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(sum_out), out.data_ptr(),
+                                   save_mean.data_ptr() if save_mean is not None else None, save_invstd.data_ptr() if save_invstd is not None else None, _stream()), "nsk_layernorm_fwd")
     return out, x if residual is None else sum_out, save_mean, save_invstd
 
 
@@ -1060,19 +1060,19 @@ def layernorm_bwd(dy, s, gamma, save_mean, save_invstd, dsum=None, dx=None, dgam
     if dx is None:
         dx = torch.empty_like(s)
     else:
-        _like(dx, s)
+        _like(dx, s), _ptr(dx)
     if dgamma is not None:
-        _floats(dgamma, C)
+        _floats(dgamma, C), _ptr(dgamma)
     elif want_affine:
         dgamma = torch.empty(C, dtype=torch.float32, device=s.device)
     if dbeta is not None:
-        _floats(dbeta, C)
+        _floats(dbeta, C), _ptr(dbeta)
     elif want_affine:
         dbeta = torch.empty(C, dtype=torch.float32, device=s.device)
     ws = ws or Workspace(s.device)
     wp, wb = ws.get(need if dgamma is not None or dbeta is not None else 0)
-    _check(lib().nsk_layernorm_bwd(d, _ptr(s), _ptr(dy), _ptr(dsum), _ptr(gamma), _ptr(save_mean), _ptr(save_invstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
-                                   int(bool(accumulate)), wp, wb, _stream()), "nsk_layernorm_bwd")
+    _check(lib().nsk_layernorm_bwd(d, _ptr(s), _ptr(dy), _ptr(dsum), _ptr(gamma), _ptr(save_mean), _ptr(save_invstd), dx.data_ptr(),
+                                   dgamma.data_ptr() if dgamma is not None else None, dbeta.data_ptr() if dbeta is not None else None, int(bool(accumulate)), wp, wb, _stream()), "nsk_layernorm_bwd")
     return dx, dgamma, dbeta
 
 
@@ -1166,10 +1166,10 @@ def glr_step(gi, state, bias=None, slots=None, y=None, want_y=True):
         raise ValueError(f"gi holds three gates a channel: [N, 3 * H], got {tuple(gi.shape)}")
     _floats(state, S, H), _floats(bias, width)
     if y is not None:
-        _rows_of(y, gi, N, H)
+        _rows_of(y, gi, N, H), _ptr(y)
     elif want_y:
         y = torch.empty(N, H, dtype=gi.dtype, device=gi.device)
-    _check(lib().nsk_glr_step(_dtype_code(gi), N, H, S, _ptr(gi), _ptr(bias), _lengths_ptr(slots, N), _ptr(state), _ptr(y), _stream()), "nsk_glr_step")
+    _check(lib().nsk_glr_step(_dtype_code(gi), N, H, S, _ptr(gi), _ptr(bias), _lengths_ptr(slots, N), _ptr(state), y.data_ptr() if y is not None else None, _stream()), "nsk_glr_step")
     return y
 
 
