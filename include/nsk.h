@@ -112,7 +112,8 @@ int nsk_last_hip_error(void);
  *   NSK_IGEMM_TILE = 1..7                           (tile shape of the generic kernel, which then takes every plain layer);
  *   NSK_GRU_SPLIT = 1, 2, 4                         (most blocks that share a sample of nsk_gru_seq_*);
  *   NSK_GRU_FAR                                     (set = such blocks run on XCDs of their own);
- *   NSK_GRU_POLLS = n                               (failed polls after which such a block gives up; 0: at its first wait). */
+ *   NSK_GRU_POLLS = n                               (failed polls after which such a block gives up; 0: at its first wait);
+ *   NSK_GLR_POLLS = n                               (looks for another block's state after which a block of nsk_glr_* makes it itself). */
 void nsk_test_hooks_reload(void);
 
 /* Output extent of a convolution.  Host only.  NSK_ERR_BAD_DESC if the descriptor is invalid

@@ -34,9 +34,11 @@ __device__ inline float sigmoid(float a)
 // left, leaves the state that leaves it, and then goes through its steps again, which are still in its registers.
 // The state behind a segment is A h + B with the h in front of it, whichever block computes that, so the results do not depend on how far the others are.
 // Waiting ends: blocks take numbers from a counter as they begin, and a block waits only for smaller numbers, whose blocks have begun and leave (A, B) before
-// they wait themselves.
+// they wait themselves.  And if it did not (a caller that lets something else write to this call's workspace): after kPolls looks, about a second, a block goes through all steps
+// in front of its own by itself.
 constexpr int kStretch = NSK_GLR_STRETCH;
 constexpr int kMostWaves = 16;
+constexpr int kPolls = 1 << 20;
 struct Sizes {
     int T, N, H;
     int stretches;          // of the whole sequence
@@ -44,6 +46,7 @@ struct Sizes {
     unsigned tiles;
     int groups;             // parts of the tiles that have counters of their own
     int flat;               // tiles go on across sequences (1), or each sequence has tiles of its own (0)
+    int polls;              // looks after which a block makes the state that enters its segment itself
     long long gi_t, gi_n, y_t, y_n;
 };
 typedef unsigned long long u64;
@@ -93,8 +96,8 @@ __device__ inline bool place(const Sizes &z, const Exchange &x, unsigned &tile, 
     return true;
 }
 
-// The state that enters a segment; called by one wavefront.  v0 enters the first one; A, B: this segment's.
-__device__ inline float entering(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B)
+// The state that enters a segment; called by one wavefront.  v0 enters the first one; A, B: this segment's; alone() goes through the steps in front of it.
+template <typename F> __device__ inline float entering(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B, F &&alone)
 {
     if (z.segments == 1) return v0;
     const int lane = threadIdx.x & 63;
@@ -106,7 +109,7 @@ __device__ inline float entering(const Sizes &z, const Exchange &x, unsigned til
     }
     // back to the nearest segment whose state is there, over those whose (A, B) are, four at a time
     float v = v0;
-    int j = segment - 1;
+    int j = segment - 1, polls = z.polls;
     for (bool found = false; j >= 0 && !found;) {
         unsigned behind[4];
         u64 ab[4];
@@ -125,6 +128,11 @@ __device__ inline float entering(const Sizes &z, const Exchange &x, unsigned til
                 found = true;
             } else if (j > 0 && !__builtin_amdgcn_ballot_w64(ab[i] == ~0ull)) --j;
             else wait = true;
+        }
+        if (wait && polls-- <= 0) {
+            v = alone();
+            j = segment;        // (nothing is left to apply)
+            break;
         }
         if (wait) __builtin_amdgcn_s_sleep(2);
     }
@@ -280,7 +288,7 @@ __device__ inline void fold(const float (&f)[kStretch], const float (&x)[kStretc
 }
 
 // (A, B) of a block's stretches through LDS; the value that enters this wavefront's stretch, and the one that leaves the block's last.
-__device__ inline float join(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B, float &leaves)
+template <typename F> __device__ inline float join(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B, float &leaves, F &&alone)
 {
     __shared__ float part[kMostWaves][2][64], enters[64];
     const int lane = threadIdx.x & 63, wave = wave_of_block(), waves = blockDim.x >> 6;
@@ -295,7 +303,7 @@ __device__ inline float join(const Sizes &z, const Exchange &x, unsigned tile, i
                 A *= part[w][0][lane];
                 B = fmaf(part[w][0][lane], B, part[w][1][lane]);
             }
-            v0 = entering(z, x, tile, segment, v0, A, B);
+            v0 = entering(z, x, tile, segment, v0, A, B, alone);
             enters[lane] = v0;
             leaves = fmaf(A, v0, B);
         }
@@ -336,7 +344,20 @@ __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, con
         apply_gates(f, x, o);
         fold(f, x, A, B);
     }
-    float h = join(z, ex, tile, segment, h0 ? h0[l.q] : 0.f, A, B, leaves);
+    const float start = h0 ? h0[l.q] : 0.f;
+    float h = join(z, ex, tile, segment, start, A, B, leaves, [&] {
+        float v = start;
+        const int end = segment * (int)(blockDim.x >> 6) * kStretch;
+#pragma unroll 1
+        for (int t = 0; t < end; ++t) {
+            const __amdgpu_buffer_rsrc_t r = Rows<const T>{gi + gi0 + t * z.gi_t, 1}.at();
+            float s, rest;
+            sigmoid2(load<T>(r, l.gi, 0) + b.f, s, rest);
+            const float c = load<T>(r, l.gi, (unsigned)z.H * (unsigned)sizeof(T)) + b.c;
+            v = t < len ? s * v + rest * c : v;
+        }
+        return v;
+    });
     if (h_last && segment == z.segments - 1 && wave == 0 && l.there) h_last[l.q] = leaves;
     if (!mine) return;
     if (saved && l.there) saved[s * all + l.q] = h;
@@ -423,7 +444,18 @@ __global__ __launch_bounds__(1024) void glr_bwd_kernel(Sizes z, Exchange ex, con
             B = f[i] * (B + u[i]);
         }
     }
-    float E = join(z, ex, tile, segment, dh_last ? dh_last[l.q] : 0.f, A, B, leaves);
+    const float start = dh_last ? dh_last[l.q] : 0.f;
+    float E = join(z, ex, tile, segment, start, A, B, leaves, [&] {
+        float v = start;
+        const int end = (z.segments - segment) * waves * kStretch;
+#pragma unroll 1
+        for (int t = z.T - 1; t >= end; --t) {
+            const __amdgpu_buffer_rsrc_t r = Rows<const T>{gi + gi0 + t * z.gi_t, 1}.at(), ry = Rows<const T>{dy + y0 + t * z.y_t, dy ? 1 : 0}.at();
+            const float s = sigmoid(load<T>(r, l.gi, 0) + b.f), o = sigmoid(load<T>(r, l.gi, 2 * gate) + b.o), up = load<T>(ry, l.y, 0);
+            v = t < len ? s * (v + up * o) : v;
+        }
+        return v;
+    });
     if (dh0 && segment == z.segments - 1 && wave == 0 && l.there) dh0[l.q] = leaves;
     if (!mine) return;
     if (some) {
@@ -497,7 +529,7 @@ Plan plan_of(const nsk_glr_desc_t &d)
 {
     Plan p{};
     const long long es = d.dtype == NSK_BF16 ? 2 : 4;
-    p.z = {d.T, d.N, d.H, ceil_div(d.T, kStretch), 1, 0, 1, 0, d.gi_t, d.gi_n, d.y_t, d.y_n};
+    p.z = {d.T, d.N, d.H, ceil_div(d.T, kStretch), 1, 0, 1, 0, hooks().glr_polls >= 0 ? hooks().glr_polls : kPolls, d.gi_t, d.gi_n, d.y_t, d.y_n};
     // a tile reaches over 63 / H + 1 further sequences, whose offsets have to fit 30 bits (those of a single sequence do)
     const long long over = d.H < 64 ? 63 / d.H + 1 : 1, stride = d.gi_n > d.y_n ? d.gi_n : d.y_n;
     p.z.flat = stride < (1LL << 30) && (over * stride + d.H) * es < (1LL << 30);

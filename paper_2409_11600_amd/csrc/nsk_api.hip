@@ -480,6 +480,8 @@ void read_hooks()
     h.gru_split = split > 0 ? (int)split : 0;
     const long long polls = num("NSK_GRU_POLLS");
     h.gru_polls = polls >= 0 && polls <= INT_MAX ? (int)polls : -1;
+    const long long looks = num("NSK_GLR_POLLS");
+    h.glr_polls = looks >= 0 && looks <= INT_MAX ? (int)looks : -1;
     g_hooks = h;
     g_hooks_read = true;
 }

@@ -309,6 +309,17 @@ def test_long_sequences_that_hold_the_mark_of_nothing(T, N, H):
         assert torch.equal(dgi[..., :H][:, keep], want[3][..., :H][:, keep]) and torch.equal(dgi[..., 2 * H:][:, keep], want[3][..., 2 * H:][:, keep])
 
 
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,H", LONG)
+def test_blocks_that_wait_for_nobody(nsk_env, T, N, H, dtype, ragged):
+    """Blocks that look once for the state in front of their segment and make it themselves if it is not there: the same values to rounding."""
+    nsk_env("NSK_GLR_POLLS", "0")
+    print(f"recurrence, no waiting, T={T} N={N} H={H} {dtype} ragged={ragged}", flush=True)
+    gi, dy, bias, h0, dh_last, lengths = make(T + H + 1, T, N, H, dtype, ragged)
+    check(gi, dy, bias, h0, dh_last, lengths, dtype)
+
+
 def test_offsets_beyond_32_bits():
     """Rows whose offsets, in elements and in bytes, pass 2^31 and 2^32: the last sequences of a batch-major tensor of 2^31 + elements against the same alone."""
     H, T = 128, 700
