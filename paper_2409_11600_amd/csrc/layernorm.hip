@@ -4,7 +4,7 @@
 //   dgamma = sum over rows of dy * xh,  dbeta = sum over rows of dy
 // Bound by memory: a row is read once and stays in the registers of the lanes that share it (2 to 1024 of them), so that the variance is the mean square of
 // the differences from the mean itself, and the backward pass sums dy * xh and dy for the weights on the way.  us (TB/s of what has to move): 65536 x 768 bf16 with a
-// residual 78 (5.2), backward 61 (4.9); 30011 x 1001 bf16 backward 39-44 (4.1-4.6), as fast as rows of 1000 or 1008; 10000 x 256 fp32 backward 10.2 and the joining
+// residual 70 (5.8), backward 61 (4.9); 30011 x 1001 bf16 backward 39-44 (4.1-4.6), as fast as rows of 1000 or 1008; 10000 x 256 fp32 backward 10.2 and the joining
 // launch 3.4; 300000 x 64 bf16 13.8 (5.6).  The backward pass has the next row of each lane on its way while one is worked on: its registers leave room for two
 // wavefronts a SIMD, and those alone had 24 KB a compute unit in flight (65536 x 768 bf16 121 us without).
 #include "nsk_internal.h"
@@ -357,7 +357,10 @@ __global__ __launch_bounds__(1024) void layernorm_dparam_final_kernel(const floa
     }
 }
 
-// Lanes that share a row, and vectors of each.
+// Lanes that share a row, and vectors of each: as many lanes as there are vectors up to a wavefront, then two vectors a lane, then more wavefronts, whose sums go through LDS.
+// us forward with a residual / backward with dsum, otherwise in brackets: 20000 x 768 bf16 64 lanes of two vectors 26 / 33 (256 of one 33 / 43); 8000 x 1500 256 of one 20 / 25
+// (64 of four 21 / 41, whose registers leave one or two wavefronts a SIMD); 4000 x 3000 256 of two 20 / 26 (1024 of one 35 / 29), 4000 x 4096 27 / 33 (36 / 30); 2000 x 6000 1024 of one 23 / 24
+// (256 of four 21 / 35), 2000 x 8192 30 / 32 (28 / 41).
 struct Plan {
     int lanes, k;       // lanes 0: the kernels that hold nothing
 };
@@ -378,7 +381,8 @@ Plan plan_of(const nsk_layernorm_desc_t &d)
 // 31 for dx alone).
 constexpr bool on_the_way(Plan p) { return p.lanes > 0 && !(p.lanes == 1024 && p.k == 2); }
 int rows_a_block(const Plan &p) { return p.lanes == 0 || p.lanes >= 256 ? 1 : 256 / p.lanes; }
-// Blocks of the backward pass, each with sums of its own.
+// Blocks of the backward pass, each with sums of its own; 512, two a compute unit, are what its registers leave room for at once.  us with dsum, 256 / 512 / 1024 of them:
+// 10000 x 256 fp32 13.4, 13.0, 13.6; 65536 x 768 bf16 86, 79, 87; 65536 x 768 fp32 225, 150, 157; 300000 x 64 bf16 42, 34, 37.
 int shares_of(const nsk_layernorm_desc_t &d)
 {
     const Plan p = plan_of(d);
@@ -427,7 +431,9 @@ int nsk_layernorm_fwd(const nsk_layernorm_desc_t *desc, const void *x, const voi
         unaligned16(save_invstd))
         return NSK_ERR_ALIGNMENT;
     const Plan p = plan_of(*desc);
-    const long long need = (desc->rows + rows_a_block(p) - 1) / rows_a_block(p), most = p.lanes == 0 || p.lanes == 1024 ? 512 : 2048;
+    // (a row or a few for every block: 65536 x 768 bf16 with a residual 70 us, 78 with 2048 blocks that go round, 74 with 512; blocks of a row of 1024 lanes, whose gamma and beta are
+    // long, go round: 1000 x 16000 bf16 30 with 512 blocks, 32 with one a row)
+    const long long need = (desc->rows + rows_a_block(p) - 1) / rows_a_block(p), most = p.lanes == 0 || p.lanes == 1024 ? 512 : 1 << 20;
     const dim3 grid((unsigned)(need < most ? need : most));
     hipStream_t st = (hipStream_t)stream;
     auto launch = [&](auto one) {
