@@ -158,10 +158,9 @@ def test_infinities_and_nan_stay_in_their_rows(C):
         assert y[3].isnan().any() and y[7].isnan().all()
 
 
-def test_offsets_beyond_32_bits():
-    """More than 2^31 elements, 2^32 bytes: the last rows against the same alone."""
-    C = 1000
-    rows = (1 << 31) // C + 40
+@pytest.mark.parametrize("rows,C", [((1 << 31) // 1000 + 40, 1000), ((1 << 22) + 100, 264)])
+def test_many_elements_and_many_rows(rows, C):
+    """More than 2^31 elements, 2^32 bytes; and more rows than blocks are launched for: the last rows against the same alone."""
     x = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda:0")
     x[:8].normal_()
     x[-8:].normal_()
