@@ -525,7 +525,7 @@ struct Plan {
     int waves;
     unsigned blocks;
 };
-Plan plan_of(const nsk_glr_desc_t &d)
+Plan plan_of(const nsk_glr_desc_t &d, int pass)
 {
     Plan p{};
     const long long es = d.dtype == NSK_BF16 ? 2 : 4;
@@ -540,11 +540,14 @@ Plan plan_of(const nsk_glr_desc_t &d)
     // Large ones where tiles are few: fewer segments have to find each other.  us forward / backward with 2 / 4 / 8 / 16 wavefronts: T=200, N=1024, bf16 768 channels (12288 tiles) 156 / 250,
     // 165 / 274, 183 / 315; T=2048, N=32, bf16 768 channels (384) 104 / 154, 86 / 142, 89 / 157, 111 / 171; T=65536, N=1, bf16 512 channels (8) 246 / 243, 122 / 154, 84 / 128, 85 / 127; the same with
     // 64 channels (one) 78 / 80 with 4, 44 / 47, 29 / 32.  T=130 (9 stretches), N=512, bf16 768 channels, 2 / 3 of them: 113 / 173, 101 / 169.
-    // One segment and no exchange where a block can take all stretches: up to 8 always (T=128, N=256, bf16 1280 channels, one / two segments: 79 / 137, 84 / 138), up to 16
-    // while every block has a compute unit to itself (T=200, N=50, fp32 256 channels: 11.0 / 14.9, 14.0 / 17.1).
+    // One segment and no exchange where a block can take all stretches: up to 8 (T=128, N=256, bf16 1280 channels, one / two segments: 79 / 137, 84 / 138), up to 16
+    // while every block has a compute unit to itself (T=200, N=50, fp32 256 channels: 11.0 / 14.9, 14.0 / 17.1); the backward pass, of whose wavefronts a unit holds 16, has no room for
+    // two or three whole blocks of 5 to 8 where many are waiting (N=512, bf16 768 channels, one segment / blocks of two, backward: T=80 119, 106; T=96 132, 120; T=128 162, 157; with
+    // 1024 tiles, N=128 and 512 channels, T=112: 26.9, 29.1).
     const int few = p.z.stretches % 6 == 3 ? 3 : 2;
     const int most = tiles >= 1024 ? few : tiles > 256 ? 4 : tiles >= 8 ? 8 : kMostWaves;
-    p.z.segments = p.z.stretches <= 8 || (p.z.stretches <= kMostWaves && tiles <= 256) ? 1 : ceil_div(p.z.stretches, most);
+    const int whole = pass == NSK_PASS_DGRAD && tiles >= 2048 ? 4 : 8;
+    p.z.segments = p.z.stretches <= whole || (p.z.stretches <= kMostWaves && tiles <= 256) ? 1 : ceil_div(p.z.stretches, most);
     p.waves = ceil_div(p.z.stretches, p.z.segments);
     p.z.segments = ceil_div(p.z.stretches, p.waves);
     p.blocks = (unsigned)(p.z.groups * ((tiles + p.z.groups - 1) / p.z.groups) * p.z.segments);
@@ -575,7 +578,7 @@ size_t nsk_glr_saved_bytes(const nsk_glr_desc_t *desc)
 size_t nsk_glr_workspace_bytes(const nsk_glr_desc_t *desc, int pass)
 {
     nsk_glr_desc_t d;
-    return (pass == NSK_PASS_FWD || pass == NSK_PASS_DGRAD) && check(desc, d) == NSK_OK ? workspace_of(plan_of(d)) : 0;
+    return (pass == NSK_PASS_FWD || pass == NSK_PASS_DGRAD) && check(desc, d) == NSK_OK ? workspace_of(plan_of(d, pass)) : 0;
 }
 
 int nsk_glr_fwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0, void *y, float *h_last, float *saved,
@@ -587,7 +590,7 @@ int nsk_glr_fwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, c
     if (!gi || (!y && !h_last)) return NSK_ERR_NULL;
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(h0) || unaligned16(y) || unaligned16(h_last) || unaligned16(saved) || unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, NSK_PASS_FWD);
     if (p.z.segments > 1 && (!workspace || workspace_bytes < workspace_of(p))) return NSK_ERR_WORKSPACE;
     const dim3 grid(p.blocks), block((unsigned)p.waves * 64);
     hipStream_t st = (hipStream_t)stream;
@@ -611,7 +614,7 @@ int nsk_glr_bwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, c
     if (!gi || !saved || (!dy && !dh_last) || !dgi) return NSK_ERR_NULL;
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(saved) || unaligned16(dy) || unaligned16(dh_last) || unaligned16(dgi) || unaligned16(dh0) || unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, NSK_PASS_DGRAD);
     if (p.z.segments > 1 && (!workspace || workspace_bytes < workspace_of(p))) return NSK_ERR_WORKSPACE;
     const dim3 grid(p.blocks), block((unsigned)p.waves * 64);
     hipStream_t st = (hipStream_t)stream;

@@ -263,7 +263,7 @@ def test_tokens_one_by_one_are_the_sequence():
     in_bound(host(y), wy, ey + U * np.abs(wy), "y")
 
 
-LONG = [(300, 1, 64), (2100, 3, 24), (4000, 20, 40), (20000, 1, 1), (700, 90, 200)]      # several segments: one tile, two, 13, one, 282
+LONG = [(300, 1, 64), (2100, 3, 24), (4000, 20, 40), (20000, 1, 1), (700, 90, 200), (90, 2100, 64)]      # several segments: one tile, two, 13, one, 282, 2100
 
 
 @pytest.mark.parametrize("T,N,H", LONG)
