@@ -1010,29 +1010,24 @@ def _floats(t, *shape):
         raise ValueError(f"a float32 tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)}")
 
 
-def _like(t, ref):
-    """t, if it is given: of ref's type and shape."""
-    if t is not None and (t.dtype is not ref.dtype or t.shape != ref.shape):
-        raise ValueError(f"a {ref.dtype} tensor of shape {tuple(ref.shape)} is wanted, got {t.dtype} {tuple(t.shape)}")
-
-
-def _rows_of(t, ref, *shape):
-    """t, if it is given: of ref's type and that shape."""
-    if t is not None and (t.dtype is not ref.dtype or t.shape != shape):
-        raise ValueError(f"a {ref.dtype} tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)}")
+def _like(t, dtype, shape):
+    """t, if it is given: of that type and shape."""
+    if t is not None and (t.dtype is not dtype or t.shape != shape):
+        raise ValueError(f"a {dtype} tensor of shape {tuple(shape)} is wanted, got {t.dtype} {tuple(t.shape)}")
 
 
 def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, residual=None, out=None, sum_out=None, save_mean=None, save_invstd=None, save=True):
     """y = layer norm of s = x + residual over the last axis.  Returns (y, s, mean, invstd): s is x where there is no residual; with
     save=False (nothing follows that needs them) the buffers that are not given are not made, and None comes back for them."""
-    C = int(x.shape[-1])
+    dtype, shape = x.dtype, x.shape
+    C = shape[-1]
     rows = x.numel() // C if C else 0
     d, _ = _layernorm_call(rows, C, _dtype_code(x), float(eps))
-    _floats(gamma, C), _floats(beta, C), _like(residual, x), _like(sum_out, x)
+    _floats(gamma, C), _floats(beta, C), _like(residual, dtype, shape), _like(sum_out, dtype, shape)
     if out is None:
         out = torch.empty_like(x)
     else:
-        _like(out, x), _ptr(out)
+        _like(out, dtype, shape), _ptr(out)
     if save and sum_out is None and residual is not None:
         sum_out = torch.empty_like(x)
     if save_mean is not None:
@@ -1052,15 +1047,16 @@ def layernorm_bwd(dy, s, gamma, save_mean, save_invstd, dsum=None, dx=None, dgam
                   ws: Optional[Workspace] = None):
     """s: what layernorm_fwd returned as such.  Returns (dx, dgamma, dbeta); dx includes dsum, the gradient that reaches s past the normalisation.
     want_affine=False: no gradients of gamma and beta but into buffers that are given."""
-    C = int(s.shape[-1])
+    dtype, shape = s.dtype, s.shape
+    C = shape[-1]
     rows = s.numel() // C if C else 0
     d, need = _layernorm_call(rows, C, _dtype_code(s), 1e-5)
-    _like(dy, s), _floats(gamma, C), _floats(save_mean, rows), _floats(save_invstd, rows), _like(dsum, s)
+    _like(dy, dtype, shape), _floats(gamma, C), _floats(save_mean, rows), _floats(save_invstd, rows), _like(dsum, dtype, shape)
     assert not accumulate or not want_affine or (dgamma is not None and dbeta is not None)
     if dx is None:
         dx = torch.empty_like(s)
     else:
-        _like(dx, s), _ptr(dx)
+        _like(dx, dtype, shape), _ptr(dx)
     if dgamma is not None:
         _floats(dgamma, C), _ptr(dgamma)
     elif want_affine:
@@ -1115,9 +1111,9 @@ def glr_fwd(gi, bias=None, h0=None, lengths=None, y=None, h_last=None, saved=Non
     if y is None and want_y:
         y = torch.empty(T, N, H, dtype=gi.dtype, device=dev) if gt >= gn else torch.empty(N, T, H, dtype=gi.dtype, device=dev).transpose(0, 1)
     else:
-        _rows_of(y, gi, T, N, H)
+        _like(y, gi.dtype, (T, N, H))
     if h_last is None:
-        h_last = torch.empty(N, H, dtype=torch.float32, device=dev)
+        h_last = torch.empty(N, H, dtype=torch.float32, device=dev) if h0 is None else torch.empty_like(h0)
     else:
         _floats(h_last, N, H)
     stretches = -(-T // NSK_GLR_STRETCH)
@@ -1139,21 +1135,24 @@ def glr_bwd(gi, saved, bias=None, dy=None, dh_last=None, lengths=None, dgi=None,
     """Gradients of glr_fwd: (dgi, dh0).  dgi lies as gi does."""
     T, N, H = _glr_dims(gi)
     dev = gi.device
+    strides = gi.stride()
     if dgi is None:
-        dgi = torch.empty_strided(gi.shape, gi.stride(), dtype=gi.dtype, device=dev)
+        dgi = torch.empty_like(gi)
+        if dgi.stride() != strides:         # (rows with room between them)
+            dgi = torch.empty_strided(gi.shape, strides, dtype=gi.dtype, device=dev)
     else:
-        _like(dgi, gi)
+        _like(dgi, gi.dtype, gi.shape), _rows_ptr(dgi, gi)
     if dh0 is not None:
         _floats(dh0, N, H)
     elif want_dh0:
-        dh0 = torch.empty(N, H, dtype=torch.float32, device=dev)
-    _floats(bias, 3 * H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H), _floats(dh_last, N, H), _rows_of(dy, gi, T, N, H)
-    gt, gn, _ = gi.stride()
+        dh0 = torch.empty(N, H, dtype=torch.float32, device=dev) if dh_last is None else torch.empty_like(dh_last)
+    _floats(bias, 3 * H), _floats(saved, -(-T // NSK_GLR_STRETCH), N, H), _floats(dh_last, N, H), _like(dy, gi.dtype, (T, N, H))
+    gt, gn, _ = strides
     yt, yn, _ = (0, 0, 1) if dy is None else dy.stride()
     d, need = _glr_call(T, N, H, _dtype_code(gi), gt, gn, yt, yn, NSK_PASS_DGRAD)
     ws = ws or Workspace(dev)
     wp, wb = ws.get(need)
-    _check(lib().nsk_glr_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(dy), _ptr(dh_last), _rows_ptr(dgi, gi),
+    _check(lib().nsk_glr_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(dy), _ptr(dh_last), dgi.data_ptr(),
                              _ptr(dh0), wp, wb, _stream()), "nsk_glr_bwd")
     return dgi, dh0
 
@@ -1166,7 +1165,7 @@ def glr_step(gi, state, bias=None, slots=None, y=None, want_y=True):
         raise ValueError(f"gi holds three gates a channel: [N, 3 * H], got {tuple(gi.shape)}")
     _floats(state, S, H), _floats(bias, width)
     if y is not None:
-        _rows_of(y, gi, N, H), _ptr(y)
+        _like(y, gi.dtype, (N, H)), _ptr(y)
     elif want_y:
         y = torch.empty(N, H, dtype=gi.dtype, device=gi.device)
     _check(lib().nsk_glr_step(_dtype_code(gi), N, H, S, _ptr(gi), _ptr(bias), _lengths_ptr(slots, N), _ptr(state), y.data_ptr() if y is not None else None, _stream()), "nsk_glr_step")
