@@ -77,7 +77,7 @@ constexpr unsigned kNaN = 0x7fc00000u;      // (in place of a NaN of all ones)
 
 // The tile of this block and which of its segments (in the order in which they wait for each other); false: there is nothing left for it.
 // Blocks are handed to the eight XCDs in turn: with 8 or 32 groups, all segments of a tile are on one XCD, and so are most neighbouring tiles, which share the cache
-// lines at their ends where rows are not whole ones.  (us forward / backward, 1 / 8 / 32 groups, T=2048, N=32, bf16 768 channels, 6144 blocks of 4 wavefronts: 165 / 176,
+// lines at their ends where rows are not whole ones.  (us forward / backward, 1 / 8 / 32 groups, T=2048, N=32, bf16 768 channels, 12288 blocks of 4 wavefronts: 165 / 176,
 // 89 / 143, 86 / 142: a counter gives out a number in 12 ns; ragged T=777, N=33, fp32 201 channels: 25 / 43, 19 / 37, 20 / 42.)
 __device__ inline bool place(const Sizes &z, const Exchange &x, unsigned &tile, int &segment)
 {
@@ -537,7 +537,7 @@ Plan plan_of(const nsk_glr_desc_t &d, int pass)
     p.z.tiles = (unsigned)tiles;
     p.z.groups = tiles >= 256 ? kMostGroups : tiles >= 8 ? 8 : 1;
     // Small blocks where there are many: they fill the compute units evenly and wait at different times; no more places than stretches, an idle wavefront holds registers.
-    // Large ones where tiles are few: fewer segments have to find each other.  us forward / backward with 2 / 4 / 8 / 16 wavefronts: T=200, N=1024, bf16 768 channels (12288 tiles) 156 / 250,
+    // Large ones where tiles are few: fewer segments have to find each other.  us forward / backward with 2 / 4 / 8 / 16 wavefronts: T=200, N=512, bf16 768 channels (6144 tiles) 156 / 250,
     // 165 / 274, 183 / 315; T=2048, N=32, bf16 768 channels (384) 104 / 154, 86 / 142, 89 / 157, 111 / 171; T=65536, N=1, bf16 512 channels (8) 246 / 243, 122 / 154, 84 / 128, 85 / 127; the same with
     // 64 channels (one) 78 / 80 with 4, 44 / 47, 29 / 32.  T=130 (9 stretches), N=512, bf16 768 channels, 2 / 3 of them: 113 / 173, 101 / 169.
     // One segment and no exchange where a block can take all stretches: up to 8 (T=128, N=256, bf16 1280 channels, one / two segments: 79 / 137, 84 / 138), up to 16
