@@ -96,9 +96,15 @@ __device__ inline bool place(const Sizes &z, const Exchange &x, unsigned &tile, 
     return true;
 }
 
+// (Room in LDS where tiles are few and looks go back far: T=65536, N=1, bf16 512 channels 86 us without, 78 with it.  Small blocks look back one segment or two, and the LDS would leave fewer of
+// them on a compute unit.)
+__host__ __device__ inline int passed_of(int waves) { return waves >= 8 ? 24 : 0; }
 // The state that enters a segment; called by one wavefront.  v0 enters the first one; A, B: this segment's; alone() goes through the steps in front of it.
 template <typename F> __device__ inline float entering(const Sizes &z, const Exchange &x, unsigned tile, int segment, float v0, float A, float B, F &&alone)
 {
+    // (A, B) of the segments that the look passes, nearest first: a second load of them takes as long as a look
+    extern __shared__ u64 passed[];
+    const int room = passed_of(blockDim.x >> 6);
     if (z.segments == 1) return v0;
     const int lane = threadIdx.x & 63;
     const size_t step = (size_t)z.tiles * 64, at = (size_t)tile * 64 + lane;
@@ -126,8 +132,10 @@ template <typename F> __device__ inline float entering(const Sizes &z, const Exc
             if (!__builtin_amdgcn_ballot_w64(behind[i] == ~0u)) {
                 v = value(behind[i]);
                 found = true;
-            } else if (j > 0 && !__builtin_amdgcn_ballot_w64(ab[i] == ~0ull)) --j;
-            else wait = true;
+            } else if (j > 0 && !__builtin_amdgcn_ballot_w64(ab[i] == ~0ull)) {
+                if (segment - 1 - j < room) passed[(segment - 1 - j) * 64 + lane] = ab[i];
+                --j;
+            } else wait = true;
         }
         if (wait && polls-- <= 0) {
             v = alone();
@@ -136,10 +144,15 @@ template <typename F> __device__ inline float entering(const Sizes &z, const Exc
         }
         if (wait) __builtin_amdgcn_s_sleep(2);
     }
-    // and on from there
+    // and on from there: over those further back than there was room for first
+    int k = j + 1;
 #pragma unroll 4
-    for (int k = j + 1; k < segment; ++k) {
+    for (; k < segment - room; ++k) {
         const u64 ab = seen(x.ab + k * step + at);
+        v = fmaf(value((unsigned)ab), v, value((unsigned)(ab >> 32)));
+    }
+    for (; k < segment; ++k) {
+        const u64 ab = passed[(segment - 1 - k) * 64 + lane];
         v = fmaf(value((unsigned)ab), v, value((unsigned)(ab >> 32)));
     }
     if (!last) {
@@ -321,7 +334,8 @@ template <typename F> __device__ inline float join(const Sizes &z, const Exchang
 
 // Bound by memory where tiles are many (3 + 1 elements and 1/4 byte a step and channel): bf16, T=2048, N=32, 768 channels 86 us, 4.8 TB/s of what a copy reaches 5.1 of;
 // the vector unit, with four transcendental of some 25 instructions a step, is half busy.  By the hand-over where tiles are few: bf16, T=65536, N=1, 512 channels
-// 85 us (3.3 TB/s; wavefronts wait two thirds of their time, a tile gets on by a segment in 0.16 us); and by one chain of loads, gates and stores where a call is short: fp32, T=200,
+// 78 us (3.6 TB/s; of the 13 us that a block lasts, its number takes 1, its loads 2, its steps 2, looking back 5 to 6: two or three loads one behind the other, 2 us each while the memory is
+// loaded); and by one chain of loads, gates and stores where a call is short: fp32, T=200,
 // N=50, 256 channels 11 us for 42 MB.  (Wider look-backs, 8 or 16 segments at a time or 4 by each wavefront, cost more in traffic than they gave: 92, 97, 118 us for the long one.)
 template <typename T>
 __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
@@ -598,7 +612,7 @@ int nsk_glr_fwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, c
     unset(p, workspace, st);
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        hipLaunchKernelGGL(glr_fwd_kernel<T>, grid, block, 0, st, p.z, ex, (const T *)gi, bias, lengths, h0, (T *)y, h_last, saved);
+        hipLaunchKernelGGL(glr_fwd_kernel<T>, grid, block, p.z.segments > 1 ? passed_of(p.waves) * 64 * sizeof(u64) : 0, st, p.z, ex, (const T *)gi, bias, lengths, h0, (T *)y, h_last, saved);
     };
     if (d.dtype == NSK_BF16) launch(bf16_t{});
     else launch(float{});
@@ -622,7 +636,7 @@ int nsk_glr_bwd(const nsk_glr_desc_t *desc, const void *gi, const float *bias, c
     unset(p, workspace, st);
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        hipLaunchKernelGGL(glr_bwd_kernel<T>, grid, block, 0, st, p.z, ex, (const T *)gi, bias, lengths, saved, (const T *)dy, dh_last, (T *)dgi, dh0);
+        hipLaunchKernelGGL(glr_bwd_kernel<T>, grid, block, p.z.segments > 1 ? passed_of(p.waves) * 64 * sizeof(u64) : 0, st, p.z, ex, (const T *)gi, bias, lengths, saved, (const T *)dy, dh_last, (T *)dgi, dh0);
     };
     if (d.dtype == NSK_BF16) launch(bf16_t{});
     else launch(float{});
