@@ -11,12 +11,16 @@ namespace {
 
 bool unaligned16(const void *p) { return ((uintptr_t)p & 15) != 0; }
 
-// sigmoid(a) and 1 - sigmoid(a), both to the last places: near 1 the difference from it would keep none of the small one's.  The hardware's exponential (1 ulp) and
-// its reciprocal with a Newton step: a product of hundreds of gates adds up a rounding that leans to one side (2000 steps of 256 channels, dh0 against 64 bits: 3.5e-7
+// sigmoid(a) and 1 - sigmoid(a), each to within 10 units of 2^-24 of itself whatever the argument: near 1 the difference from it would keep none of the small one's.
+// The hardware's exponential (1 ulp) takes t = |a| log2(e), whose rounding alone would put |a| such units into the small one (a memory of 3000 steps is an argument of 8).
+// What t lost of the argument, |a| - t ln(2), comes back as a factor.  log2(e) is rounded down so far that nothing is ever gained, so the fused product's clamp to [0, 1], which
+// takes no instruction, changes nothing but the NaN of an infinite argument.  ln(2) in one word leaves 0.05 |a| units, 4 at the argument where the exponential ends.
+// The reciprocal takes a Newton step: a product of hundreds of gates adds up a rounding that leans to one side (2000 steps of 256 channels, dh0 against 64 bits: 3.5e-7
 // without the step, 2.0e-7 with it; no difference in time).
 __device__ inline void sigmoid2(float a, float &s, float &rest)
 {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(a)), x = 1.f + e, y = __builtin_amdgcn_rcpf(x);
+    const float m = fabsf(a), t = 1.4426949f * m, lost = fminf(fmaxf(fmaf(t, -0.693147182f, m), 0.f), 1.f), e0 = __builtin_amdgcn_exp2f(-t);
+    const float e = fmaf(e0, -lost, e0), x = 1.f + e, y = __builtin_amdgcn_rcpf(x);
     const float big = fmaf(fmaf(-x, y, 1.f), y, y), small = e * big;
     s = a >= 0.f ? big : small;
     rest = a >= 0.f ? small : big;

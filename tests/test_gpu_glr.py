@@ -187,6 +187,45 @@ def test_gates_at_their_ends():
             in_bound(host(dh0), host((dy.double() * o).sum(0) + dh_last.double()), (T + 12) * U * host((dy.double() * o).abs().sum(0) + dh_last.abs()), "dh0")
 
 
+@pytest.mark.parametrize("low,high", [(0.0, 4.0), (4.0, 8.0), (8.0, 12.0), (12.0, 16.0), (16.0, 24.0), (24.0, 80.0)])
+def test_a_gate_that_is_nearly_closed(low, high):
+    """Gates whose arguments are exact (no bias) to within a few units, whatever the argument.  With u = 2^-24: the exponential is good to 1 ulp = 2 u and
+    rounded once more when its argument's rounding is put back, 3 u; 1 + e, its reciprocal and the product of the two add u each: 6 u.  ln(2) in one word is off by 2.7e-9 of itself:
+    0.05 u for a unit of the argument, 1.2 u at 24 and 4 u at 80: 8 u and 10 u.  h = f * 1 + (1 - f) * 0 and 0 + (1 - f) * 1 are the gates themselves (one product by 1,
+    one sum with 0: exact), y = o * 1.  A product of two gates has both errors and u, each further product u.  All steps at once and one token take the same gates."""
+    H, n = 4096, 8 if high <= 24 else 10
+    a = torch.linspace(low, high, H, device="cuda:0")
+    a[0], a[-1] = low, high
+    gate = lambda x: (S.sigmoid(host(x)), S.sigmoid(-host(x)))
+    one, far = torch.ones(H, device="cuda:0"), torch.full((H,), float("inf"), device="cuda:0")
+    rel = lambda got, want, units, what: in_bound(host(got), want, units * U * np.abs(want), (what, low))
+
+    def both(f, c, o, h0):
+        """(y, h, saved) of one step, and the same for a token."""
+        gi = torch.cat((f, c, o))[None, None]
+        y, h, saved = B.glr_fwd(gi, None, h0=h0[None])
+        state = h0[None].clone()
+        y2 = B.glr_step(gi[0], state, None)
+        in_bound(host(state), host(h), 2 * U * np.abs(host(h)), "token state")
+        in_bound(host(y2), host(y[0]), 3 * U * np.abs(host(y[0])), "token y")
+        return gi, y, h, saved
+
+    for x in (a, -a):
+        f, keep = gate(x)
+        _, _, h, _ = both(x, 0 * one, 0 * one, one)
+        rel(h[0], f, n, "f")
+        gi, _, h, saved = both(x, one, 0 * one, 0 * one)
+        rel(h[0], keep, n, "1 - f")
+        dgi, dh0 = B.glr_bwd(gi, saved, None, dh_last=one[None])
+        rel(dh0[0], f, n, "dh0")
+        rel(dgi[0, 0, H:2 * H], keep, n, "dc")
+        rel(dgi[0, 0, :H], -f * keep, 2 * n + 1, "df")
+        gi, y, _, saved = both(-far, one, x, one)              # f = 0: h = c = 1
+        rel(y[0, 0], f, n, "o")
+        dgi, _ = B.glr_bwd(gi, saved, None, dy=one[None, None])
+        rel(dgi[0, 0, 2 * H:], f * keep, 2 * n + 2, "do")
+
+
 def test_a_nan_stays_in_its_channel():
     gi, dy, bias, h0, _, _ = make(19, 300, 2, 70, "f32", False)
     want = B.glr_fwd(gi, bias, h0=h0)
