@@ -210,7 +210,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void layernorm_bwd_kerne
         if (row + step < rows) fetch(row + step);
 #pragma unroll
         for (int i = 0; i < S::SIZE; ++i) {
-            v[i] = (v[i] - m) * inv;        // (where the lane has nothing: anything, and d is 0)
+            v[i] = (v[i] - m) * (s.valid(i) ? inv : 0.f);       // (where the lane has nothing: 0, as d is; the product with a large mean could be infinite)
             if (PARAMS) {
                 dg[i] += d[i] * v[i];
                 db[i] += d[i];

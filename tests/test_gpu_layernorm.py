@@ -158,6 +158,27 @@ def test_infinities_and_nan_stay_in_their_rows(C):
         assert y[3].isnan().any() and y[7].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [1, 3, 5, 13, 31, 64, 65, 130, 200])
+def test_constant_rows_of_very_large_values(C, dtype):
+    """Rows whose mean times invstd is beyond the largest float though no difference from the mean is (their values a power of two, whose sum and mean are exact; a single column
+    also of the type's lowest value): xh is 0, and dx what the means of dy * gamma leave.  Lanes without a part of the row must not put anything into its sums."""
+    _, _, dy, dsum, gamma, beta = make(31, 6, C, dtype)
+    top = 2.0 ** 120 if C > 1 else torch.finfo(torch_dtype(dtype)).min
+    s = torch.full((6, C), top, dtype=dy.dtype, device="cuda:0")
+    s[1], s[4] = -top, 1.0
+    y, _, mean, invstd = B.layernorm_fwd(s, gamma, beta)
+    assert torch.equal(mean, s[:, 0].float()) and torch.equal(y, beta.to(s.dtype).expand(6, C))
+    dx, dgamma, dbeta = B.layernorm_bwd(dy, s, gamma, mean, invstd, dsum=dsum)
+    hd, hg, hi = host(dy), host(gamma), host(invstd)
+    want, wg, wb = S.layernorm_bwd(hd, host(s), hg, host(mean), hi, host(dsum))
+    gh = np.abs(hd * hg)
+    parts = hi[:, None] * (gh * 8 * U + (C + 8) * U * gh.mean(axis=1, keepdims=True)) + 2 * U * np.abs(host(dsum))
+    in_bound(host(dx), want, half(dtype) * np.abs(want) + 1.02 * parts + U * np.abs(want) + 1e-38, "dx")
+    assert not wg.any() and not dgamma.any()
+    in_bound(host(dbeta), wb, 8 * U * np.abs(hd).sum(axis=0), "dbeta")
+
+
 @pytest.mark.parametrize("rows,C", [((1 << 31) // 1000 + 40, 1000), ((1 << 22) + 100, 264)])
 def test_many_elements_and_many_rows(rows, C):
     """More than 2^31 elements, 2^32 bytes; and more rows than blocks are launched for: the last rows against the same alone."""
