@@ -136,8 +136,10 @@ class TokenStream:
             s[place].zero_()
 
     def step(self, tokens: torch.Tensor, slots: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """tokens: int32 [n], one for each of the sequences at the places `slots` (int32 [n], none twice; None: the first n).  Returns the logits [n, K] behind
-        them, float; a slot that is no place is idle, and its logits are NaN."""
+        """tokens: int32 [n], one for each of the sequences at the places `slots` (int32 [n], none twice; None: the first n, of which there have to be so many).
+        Returns the logits [n, K] behind them, float; a slot that is no place is idle, and its logits are NaN."""
+        if slots is None and tokens.numel() > self.places:
+            raise ValueError(f"{tokens.numel()} tokens for the first places of {self.places}")
         m, w, ws = self.m, self.m.w, self.ws
         x, residual = B.embedding_fwd(tokens, w["table"]), None
         for k in range(m.L):

@@ -147,3 +147,12 @@ def test_binding_refusals():
         B.param8_table([(z(n), z(n - 1), *state, None, 0.0)])
     with pytest.raises(AssertionError):
         B.param8_table([(z(n), z(n), state[0], state[1], state[2], z(1), None, 0.0)])
+
+
+def test_more_tokens_than_places():
+    """Tokens without slots are those of the first places: more of them are turned away before any state has moved on."""
+    from types import SimpleNamespace
+    from paper_2409_11600_amd.linear_recurrent import TokenStream
+    stream = TokenStream(SimpleNamespace(H=4, L=2, device="cpu", w={"table": torch.zeros(5, 4)}), 3)
+    with pytest.raises(ValueError, match="4 tokens"):
+        stream.step(torch.zeros(4, dtype=torch.int32))

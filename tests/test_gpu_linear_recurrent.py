@@ -107,6 +107,22 @@ def test_tokens_one_by_one_give_the_logits_of_the_sequences(dtype):
     assert max_rel_err(got, want) <= TOL[dtype]
 
 
+@pytest.mark.parametrize("n", [1, 4, 6])
+def test_tokens_without_slots_are_those_of_the_first_places(n):
+    tokens, labels, lengths, p = model(80, 9, 6, 32, 48, 64, 3, 2)
+    m = GpuLinearRecurrentClassifier(tokens, labels, p, lengths)
+    one, other = TokenStream(m, 6), TokenStream(m, 6)
+    tok, first = torch.from_numpy(tokens).cuda(), torch.arange(n, dtype=torch.int32, device="cuda:0")
+    for t in range(9):
+        got, want = one.step(tok[t, :n].clone()), other.step(tok[t, :n].clone(), first)
+        assert got.shape == (n, 3) and torch.equal(got, want) and torch.isfinite(got).all()
+    assert all(torch.equal(a, b) and not a[n:].any() for a, b in zip(one.states, other.states))
+    before = [s.clone() for s in one.states]
+    with pytest.raises(ValueError):
+        one.step(torch.zeros(7, dtype=torch.int32, device="cuda:0"))
+    assert all(torch.equal(a, b) for a, b in zip(one.states, before))
+
+
 def test_forward_and_backward_in_a_graph():
     tokens, labels, lengths, p = model(79, 30, 8, 32, 64, 64, 2, 2)
     stream = torch.cuda.Stream()
