@@ -568,7 +568,10 @@ Plan plan_of(const nsk_glr_desc_t &d, int pass)
     p.z.segments = p.z.stretches <= whole || (p.z.stretches <= kMostWaves && tiles <= 256) ? 1 : ceil_div(p.z.stretches, most);
     p.waves = ceil_div(p.z.stretches, p.z.segments);
     p.z.segments = ceil_div(p.z.stretches, p.waves);
-    p.blocks = (unsigned)(p.z.groups * ((tiles + p.z.groups - 1) / p.z.groups) * p.z.segments);
+    // (as many blocks for every group, so some of them may find nothing left: by what check() lets through, tiles * segments blocks are fewer than 2^32 threads, but these need not be)
+    auto blocks = [&] { return (tiles + p.z.groups - 1) / p.z.groups * p.z.groups * p.z.segments; };
+    if (blocks() * p.waves * 64 >= 1LL << 32) p.z.groups = 1;
+    p.blocks = (unsigned)blocks();
     return p;
 }
 size_t workspace_of(const Plan &p) { return p.z.segments > 1 ? exchange_words(p.z) * sizeof(unsigned) : 0; }

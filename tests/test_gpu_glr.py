@@ -377,6 +377,35 @@ def test_offsets_beyond_32_bits():
             in_bound(host(a.float()), host(b.float()), 2.0 ** -6 * np.abs(host(b.float())) + 1e-4, "part")
 
 
+def test_a_launch_of_nearly_all_threads_that_there_are():
+    """Nine tiles of 70 million steps: with as many blocks for each of eight groups of tiles the launch would have more than 2^32 threads.  The same steps in seven calls, each of which
+    begins with the state that the one before left, take the same stretches and segments: the same bits."""
+    N, T, parts = 9, 70_000_000, 7
+    each = T // parts
+    g = torch.Generator(device="cuda").manual_seed(43)
+    gi = torch.randn((N, T, 3), generator=g, device="cuda:0", dtype=torch.bfloat16).transpose(0, 1)
+    dy = torch.randn((N, T, 1), generator=g, device="cuda:0", dtype=torch.bfloat16).transpose(0, 1)
+    bias, h0, dh_last = torch.tensor([1.0, 0.2, -0.1], device="cuda:0"), torch.randn((N, 1), generator=g, device="cuda:0"), torch.randn((N, 1), generator=g, device="cuda:0")
+    ws = B.Workspace("cuda:0")
+    print("recurrence T=70000000 N=9 H=1 bf16 forward", flush=True)
+    y, h_last, saved = B.glr_fwd(gi, bias, h0=h0, ws=ws)
+    torch.cuda.synchronize()
+    print("backward", flush=True)
+    dgi, dh0 = B.glr_bwd(gi, saved, bias, dy=dy, dh_last=dh_last, ws=ws)
+    torch.cuda.synchronize()
+    cut = lambda t, k: t[k * each:(k + 1) * each]
+    h = h0
+    for k in range(parts):
+        y2, h, s2 = B.glr_fwd(cut(gi, k), bias, h0=h, ws=ws)
+        assert torch.equal(y2, cut(y, k)) and torch.equal(s2, saved[k * each // 16:(k + 1) * each // 16])
+    assert torch.equal(h, h_last)
+    d = dh_last
+    for k in reversed(range(parts)):
+        g2, d = B.glr_bwd(cut(gi, k), saved[k * each // 16:(k + 1) * each // 16], bias, dy=cut(dy, k), dh_last=d, ws=ws)
+        assert torch.equal(g2, cut(dgi, k))
+    assert torch.equal(d, dh0)
+
+
 @pytest.mark.parametrize("T,N,H", [(90, 4, 72), (3000, 1, 64)])
 def test_on_a_stream_and_in_a_graph(T, N, H):
     gi, dy, bias, h0, dh_last, lengths = make(31, T, N, H, "bf16", True)
