@@ -338,18 +338,28 @@ def _pair(v) -> Tuple[int, int]:
 
 class Workspace:
     """Caller-owned scratch buffer, grown on demand and then reused (the paper's pooling idea:
-    nothing is allocated in steady state)."""
+    nothing is allocated in steady state).  A workspace belongs to one stream at a time: calls that run beside each other
+    need one each.  Buffers that became too small are kept as long as it lives: a captured graph, or work on a stream other than
+    the one that the allocator knows them by, may still use them.  A new one is larger by half at least, so that all of them
+    together are at most three times the last."""
 
     def __init__(self, device="cuda:0"):
         self.device = torch.device(device)
         self.buf: Optional[torch.Tensor] = None
+        self.size = 0               # the most that was asked for, which is what calls see
+        self.outgrown = []
 
     def get(self, nbytes: int):
         if nbytes == 0:
             return None, 0
-        if self.buf is None or self.buf.numel() < nbytes:
-            self.buf = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
-        return self.buf.data_ptr(), self.buf.numel()
+        if nbytes > self.size:
+            held = 0 if self.buf is None else self.buf.numel()
+            if nbytes > held:
+                if self.buf is not None:
+                    self.outgrown.append(self.buf)
+                self.buf = torch.empty(max(int(nbytes), held + held // 2), dtype=torch.uint8, device=self.device)
+            self.size = int(nbytes)
+        return self.buf.data_ptr(), self.size
 
 
 def conv_desc(act_dims, filt_dims, stride, pad, dilation, dtype_code, layout) -> nsk_conv_desc_t:

@@ -156,3 +156,24 @@ def test_more_tokens_than_places():
     stream = TokenStream(SimpleNamespace(H=4, L=2, device="cpu", w={"table": torch.zeros(5, 4)}), 3)
     with pytest.raises(ValueError, match="4 tokens"):
         stream.step(torch.zeros(4, dtype=torch.int32))
+
+
+def test_an_outgrown_workspace_is_kept():
+    """What a captured graph or another stream's work may still use is not handed back while the workspace lives; no call that fits makes a new buffer, and ones that want
+    a little more each time do not make a thousand."""
+    import gc
+    import weakref
+    ws = B.Workspace("cpu")
+    assert ws.get(0) == (None, 0)
+    at, size = ws.get(64)
+    assert size == 64 and ws.get(16) == (at, 64) and ws.get(64) == (at, 64)
+    first = weakref.ref(ws.buf)
+    assert ws.get(1 << 20)[1] == 1 << 20 and ws.get(100)[1] == 1 << 20
+    gc.collect()
+    assert first() is not None and first().data_ptr() == at
+    seen = set()
+    for n in range(1000, 2000):
+        at, size = (ws if n > 1000 else (ws := B.Workspace("cpu"))).get(n)
+        assert size == n and ws.buf.data_ptr() == at and ws.buf.numel() >= n
+        seen.add(at)
+    assert len(seen) <= 3 and sum(b.numel() for b in ws.outgrown) <= 2 * ws.buf.numel()
