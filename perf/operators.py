@@ -12,7 +12,6 @@ Recurrence, gates in the order (f, c, o) of gi [T,N,3H], per sequence n and chan
   Its backward pass also takes the states that enter the steps 0, 16, 32, ... (float), which the forward pass leaves.
 AdamW: m and r = sqrt(v) are e4m3 values times a power of two for each 256 elements, rounded at random (the numbers come from a seed).
 """
-import functools
 import math
 
 import numpy as np
@@ -308,11 +307,16 @@ def _plain(state):
 
 # ---------------------------------------------------------------------------------------------------------------- the framework's calls
 
-@functools.lru_cache(maxsize=1)
+_WORKSPACES = {}
+
+
 def _workspace():
-    """The scratch memory that a program keeps for all calls of a stream."""
+    """The scratch memory that a program keeps for the calls of a stream (calls on another one may run beside them)."""
     from paper_2409_11600_amd import binding as B
-    return B.Workspace("cuda:0")
+    key = torch.cuda.current_device(), B._stream()
+    if key not in _WORKSPACES:
+        _WORKSPACES[key] = B.Workspace(torch.device("cuda", key[0]))
+    return _WORKSPACES[key]
 
 
 def _own(state):
