@@ -377,6 +377,64 @@ def test_offsets_beyond_32_bits():
             in_bound(host(a.float()), host(b.float()), 2.0 ** -6 * np.abs(host(b.float())) + 1e-4, "part")
 
 
+def sequences_in_bound(at, inputs, outputs, dtype):
+    """The outputs (y, h_last, saved, dgi, dh0) of the sequences `at` against the oracle."""
+    gi, dy, bias, h0, dh_last, lengths = inputs
+    part = lambda t: host(t[:, at] if t.dim() == 3 else t[at])
+    (states, wy, wg, w0), (es, ey, eg, e0) = bounds(part(gi), host(bias), part(h0), None if lengths is None else lengths[at].cpu().numpy(), part(dy), part(dh_last))
+    y, h_last, saved, dgi, dh0 = (part(t) for t in outputs)
+    r = half(dtype)
+    in_bound(h_last, states[-1], es[-1], "h_last")
+    in_bound(saved, states[:-1][::16], es[:-1][::16], "saved")
+    in_bound(y, wy, ey * (1 + r) + r * np.abs(wy), "y")
+    in_bound(dgi, wg, eg * (1 + r) + r * np.abs(wg), "dgi")
+    in_bound(dh0, w0, e0, "dh0")
+
+
+@pytest.mark.parametrize("dtype,T,N,H,stride", [("bf16", 300, 3, 65, (1 << 29) + 24), ("f32", 300, 3, 65, (1 << 28) + 20), ("bf16", 40, 2, 7, (1 << 31) + 8), ("f32", 700, 2, 130, (1 << 30) + 4),
+                                                ("bf16", 300, 9, 7, 54_000_000)])
+def test_sequences_far_from_each_other(dtype, T, N, H, stride):
+    """Sequences that begin so far from each other that a tile cannot go on from one to the next (a lane's offset has 30 bits), against the oracle; nothing else is written.
+    In the last case it is a tile's ten sequences that are too far for the bits, not two of them.  Where dense tensors have as few tiles, and so blocks of the same size, their bits."""
+    print(f"recurrence, far apart, T={T} N={N} H={H} {dtype} stride={stride}", flush=True)
+    gi, dy, bias, h0, dh_last, lengths = make(T + H, T, N, H, dtype, True)
+    dense = check(gi, dy, bias, h0, dh_last, lengths, dtype)
+
+    def far(width, fill):
+        buf = torch.full(((N - 1) * stride + T * width,), fill, dtype=gi.dtype, device="cuda:0")
+        return buf, buf.as_strided((T, N, width), (width, stride, 1))
+
+    (_, fgi), (_, fdy), (by, fy), (bg, fg) = far(3 * H, 0.0), far(H, 0.0), far(H, float("nan")), far(3 * H, float("nan"))
+    fgi.copy_(gi), fdy.copy_(dy)
+    _, h2, s2 = B.glr_fwd(fgi, bias, h0=h0, lengths=lengths, y=fy)
+    _, d2 = B.glr_bwd(fgi, s2, bias, dy=fdy, dh_last=dh_last, lengths=lengths, dgi=fg)
+    torch.cuda.synchronize()
+    sequences_in_bound(list(range(N)), (gi, dy, bias, h0, dh_last, lengths), (fy, h2, s2, fg, d2), dtype)
+    if N * -(-H // 64) < 8:
+        assert all(torch.equal(a, b) for a, b in zip((fy, h2, s2, fg, d2), dense))
+    for buf, part in ((by, fy), (bg, fg)):
+        part.fill_(float("nan"))
+        assert all(bool(buf[k:k + (1 << 28)].isnan().all()) for k in range(0, buf.numel(), 1 << 28))
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,H", [(140, 1024, 64), (230, 700, 96), (170, 1024, 64), (330, 520, 128)])
+def test_small_blocks_where_tiles_are_many(T, N, H, dtype, ragged):
+    """Blocks of three stretches (9, 15 and 21 of them) and of two (11), in both directions: sequences here and there against the oracle, and all the same bits twice."""
+    print(f"recurrence, small blocks, T={T} N={N} H={H} {dtype} ragged={ragged}", flush=True)
+    gi, dy, bias, h0, dh_last, lengths = make(T + N, T, N, H, dtype, ragged)
+    ws = B.Workspace("cuda:0")
+
+    def run():
+        y, h_last, saved = B.glr_fwd(gi, bias, h0=h0, lengths=lengths, ws=ws)
+        return (y, h_last, saved, *B.glr_bwd(gi, saved, bias, dy=dy, dh_last=dh_last, lengths=lengths, ws=ws))
+
+    got = run()
+    assert all(torch.equal(a, b) for a, b in zip(run(), got))
+    sequences_in_bound([0, 1, 2, 3, 63, 64, N // 2, N - 65, N - 2, N - 1], (gi, dy, bias, h0, dh_last, lengths), got, dtype)
+
+
 def test_a_launch_of_nearly_all_threads_that_there_are():
     """Nine tiles of 70 million steps: with as many blocks for each of eight groups of tiles the launch would have more than 2^32 threads.  The same steps in seven calls, each of which
     begins with the state that the one before left, take the same stretches and segments: the same bits."""
