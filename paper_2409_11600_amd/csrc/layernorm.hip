@@ -377,9 +377,10 @@ Plan plan_of(const nsk_layernorm_desc_t &d)
     if (vectors <= 2048) return {1024, 2};
     return {0, 0};
 }
-// The pass that makes dx also makes the sums for gamma and beta, unless their registers would not fit (16384 bf16 columns, 2048 rows: 147 us with spilled ones,
-// 31 for dx alone).
-constexpr bool on_the_way(Plan p) { return p.lanes > 0 && !(p.lanes == 1024 && p.k == 2); }
+// The pass that makes dx also makes the sums for gamma and beta, unless their registers would not fit: two vectors of each of 1024 lanes, which in bf16 are 16 elements and spill 125
+// registers, in fp32 8 and 6.  us with it / with a pass of its own for the sums: bf16, dsum, 2048 x 12000 150 / 62, 2048 x 16384 167 / 83; fp32, dsum, 4000 x 6000 79 / 113, 4000 x 8192
+// 109 / 154, 2000 x 5000 36 / 48, 300 x 8192 16 / 21, 4000 x 6000 without dsum 59 / 99.
+constexpr bool on_the_way(Plan p, size_t element_bytes) { return p.lanes > 0 && !(p.lanes == 1024 && p.k == 2 && element_bytes == 2); }
 int rows_a_block(const Plan &p) { return p.lanes == 0 || p.lanes >= 256 ? 1 : 256 / p.lanes; }
 // Blocks of the backward pass, each with sums of its own; 512, two a compute unit, are what its registers leave room for at once.  us with dsum, 256 / 512 / 1024 of them:
 // 10000 x 256 fp32 13.4, 13.0, 13.6; 65536 x 768 bf16 86, 79, 87; 65536 x 768 fp32 225, 150, 157; 300000 x 64 bf16 42, 34, 37.
@@ -470,7 +471,7 @@ int nsk_layernorm_bwd(const nsk_layernorm_desc_t *desc, const void *s, const voi
     float *const partial = (float *)workspace;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        if (params && !on_the_way(p))
+        if (params && !on_the_way(p, sizeof(T)))
             hipLaunchKernelGGL(layernorm_dparam_wide_kernel<T>, dim3((unsigned)shares, (unsigned)ceil_div(C, 256)), dim3(256), 0, st, (const T *)s, (const T *)dy, save_mean, save_invstd,
                                partial, desc->rows, C);
         if (p.lanes == 0)
@@ -479,7 +480,7 @@ int nsk_layernorm_bwd(const nsk_layernorm_desc_t *desc, const void *s, const voi
         with(p, [&](auto lanes, auto k) {
             constexpr int L = decltype(lanes)::value, N = decltype(k)::value;
             const dim3 block(L > 256 ? L : 256);
-            constexpr bool ON_THE_WAY = on_the_way({L, N});
+            constexpr bool ON_THE_WAY = on_the_way({L, N}, sizeof(T));
             if (params && ON_THE_WAY)
                 hipLaunchKernelGGL((layernorm_bwd_kernel<T, L, N, ON_THE_WAY>), grid, block, L < 256 ? 2 * C * sizeof(float) : 0, st, (const T *)s, (const T *)dy, (const T *)dsum, gamma, save_mean,
                                    save_invstd, (T *)dx, partial, desc->rows, C);
