@@ -8,13 +8,12 @@ from paper_2409_11600_amd import binding as B
 
 def test_each_stream_has_its_own(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(operators, "_WORKSPACES", {})
     made = {}
     for stream in (0, 71, 0, 72, 71):
         monkeypatch.setattr(B, "_stream", lambda: stream)
         assert made.setdefault(stream, operators._workspace()) is operators._workspace()
     assert len({id(ws) for ws in made.values()}) == 3
-    for stream in (71, 72):
-        del operators._WORKSPACES[0, stream]
 
 
 @pytest.mark.gpu
