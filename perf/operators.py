@@ -313,10 +313,10 @@ _WORKSPACES = {}
 def _workspace():
     """The scratch memory that a program keeps for the calls of a stream (calls on another one may run beside them)."""
     from paper_2409_11600_amd import binding as B
-    key = torch.cuda.current_device(), B._stream()
-    if key not in _WORKSPACES:
-        _WORKSPACES[key] = B.Workspace(torch.device("cuda", key[0]))
-    return _WORKSPACES[key]
+    stream = B._stream()
+    if stream not in _WORKSPACES:
+        _WORKSPACES[stream] = B.Workspace("cuda:0")
+    return _WORKSPACES[stream]
 
 
 def _own(state):
