@@ -503,7 +503,8 @@ int nsk_layernorm_bwd(const nsk_layernorm_desc_t *desc, const void *s, const voi
  * or NULL.  For every sequence n and channel, steps t < lengths[n] (NULL: all T):
  *   f = sigmoid(gi_f + b_f),  c = gi_c + b_c,  o = sigmoid(gi_o + b_o),  h_t = f * h_{t-1} + (1 - f) * c,  y_t = o * h_t.
  * In later steps h stays, y and the gradients are zero and gi, dy are not used, whatever they hold.  A length below 0 counts as
- * 0, one above T as T.  States are float throughout.
+ * 0, one above T as T.  States are float throughout.  Steps are grouped, h behind a group being A * h + B with A the product of
+ * its gates: where h is infinite and A so small that it is 0 in float, that is NaN.
  * Rows of 3H (gi, dgi) and H (y, dy) elements are contiguous; strides say where they begin: element (t, n, 0) lies at
  * t * gi_t + n * gi_n.  Both strides of a pair 0: dense [T,N,..].  [N,T,..] is gi_n = T * gi_t.  Rows must not overlap, and
  * the rows of one step or those of one sequence have to lie together (no row of another one between them). */
@@ -546,7 +547,8 @@ int nsk_glr_step(int dtype, int N, int H, int S, const void *gi, const float *bi
  * thousandth in a step and would stand still if rounded to nearest.  An r above zero is never held as zero, so that no weight is
  * divided by eps alone.  Infinite or NaN moments become NaN and do not enter the scale: they stay with their element.
  * The random bits are a function of `seed`, the tensor's place in `params` and the element's in the tensor; a caller takes
- * another seed for every step.  With mix(x): x ^= x >> 16, x *= 0x243F6A89, x ^= x >> 15, x *= 0xB7E15163, x ^= x >> 16 on 32
+ * another seed for every step.  (A captured graph keeps the step and the seed that it was captured with: replayed, it would
+ * round every step with the same bits, whose mean is not the exact value.  The call stays outside of graphs that are replayed.)  With mix(x): x ^= x >> 16, x *= 0x243F6A89, x ^= x >> 15, x *= 0xB7E15163, x ^= x >> 16 on 32
  * bits, element i of tensor k has u = mix(i * 0x9E3779B9 + (i >> 32) * 0x85A308D3 + mix(seed + k * 0x9E3779B9)); a magnitude is
  * rounded up where the part below its last place is at least 1 - (u & 0xffff) / 65536 of a place (m), (u >> 16) for r. */
 #define NSK_ADAMW8_BLOCK 256

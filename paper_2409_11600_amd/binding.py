@@ -1191,7 +1191,8 @@ def adamw8_state(n: int, device="cuda:0"):
 
 def param8_table(records):
     """records: iterable of (w, grad, m, r, scale_m, scale_r, w_lp or None, weight_decay) -> ctypes array of nsk_param8_t (keep the tensors
-    alive while it is in use)."""
+    alive while it is in use).  Pointers and sizes alone, made once and used for every step; it takes 3 us a tensor on the host, many
+    times the step of small ones, so gradients had better keep their buffers."""
     records = list(records)
     tab = (nsk_param8_t * len(records))()
     for i, (w, g, m, r, sm, sr, lp, wd) in enumerate(records):

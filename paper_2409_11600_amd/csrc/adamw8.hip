@@ -77,8 +77,8 @@ __device__ inline unsigned wave_max(unsigned v)
 }
 
 // A wavefront takes a block of 256 elements, four a lane: 16 bytes of w and g, 4 of m and r, and the largest magnitudes by exchange among its lanes, no LDS.
-// Bound by memory, 20 or 22 bytes a weight: 64 million weights in 82 tensors with copies 258 us (5.5 TB/s), 8.8 million in 7 without 30 us (5.9 TB/s, partly from
-// the last-level cache), 95 small tensors 9 us for two launches.  Of 450 vector instructions a block 4 in 10 are the correctly rounded square root, the random
+// Bound by memory, 20 or 22 bytes a weight: 64 million weights in 82 tensors with copies 258 us (5.5 TB/s), 8.8 million in 7 without 34 us (5.2 TB/s; 30 where
+// they are still in the last-level cache), 95 small tensors 10 us for two launches.  Of 450 vector instructions a block 4 in 10 are the correctly rounded square root, the random
 // bits and the rounding; the update's quotient takes the hardware's reciprocal (1 ulp), which no held value depends on.
 __global__ __launch_bounds__(256) void adamw8_kernel(const Table tab, Coef ac, const float *__restrict__ grad_scale)
 {

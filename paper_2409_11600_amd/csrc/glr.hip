@@ -341,11 +341,11 @@ template <typename F> __device__ inline float join(const Sizes &z, const Exchang
     return mine;
 }
 
-// Bound by memory where tiles are many (3 + 1 elements and 1/4 byte a step and channel): bf16, T=2048, N=32, 768 channels 86 us, 4.8 TB/s of what a copy reaches 5.1 of;
+// Bound by memory where tiles are many (3 + 1 elements and 1/4 byte a step and channel): bf16, T=2048, N=32, 768 channels 87 us, 4.8 TB/s of what a copy reaches 5.1 of;
 // the vector unit, with four transcendental of some 25 instructions a step, is half busy.  By the hand-over where tiles are few: bf16, T=65536, N=1, 512 channels
-// 78 us (3.6 TB/s; of the 13 us that a block lasts, its number takes 1, its loads 2, its steps 2, looking back 5 to 6: two or three loads one behind the other, 2 us each while the memory is
+// 77 us (3.6 TB/s; of the 13 us that a block lasts, its number takes 1, its loads 2, its steps 2, looking back 5 to 6: two or three loads one behind the other, 2 us each while the memory is
 // loaded); and by one chain of loads, gates and stores where a call is short: fp32, T=200,
-// N=50, 256 channels 11 us for 42 MB.  (Wider look-backs, 8 or 16 segments at a time or 4 by each wavefront, cost more in traffic than they gave: 92, 97, 118 us for the long one.)
+// N=50, 256 channels 12 us for 42 MB.  (Wider look-backs, 8 or 16 segments at a time or 4 by each wavefront, cost more in traffic than they gave: 92, 97, 118 us for the long one.)
 template <typename T>
 __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
                                                        const float *__restrict__ h0, T *__restrict__ y, float *__restrict__ h_last, float *__restrict__ saved)
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(1024) void glr_fwd_kernel(Sizes z, Exchange ex, con
     if (ends) store_zeros(out, z.y_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.y, 0, 1);
 }
 
-// bf16, T=2048, N=32, 768 channels 142 us, 5.1 TB/s; fp32 with lengths and odd rows, T=777, N=33, 201 channels 36 us; T=200, N=50, fp32 256 channels 14.9 us.
+// bf16, T=2048, N=32, 768 channels 144 us, 5.0 TB/s; fp32 with lengths and odd rows, T=777, N=33, 201 channels 36 us; T=200, N=50, fp32 256 channels 15.4 us.
 // Backwards a stretch takes E, the gradient of the state that leaves it, to A E + B.  What a step needs for that: f, u = dy o, and with the states, which
 // come from the saved one, k = 1 - f and d = (h_{t-1} - c) f (1 - f).  The gradient of the gate o depends on nothing later.
 template <typename T>
@@ -499,6 +499,8 @@ __global__ __launch_bounds__(1024) void glr_bwd_kernel(Sizes z, Exchange ex, con
     if (ends) store_zeros(dgi + at, z.gi_t, len - t0, z.T - t0 < kStretch ? z.T - t0 : kStretch, l.gi, gate, 3);
 }
 
+// An element a lane, 64 of a sequence a block.  us on the device in bf16 / fp32 (floor): N=50, 256 channels 2.6, latency alone; N=1024, 1024 channels 6.8 / 7.1 (3.3 / 4.9), from the last-level
+// cache, and less than the host takes for the call; N=4096, 2048 channels 33.6 / 41.4 (26.4 / 39.6): memory in fp32; in bf16 loads and stores of 2 bytes a lane reach 4.0 TB/s.
 template <typename T>
 __global__ __launch_bounds__(64) void glr_step_kernel(int H, int S, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ slots,
                                                       float *__restrict__ state, T *__restrict__ y, unsigned tiles)

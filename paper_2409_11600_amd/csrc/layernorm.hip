@@ -4,7 +4,7 @@
 //   dgamma = sum over rows of dy * xh,  dbeta = sum over rows of dy
 // Bound by memory: a row is read once and stays in the registers of the lanes that share it (2 to 1024 of them), so that the variance is the mean square of
 // the differences from the mean itself, and the backward pass sums dy * xh and dy for the weights on the way.  us (TB/s of what has to move): 65536 x 768 bf16 with a
-// residual 70 (5.8), backward 61 (4.9); 30011 x 1001 bf16 backward 39-44 (4.1-4.6), as fast as rows of 1000 or 1008; 10000 x 256 fp32 backward 10.2 and the joining
+// residual 71 (5.7), backward 61 (4.9); 30011 x 1001 bf16 backward 39-44 (4.1-4.6), as fast as rows of 1000 or 1008; 10000 x 256 fp32 backward 10.2 and the joining
 // launch 3.4; 300000 x 64 bf16 13.8 (5.6).  The backward pass has the next row of each lane on its way while one is worked on: its registers leave room for two
 // wavefronts a SIMD, and those alone had 24 KB a compute unit in flight (65536 x 768 bf16 121 us without).
 #include "nsk_internal.h"

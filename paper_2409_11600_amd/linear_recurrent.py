@@ -3,7 +3,8 @@ product back onto the residual stream -> layer norm of the last block's final st
 
 It stands next to the GRU classifier (recurrent.py) and takes the same batches, here with a length for each sequence.  Where that one has 2T steps that wait for each
 other, all steps of a block are one call here.  Sequencing and buffer management only: every arithmetic step is a libnsk entry point; all buffers are created in the
-constructor, a step allocates nothing, and forward() and backward() can be captured into a HIP graph.
+constructor, a step allocates nothing, and forward() and backward() can be captured into a HIP graph (update() takes another step and seed each time, which a
+graph would keep).
 
 TokenStream is the same network for tokens that come one by one: the states of any number of live sequences lie in tables, and a step takes a token for some of them.
 """
