@@ -564,6 +564,86 @@ int nsk_adamw8_step_multi(int count, const nsk_param8_t *params, int step, unsig
                           float eps, const float *grad_scale, void *stream);
 
 /* ---------------------------------------------------------------------------------------------------------------
+ * A sequence model that learns from a larger one: embedding with a scale and a gradient whose time does not depend on how often
+ * words occur, a recurrence whose state is a matrix (the gated delta rule), and the loss against a teacher's largest logits.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Scaled embedding: out[i] = scale * table[tokens[i]], rounded once; rows of tokens equal to `pad` are zeros (pad: a token of
+ * [0,V), or -1: none).  Types, shapes and tokens outside [0,V) (rows of NaN, no gradient) as nsk_embedding_fwd. */
+int nsk_embedding_scaled_fwd(int dtype, int n, int E, int V, const int *tokens, const void *table, float scale, int pad, void *out,
+                             void *stream);
+/* dtable[v] (+)= scale * sum over the positions i with tokens[i] == v != pad of dout[i], as nsk_embedding_bwd.  The positions are sorted by
+ * token in the call and every token's rows are added in order of position, in stretches of a fixed number of sorted positions that are joined
+ * in order: bitwise reproducible, and a token that occurs in half of the positions takes no longer than others.  Where nsk_embedding_bwd
+ * reads all tokens once for each of up to 1024 blocks, this reads them a few times. */
+size_t nsk_embedding_scaled_bwd_workspace_bytes(int n, int E, int V);
+int nsk_embedding_scaled_bwd(int dtype, int n, int E, int V, const int *tokens, const void *dout, float scale, int pad, float *dtable,
+                             int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gated delta rule.  gi: [T,N,W], W = 2*Hk*D + H*Dv + 2*H, one product of the layer's input, in the order (q, k, v, a, b): q and k of Hk heads
+ * of D each, v of H heads of Dv, a and b of H; bias: float [2H] for (a, b), or NULL.  Head h uses the query and key of head h / (H / Hk).
+ * With e = NSK_DELTA_EPS, a state S [D,Dv] for every sequence n and head, and for steps t < lengths[n] (NULL: all T):
+ *   k^ = k / sqrt(|k|^2 + e),  q^ = q / sqrt(D * (|q|^2 + e)),  alpha = sigmoid(a + bias_a),  beta = sigmoid(b + bias_b),
+ *   S' = alpha S_{t-1},  S_t = S' + k^ (beta * (v - S'^T k^))^T,  o_t = S_t^T q^.
+ * In later steps S stays, o and the gradients are zero and gi, d_o are not used, whatever they hold.  A length below 0 counts as 0,
+ * one above T as T.  States are float throughout.  Steps are taken in chunks of 64: where a value of a step is not finite, so may be what
+ * is returned for other steps of its chunk.
+ * Rows of W (gi, dgi) and H*Dv (o, d_o) elements are contiguous; strides as in nsk_glr_desc_t.  D and Dv are at most 128; multiples of
+ * 8 with strides that are multiples of 16 bytes are loaded in vectors. */
+#define NSK_DELTA_CHUNK 64
+#define NSK_DELTA_EPS 1e-6f
+typedef struct {
+    int T, N, H, Hk, D, Dv;
+    int dtype;               /* of gi, o, d_o, dgi */
+    long long gi_t, gi_n;    /* of gi and dgi */
+    long long o_t, o_n;      /* of o and d_o */
+} nsk_delta_desc_t;
+/* Bytes of `saved`: float [ceil(T / NSK_DELTA_CHUNK)][N][H][D][Dv], the states that enter the steps 0, 64, 128, ...; 0 for an invalid
+ * descriptor.  Host only. */
+size_t nsk_delta_saved_bytes(const nsk_delta_desc_t *desc);
+/* Workspace of a pass (NSK_PASS_FWD, NSK_PASS_DGRAD); may be 0.  A call has it to itself while it runs; what it held before does not matter.
+ * Host only. */
+size_t nsk_delta_workspace_bytes(const nsk_delta_desc_t *desc, int pass);
+/* h0: float [N,H,D,Dv], NULL: zeros.  o: NULL if only the last state is wanted; h_last: NULL or float [N,H,D,Dv], the state after the last
+ * step; one of the two at least.  saved: NULL where no backward pass follows. */
+int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0, void *o,
+                  float *h_last, float *saved, void *workspace, size_t workspace_bytes, void *stream);
+/* d_o: NULL (no gradient of o), dh_last: NULL or float [N,H,D,Dv]; one of the two at least.  dgi: as gi; the column sums of its last 2H
+ * columns are the bias gradients.  dh0: NULL or float [N,H,D,Dv].  Fixed order of summation. */
+int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *saved,
+                  const void *d_o, const float *dh_last, void *dgi, float *dh0, void *workspace, size_t workspace_bytes, void *stream);
+/* One token for each of N sequences whose states lie in a table, state: float [S,H,D,Dv], updated in place.  gi: [N,W], o: [N,H*Dv] (NULL: not
+ * wanted).  slots: int [N], the entry of the table that holds sequence n's state, none twice; NULL: entry n.  A slot outside [0,S) is an idle
+ * place of the batch: o is zero there and no state changes. */
+int nsk_delta_step(int dtype, int N, int H, int Hk, int D, int Dv, int S, const void *gi, const float *bias, const int *slots,
+                   float *state, void *o, void *stream);
+
+/* Distillation: cross entropy against the M largest logits of a teacher.  Per row n, with p = softmax(top_logits[n] / tau) over the places whose
+ * index is not negative and q = softmax(logits[n] / tau) over all K:
+ *   per_row[n] = tau^2 * sum_m p_m * (log p_m - log q[top_index[n][m]]),   loss[0] = sum_n w_n * per_row[n] / sum_n w_n.
+ * weights: float [N], not negative, or NULL: ones.  A row of weight 0 is not read, and one without a place has loss and gradient 0 whatever
+ * its logits hold; where all weights are 0 the loss is 0.  The tau^2 keeps gradients of different temperatures alike.  top_index: int [N,M], the same index may
+ * occur several times (its places add up), one of K or more makes the row NaN; top_logits: float [N,M].  M is at most NSK_DISTILL_MOST.
+ * Row n of the logits begins at n * ld (0: dense).  A logit may be -infinity (q is 0 there; the loss is infinite where p is not). */
+#define NSK_DISTILL_MOST 1024
+typedef struct {
+    int N, K, M;
+    int dtype;               /* of logits, dlogits */
+    long long ld;            /* elements from a row of logits (dlogits) to the next; 0: K */
+    float tau;               /* above 0 */
+} nsk_distill_desc_t;
+/* Workspace of nsk_distill_fwd; may be 0 (0 also for an invalid descriptor).  Host only. */
+size_t nsk_distill_workspace_bytes(const nsk_distill_desc_t *desc);
+/* per_row: float [N], loss: float [1].  saved: float [N+1][2], for the backward pass: of each row the largest logit / tau and
+ * 1 / sum_k exp(logits / tau - it) (0 and 0 where the weight is 0), then sum_n w_n and its reciprocal (0 where it is 0).  Fixed order of summation. */
+int nsk_distill_fwd(const nsk_distill_desc_t *desc, const void *logits, const int *top_index, const float *top_logits,
+                    const float *weights, float *per_row, float *loss, float *saved, void *workspace, size_t workspace_bytes, void *stream);
+/* dlogits[n][k] (+)= dloss * w_n / sum(w) * tau * (q[k] - sum of p_m over the places with index k), rounded once; columns from K to ld stay.
+ * With accumulate = 0 dlogits may be the buffer of logits. */
+int nsk_distill_bwd(const nsk_distill_desc_t *desc, const void *logits, const int *top_index, const float *top_logits,
+                    const float *weights, const float *saved, float dloss, void *dlogits, int accumulate, void *stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
  * Device memory pool and cache (section "Caching and Pooling"): what hands out the raw pointers every entry point
  * above takes, for callers that have no allocator of their own.  Host code; no entry point above uses it.
  *

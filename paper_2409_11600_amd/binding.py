@@ -67,6 +67,14 @@ class nsk_glr_desc_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("T", "N", "H", "dtype")] + [(n, ctypes.c_longlong) for n in ("gi_t", "gi_n", "y_t", "y_n")]
 
 
+class nsk_delta_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("T", "N", "H", "Hk", "D", "Dv", "dtype")] + [(n, ctypes.c_longlong) for n in ("gi_t", "gi_n", "o_t", "o_n")]
+
+
+class nsk_distill_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "K", "M", "dtype")] + [("ld", ctypes.c_longlong), ("tau", ctypes.c_float)]
+
+
 class nsk_param8_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w", "grad", "m", "r", "scale_m", "scale_r", "w_lp")] + [("n", ctypes.c_size_t), ("weight_decay", ctypes.c_float)]
 
@@ -247,6 +255,29 @@ def lib() -> ctypes.CDLL:
         L.nsk_glr_step.argtypes = [ci, ci, ci, ci] + [vp] * 6
         L.nsk_adamw8_step_multi.restype = ci
         L.nsk_adamw8_step_multi.argtypes = [ci, ctypes.POINTER(nsk_param8_t), ci, ctypes.c_uint] + [ctypes.c_float] * 4 + [vp, vp]
+        dd, td = ctypes.POINTER(nsk_delta_desc_t), ctypes.POINTER(nsk_distill_desc_t)
+        L.nsk_embedding_scaled_fwd.restype = ci
+        L.nsk_embedding_scaled_fwd.argtypes = [ci, ci, ci, ci, vp, vp, ctypes.c_float, ci, vp, vp]
+        L.nsk_embedding_scaled_bwd_workspace_bytes.restype = sz
+        L.nsk_embedding_scaled_bwd_workspace_bytes.argtypes = [ci, ci, ci]
+        L.nsk_embedding_scaled_bwd.restype = ci
+        L.nsk_embedding_scaled_bwd.argtypes = [ci, ci, ci, ci, vp, vp, ctypes.c_float, ci, vp, ci, vp, sz, vp]
+        L.nsk_delta_saved_bytes.restype = sz
+        L.nsk_delta_saved_bytes.argtypes = [dd]
+        L.nsk_delta_workspace_bytes.restype = sz
+        L.nsk_delta_workspace_bytes.argtypes = [dd, ci]
+        L.nsk_delta_fwd.restype = ci
+        L.nsk_delta_fwd.argtypes = [dd] + [vp] * 7 + [vp, sz, vp]
+        L.nsk_delta_bwd.restype = ci
+        L.nsk_delta_bwd.argtypes = [dd] + [vp] * 8 + [vp, sz, vp]
+        L.nsk_delta_step.restype = ci
+        L.nsk_delta_step.argtypes = [ci] * 7 + [vp] * 6
+        L.nsk_distill_workspace_bytes.restype = sz
+        L.nsk_distill_workspace_bytes.argtypes = [td]
+        L.nsk_distill_fwd.restype = ci
+        L.nsk_distill_fwd.argtypes = [td] + [vp] * 7 + [vp, sz, vp]
+        L.nsk_distill_bwd.restype = ci
+        L.nsk_distill_bwd.argtypes = [td] + [vp] * 5 + [ctypes.c_float, vp, ci, vp]
         L.nsk_pool_create.restype = ci
         L.nsk_pool_create.argtypes = [ci, vpp]
         L.nsk_pool_get.restype = ci
@@ -289,11 +320,16 @@ EXPORTS = ("nsk_version", "nsk_test_hooks_reload", "nsk_status_string", "nsk_las
            "nsk_gru_step_supported", "nsk_gru_step_fwd", "nsk_gru_step_bwd", "nsk_gru_seq_blocks", "nsk_gru_seq_fwd", "nsk_gru_seq_bwd",
            "nsk_layernorm_bwd_workspace_bytes", "nsk_layernorm_fwd", "nsk_layernorm_bwd", "nsk_glr_saved_bytes", "nsk_glr_workspace_bytes",
            "nsk_glr_fwd", "nsk_glr_bwd", "nsk_glr_step", "nsk_adamw8_step_multi",
+           "nsk_embedding_scaled_fwd", "nsk_embedding_scaled_bwd_workspace_bytes", "nsk_embedding_scaled_bwd", "nsk_delta_saved_bytes",
+           "nsk_delta_workspace_bytes", "nsk_delta_fwd", "nsk_delta_bwd", "nsk_delta_step", "nsk_distill_workspace_bytes", "nsk_distill_fwd", "nsk_distill_bwd",
            "nsk_pool_create", "nsk_pool_get", "nsk_pool_put", "nsk_pool_cached", "nsk_pool_stats", "nsk_pool_destroy")
 NSK_POOL_DEVICE, NSK_POOL_HOST = 0, 1
 NSK_SUMSQ_PARTIALS = 256
 NSK_GLR_STRETCH = 16
 NSK_ADAMW8_BLOCK = 256
+NSK_DELTA_CHUNK = 64
+NSK_DELTA_EPS = 1e-6
+NSK_DISTILL_MOST = 1024
 
 
 def __getattr__(name):  # raw entry points under their C names: binding.nsk_conv2d_fwd(...)
@@ -1210,6 +1246,189 @@ def adamw8_step_multi(tab, step, seed, lr, beta1=0.9, beta2=0.999, eps=1e-8, gra
     """In place on the tensors of param8_table; seed: a number below 2^32, another one for every step."""
     _check(lib().nsk_adamw8_step_multi(len(tab), tab, int(step), int(seed), float(lr), float(beta1), float(beta2), float(eps), _ptr(grad_scale), _stream()),
            "nsk_adamw8_step_multi")
+
+
+# ------------------------------------------------------------------------------------ a model that learns from a larger one
+
+def _ints(t, *shape):
+    """A pointer to t: an int32 tensor of that shape on the GPU."""
+    if t.dtype is not torch.int32 or t.shape != shape:
+        raise ValueError(f"an int32 tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def embedding_scaled_fwd(tokens, table, scale=1.0, pad=None, out=None):
+    """out[i] = scale * table[tokens[i]], zeros where tokens[i] == pad.  tokens: int32 of any shape; out: [n, E]."""
+    n, (V, E) = tokens.numel(), table.shape
+    if out is None:
+        out = torch.empty(n, E, dtype=table.dtype, device=table.device)
+    else:
+        _like(out, table.dtype, (n, E)), _ptr(out)
+    _check(lib().nsk_embedding_scaled_fwd(_dtype_code(table), n, E, V, _ints(tokens, *tokens.shape), _ptr(table), scale, -1 if pad is None else pad, out.data_ptr(), _stream()),
+           "nsk_embedding_scaled_fwd")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _embedding_scaled_need(n, E, V):
+    return lib().nsk_embedding_scaled_bwd_workspace_bytes(n, E, V)
+
+
+def embedding_scaled_bwd(tokens, dout, V, scale=1.0, pad=None, dtable=None, accumulate=False, ws: Optional[Workspace] = None):
+    """Gradient of the table, float [V, E]; dout: [n, E]."""
+    n, E = tokens.numel(), dout.shape[-1]
+    if dout.numel() != n * E:
+        raise ValueError(f"a row of dout for each of {n} tokens is wanted, got {tuple(dout.shape)}")
+    if dtable is None:
+        assert not accumulate
+        dtable = torch.empty(V, E, dtype=torch.float32, device=dout.device)
+    else:
+        _floats(dtable, V, E), _ptr(dtable)
+    ws = ws or Workspace(dout.device)
+    wp, wb = ws.get(_embedding_scaled_need(n, E, V))
+    _check(lib().nsk_embedding_scaled_bwd(_dtype_code(dout), n, E, V, _ints(tokens, *tokens.shape), _ptr(dout), scale, -1 if pad is None else pad, dtable.data_ptr(),
+                                          int(bool(accumulate)), wp, wb, _stream()), "nsk_embedding_scaled_bwd")
+    return dtable
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _delta_call(T, N, heads, dtype, gi_t, gi_n, o_t, o_n, which):
+    ref = ctypes.byref(nsk_delta_desc_t(T, N, *heads, dtype, gi_t, gi_n, o_t, o_n))
+    return ref, lib().nsk_delta_workspace_bytes(ref, which)
+
+
+def _delta_width(gi, heads):
+    H, Hk, D, Dv = heads
+    if gi.shape[-1] != 2 * Hk * D + H * (Dv + 2):
+        raise ValueError(f"gi holds (q, k, v, a, b) in rows of {2 * Hk * D + H * (Dv + 2)} for (H, Hk, D, Dv) = {heads}, got {tuple(gi.shape)}")
+    return heads
+
+
+def delta_fwd(gi, heads, bias=None, h0=None, lengths=None, o=None, h_last=None, saved=None, want_o=True, save=True, ws: Optional[Workspace] = None):
+    """All steps of the gated delta rule.  heads: (H, Hk, D, Dv); gi [T,N,2*Hk*D + H*Dv + 2*H], time-major, or a transposed view of [N,T,..]; an o
+    [T,N,H*Dv] that is not given lies as gi does.  Returns (o, h_last, saved): saved is what delta_bwd reads, None with save=False; o is None with
+    want_o=False."""
+    H, Hk, D, Dv = _delta_width(gi, heads)
+    T, N, _ = gi.shape
+    dev, (gt, gn, _) = gi.device, gi.stride()
+    if o is None and want_o:
+        o = torch.empty(T, N, H * Dv, dtype=gi.dtype, device=dev) if gt >= gn else torch.empty(N, T, H * Dv, dtype=gi.dtype, device=dev).transpose(0, 1)
+    else:
+        _like(o, gi.dtype, (T, N, H * Dv))
+    if h_last is None:
+        h_last = torch.empty(N, H, D, Dv, dtype=torch.float32, device=dev)
+    else:
+        _floats(h_last, N, H, D, Dv)
+    chunks = -(-T // NSK_DELTA_CHUNK)
+    if saved is not None:
+        _floats(saved, chunks, N, H, D, Dv)
+    elif save:
+        saved = torch.empty(chunks, N, H, D, Dv, dtype=torch.float32, device=dev)
+    _floats(bias, 2 * H), _floats(h0, N, H, D, Dv)
+    ot, on, _ = (0, 0, 1) if o is None else o.stride()
+    d, need = _delta_call(T, N, tuple(heads), _dtype_code(gi), gt, gn, ot, on, NSK_PASS_FWD)
+    ws = ws or Workspace(dev)
+    wp, wb = ws.get(need)
+    _check(lib().nsk_delta_fwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(h0), _rows_ptr(o), _ptr(h_last), _ptr(saved), wp, wb, _stream()),
+           "nsk_delta_fwd")
+    return o, h_last, saved
+
+
+def delta_bwd(gi, saved, heads, bias=None, do=None, dh_last=None, lengths=None, dgi=None, dh0=None, want_dh0=True, ws: Optional[Workspace] = None):
+    """Gradients of delta_fwd: (dgi, dh0).  dgi lies as gi does."""
+    H, Hk, D, Dv = _delta_width(gi, heads)
+    T, N, _ = gi.shape
+    dev, strides = gi.device, gi.stride()
+    if dgi is None:
+        dgi = torch.empty_like(gi)
+        if dgi.stride() != strides:         # (rows with room between them)
+            dgi = torch.empty_strided(gi.shape, strides, dtype=gi.dtype, device=dev)
+    else:
+        _like(dgi, gi.dtype, gi.shape), _rows_ptr(dgi, gi)
+    if dh0 is not None:
+        _floats(dh0, N, H, D, Dv)
+    elif want_dh0:
+        dh0 = torch.empty(N, H, D, Dv, dtype=torch.float32, device=dev)
+    _floats(bias, 2 * H), _floats(saved, -(-T // NSK_DELTA_CHUNK), N, H, D, Dv), _floats(dh_last, N, H, D, Dv), _like(do, gi.dtype, (T, N, H * Dv))
+    gt, gn, _ = strides
+    ot, on, _ = (0, 0, 1) if do is None else do.stride()
+    d, need = _delta_call(T, N, tuple(heads), _dtype_code(gi), gt, gn, ot, on, NSK_PASS_DGRAD)
+    ws = ws or Workspace(dev)
+    wp, wb = ws.get(need)
+    _check(lib().nsk_delta_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(do), _ptr(dh_last), dgi.data_ptr(), _ptr(dh0),
+                               wp, wb, _stream()), "nsk_delta_bwd")
+    return dgi, dh0
+
+
+def delta_step(gi, state, heads, bias=None, slots=None, o=None, want_o=True):
+    """One token for each of N sequences: gi [N,2*Hk*D + H*Dv + 2*H]; state float [S,H,D,Dv], updated in place; slots: int32 [N] entries of state, or
+    None for the first N.  Returns o [N,H*Dv]."""
+    H, Hk, D, Dv = _delta_width(gi, heads)
+    N, S = gi.shape[0], state.shape[0]
+    _floats(state, S, H, D, Dv), _floats(bias, 2 * H)
+    if o is not None:
+        _like(o, gi.dtype, (N, H * Dv)), _ptr(o)
+    elif want_o:
+        o = torch.empty(N, H * Dv, dtype=gi.dtype, device=gi.device)
+    _check(lib().nsk_delta_step(_dtype_code(gi), N, H, Hk, D, Dv, S, _ptr(gi), _ptr(bias), _lengths_ptr(slots, N), _ptr(state), o.data_ptr() if o is not None else None, _stream()),
+           "nsk_delta_step")
+    return o
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _distill_call(N, K, M, dtype, ld, tau):
+    ref = ctypes.byref(nsk_distill_desc_t(N, K, M, dtype, ld, tau))
+    return ref, lib().nsk_distill_workspace_bytes(ref)
+
+
+def _logits_ptr(t, like=None):
+    """Pointer of [N,K] logits whose rows are contiguous and do not overlap; `like`: one whose rows lie as its own have to."""
+    (N, K), (ld, one) = t.shape, t.stride()
+    if not t.is_cuda or (one != 1 and K > 1) or (N > 1 and ld < K):
+        raise ValueError("rows of logits have to be contiguous, on the GPU, and must not overlap")
+    if like is not None and N > 1 and ld != like.stride(0):
+        raise ValueError("rows of a gradient have to lie as those of its logits")
+    return t.data_ptr()
+
+
+def _distill_args(logits, top_index, top_logits, tau, weights):
+    N, K = logits.shape
+    M = top_index.shape[-1]
+    _floats(top_logits, N, M), _floats(weights, N)
+    d, need = _distill_call(N, K, M, _dtype_code(logits), logits.stride(0) if N > 1 else 0, float(tau))
+    return need, (d, _logits_ptr(logits), _ints(top_index, N, M), _ptr(top_logits), _ptr(weights))
+
+
+def distill_fwd(logits, top_index, top_logits, tau=1.0, weights=None, per_row=None, loss=None, saved=None, ws: Optional[Workspace] = None):
+    """The loss of logits [N,K] (rows may have room between them) against a teacher's largest: top_index int32 [N,M] (negative: no place), top_logits float
+    [N,M]; weights: float [N] or None.  Returns (loss [1], per_row [N], saved [N+1,2]), float; saved is what distill_bwd reads."""
+    N, dev = logits.shape[0], logits.device
+    need, args = _distill_args(logits, top_index, top_logits, tau, weights)
+    _floats(per_row, N), _floats(loss, 1), _floats(saved, N + 1, 2)
+    if per_row is None:
+        per_row = torch.empty(N, dtype=torch.float32, device=dev)
+    if loss is None:
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+    if saved is None:
+        saved = torch.empty(N + 1, 2, dtype=torch.float32, device=dev)
+    wp, wb = (ws or Workspace(dev)).get(need)
+    _check(lib().nsk_distill_fwd(*args, _ptr(per_row), _ptr(loss), _ptr(saved), wp, wb, _stream()), "nsk_distill_fwd")
+    return loss, per_row, saved
+
+
+def distill_bwd(logits, top_index, top_logits, saved, tau=1.0, dloss=1.0, weights=None, out=None, accumulate=False):
+    """Gradient of the logits, whose rows lie as theirs; out may be logits itself unless it is added to."""
+    _, args = _distill_args(logits, top_index, top_logits, tau, weights)
+    _floats(saved, logits.shape[0] + 1, 2)
+    if out is None:
+        assert not accumulate
+        out = torch.empty_like(logits)
+        if out.stride() != logits.stride():
+            out = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=logits.device)
+    else:
+        _like(out, logits.dtype, logits.shape)
+    _check(lib().nsk_distill_bwd(*args, _ptr(saved), float(dloss), _logits_ptr(out, logits), int(bool(accumulate)), _stream()), "nsk_distill_bwd")
+    return out
 
 
 # ------------------------------------------------------------------------------------ memory pool

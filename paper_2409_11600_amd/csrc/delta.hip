@@ -1,0 +1,979 @@
+// Gated delta rule: for every sequence and head a state S [D,Dv], with k^ and q^ the normalised key and query, alpha = sigmoid(a + bias), beta = sigmoid(b + bias),
+//   S' = alpha S_{t-1},  S_t = S' + k^ (beta (v - S'^T k^))^T,  o_t = S_t^T q^.
+// Steps go in chunks of 64.  With c_i the sum of log alpha up to step i of the chunk, C the whole chunk's, S the state that enters it and (K, Q, V) its rows:
+//   A_ij = beta_i exp(c_i - c_j) k_i.k_j (j < i),  P_ij = exp(c_i - c_j) q_i.k_j (j <= i),
+//   (1 + A) U = beta (V - exp(c) K S),  O = exp(c) Q S + P U,  S <- exp(C) S + (exp(C - c) K)^T U.
+// Backwards, with G the gradient of the state that leaves the chunk and R = V - exp(c) K S:
+//   dU = P^T dO + exp(C - c) K G,  (1 + A)^T X = dU,  G <- exp(C) G + (exp(c) Q)^T dO - (beta exp(c) K)^T X,
+//   dV = beta X,  dA = -X U^T,  dP = dO U^T  (where A and P are not zero),  and with E1 = X S^T, E2 = dO S^T, E3 = U G^T:
+//   dQ = exp(c) E2 + (dP L) K,  dK = -beta exp(c) E1 + exp(C - c) E3 + (dA beta L) K + (dA beta L)^T K + (dP L)^T Q,  L_ij = exp(c_i - c_j),
+//   and the gradients of c, of beta and of the lengths of q and k from the row and column sums of the same products.
+// All products are on the fp32 matrix unit: states, gates' gradients and the results of a chunk of 64 dependent steps keep 32 bits.
+//
+// Where a product's result is the next one's right operand (S, U, X, G), it stays in its registers: v_mfma_f32_16x16x4_f32 leaves lane l rows 4 (l / 16) + r, r < 4, of column l % 16,
+// and a right operand of 16 rows is read in four steps of which step s takes from lane l one value of column l % 16; which row that is is free as long as the left operand's lane takes the same:
+// row 4 (l / 16) + s.  So a wavefront takes 16 columns of the state through all products by itself; A, P, K and Q, the left operands, lie in LDS.
+#include <math.h>
+
+#include <type_traits>
+
+#include "nsk_internal.h"
+
+namespace nsk {
+namespace {
+
+bool unaligned16(const void *p) { return ((uintptr_t)p & 15) != 0; }
+
+constexpr int kC = NSK_DELTA_CHUNK;
+constexpr int kLA = kC + 4;             // a row of A or P in LDS: neighbouring rows four banks apart
+constexpr float kEps = NSK_DELTA_EPS;
+constexpr int kMostWidth = 128;
+
+struct Sizes {
+    int T, N, H, Hk, D, Dv, chunks;
+    int vec;                            // rows of q and k are whole vectors of 16 bytes
+    long long gi_t, gi_n, o_t, o_n;
+};
+__device__ __forceinline__ int q_at(const Sizes &z, int hk) { return hk * z.D; }
+__device__ __forceinline__ int k_at(const Sizes &z, int hk) { return (z.Hk + hk) * z.D; }
+__device__ __forceinline__ int v_at(const Sizes &z, int h) { return 2 * z.Hk * z.D + h * z.Dv; }
+__device__ __forceinline__ int a_at(const Sizes &z, int h) { return 2 * z.Hk * z.D + z.H * z.Dv + h; }
+__device__ __forceinline__ int b_at(const Sizes &z, int h) { return a_at(z, h) + z.H; }
+__device__ __forceinline__ int steps_of(const Sizes &z, const int *lengths, int n)
+{
+    const int l = lengths ? lengths[n] : z.T;
+    return l < 0 ? 0 : l < z.T ? l : z.T;
+}
+__device__ __forceinline__ size_t state_at(const Sizes &z, int chunk, int n, int h) { return (((size_t)chunk * z.N + n) * z.H + h) * z.D * z.Dv; }
+
+__device__ __forceinline__ float sigmoid(float a)
+{
+    const float e = expf(-fabsf(a));
+    return (a >= 0.f ? 1.f : e) / (1.f + e);
+}
+
+// ----------------------------------------------------------------------------- products
+__device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+// A left operand's rows row0..row0+15, columns k0..k0+15 of m, or of m transposed; also a right operand's columns and rows, of m transposed or of m.
+__device__ __forceinline__ f32x4 frag(const float *m, int ld, int row0, int k0)
+{
+    const int l = threadIdx.x & 63;
+    return *(const f32x4 *)(m + (row0 + (l & 15)) * ld + k0 + 4 * (l >> 4));
+}
+__device__ __forceinline__ f32x4 frag_t(const float *m, int ld, int row0, int k0)
+{
+    const int l = threadIdx.x & 63;
+    const float *p = m + (k0 + 4 * (l >> 4)) * ld + row0 + (l & 15);
+    return (f32x4){p[0], p[ld], p[2 * ld], p[3 * ld]};
+}
+__device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c)
+{
+#pragma unroll
+    for (int s = 0; s < 4; ++s) c = mfma(a[s], b[s], c);
+    return c;
+}
+// Nothing is moved across: the fragments of one row of tiles are in flight at a time, not those of a whole product, for which there are not enough registers.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ f32x4 rows_of(const float *v, int row0) { return *(const f32x4 *)(v + row0 + 4 * ((threadIdx.x >> 4) & 3)); }
+// Sums over the 16 columns of a tile; all lanes have them.
+__device__ __forceinline__ f32x4 sum_columns(f32x4 v)
+{
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += __shfl_xor(v[r], o, 64);
+    return v;
+}
+
+// ----------------------------------------------------------------------------- what a chunk starts with
+struct alignas(16) Gates {
+    double c[kC];               // sums of log alpha: differences of far ones keep what matters
+    float beta[kC], in[kC], out[kC];        // beta, exp(c), exp(C - c)
+    float rest_a[kC], rest_b[kC];           // 1 - alpha, 1 - beta
+    float all;                  // exp(C)
+};
+// By one wavefront.  Steps from `live` on leave the state as it is.
+template <typename T> __device__ void load_gates(const Sizes &z, const T *row, const float *bias, int h, int live, Gates &g)
+{
+    const int i = threadIdx.x & 63;
+    double la = 0.;
+    float beta = 0.f, rest_a = 0.f, rest_b = 0.f;
+    if (i < live) {
+        const T *p = row + i * z.gi_t;
+        const float a = (float)p[a_at(z, h)] + (bias ? bias[h] : 0.f), b = (float)p[b_at(z, h)] + (bias ? bias[z.H + h] : 0.f);
+        // log sigmoid(a); below -1000 alpha is 0 in any type, and a sum of infinities would have no differences
+        la = a < -1000.f ? -1000. : (a < 0.f ? (double)a : 0.) - log1p(exp(-fabs((double)a)));
+        beta = sigmoid(b);
+        rest_a = sigmoid(-a);
+        rest_b = sigmoid(-b);
+    }
+    double c = la;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double up = __shfl_up(c, o, 64);
+        if (i >= o) c += up;
+    }
+    const double C = __shfl(c, 63, 64);
+    g.c[i] = c;
+    g.beta[i] = beta;
+    g.in[i] = expf((float)c);
+    g.out[i] = expf((float)(C - c));
+    g.rest_a[i] = rest_a;
+    g.rest_b[i] = rest_b;
+    if (i == 0) g.all = expf((float)C);
+}
+
+// A row of q or k: kThreads / 64 neighbouring lanes take vectors of 16 bytes in turn.
+template <typename T, int DP, int THREADS> struct RowPart {
+    static constexpr int LANES = THREADS / 64, V = 16 / sizeof(T), VECTORS = DP / V, EACH = (VECTORS + LANES - 1) / LANES;
+    struct alignas(16) Vec {
+        T v[V];
+    };
+    Vec x[EACH];
+    __device__ __forceinline__ void load(const T *row, int D, bool live, bool vec)
+    {
+        const int p = threadIdx.x % LANES;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            x[i] = {};
+            const int e0 = (p + i * LANES) * V;
+            if (!live || e0 >= D) continue;
+            if (vec) x[i] = *(const Vec *)(row + e0);
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (e0 + e < D) x[i].v[e] = row[e0 + e];
+        }
+    }
+    // 1 / sqrt(|row|^2 + eps)
+    __device__ __forceinline__ float inverse_length() const
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s += (float)x[i].v[e] * (float)x[i].v[e];
+#pragma unroll
+        for (int o = 1; o < LANES; o <<= 1) s += __shfl_xor(s, o, 64);
+        return 1.f / sqrtf(s + kEps);
+    }
+    __device__ __forceinline__ void store(float *row, float by) const
+    {
+        const int p = threadIdx.x % LANES;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int v = p + i * LANES;
+            if (v >= VECTORS) continue;
+#pragma unroll
+            for (int e = 0; e < V; e += 4)
+                *(f32x4 *)(row + v * V + e) = (f32x4){(float)x[i].v[e] * by, (float)x[i].v[e + 1] * by, (float)x[i].v[e + 2] * by, (float)x[i].v[e + 3] * by};
+        }
+    }
+};
+// Normalised keys and queries of a chunk into LDS, [64][DP + 4]; lengths: NULL, or where 1 / |k| and 1 / |q| go.
+template <typename T, int DP, int THREADS>
+__device__ __forceinline__ void load_keys(const Sizes &z, const T *row0, int hk, int live, float *K, float *Q, float *inv_k, float *inv_q)
+{
+    typedef RowPart<T, DP, THREADS> Part;
+    const int r = threadIdx.x / Part::LANES;
+    const T *row = row0 + r * z.gi_t;
+    Part k, q;
+    k.load(row + k_at(z, hk), z.D, r < live, z.vec);
+    q.load(row + q_at(z, hk), z.D, r < live, z.vec);
+    const float ik = k.inverse_length(), iq = q.inverse_length();
+    k.store(K + r * (DP + 4), ik);
+    q.store(Q + r * (DP + 4), iq / sqrtf((float)z.D));
+    if (inv_k && threadIdx.x % Part::LANES == 0) {
+        inv_k[r] = ik;
+        inv_q[r] = iq;
+    }
+}
+
+// The tiles of 16 x 16 of A and P that are not zero: 10 each.
+constexpr int kTiles = 10;
+__device__ __forceinline__ void tile_at(int t, int &bi, int &bj)
+{
+    bi = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3;
+    bj = t - bi * (bi + 1) / 2;
+}
+// exp(c_i - c_j) for this lane's elements of a tile; 0 where j > i, or j = i in a strict one.
+__device__ __forceinline__ f32x4 decays(const Gates &g, int bi, int bj, bool strict)
+{
+    const int l = threadIdx.x & 63, i0 = 16 * bi + 4 * (l >> 4), j = 16 * bj + (l & 15);
+    f32x4 d;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) d[r] = i0 + r > j || (!strict && i0 + r == j) ? expf((float)(g.c[i0 + r] - g.c[j])) : 0.f;
+    return d;
+}
+template <int DP> __device__ __forceinline__ f32x4 dot_tile(const float *X, const float *K, int bi, int bj)
+{
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k0 = 0; k0 < DP; k0 += 16) acc = multiply(frag(X, DP + 4, 16 * bi, k0), frag(K, DP + 4, 16 * bj, k0), acc);
+    return acc;
+}
+__device__ __forceinline__ void store_tile(float *m, int bi, int bj, f32x4 v)
+{
+    const int l = threadIdx.x & 63;
+    float *p = m + (16 * bi + 4 * (l >> 4)) * kLA + 16 * bj + (l & 15);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r * kLA] = v[r];
+}
+// -A and P by all wavefronts: tile t of 20, the first ten of A.  Returns the tile without beta (A) or as it is (P).
+template <int DP> __device__ __forceinline__ f32x4 make_tile(int t, const Gates &g, const float *K, const float *Q, float *A, float *P)
+{
+    int bi, bj;
+    tile_at(t < kTiles ? t : t - kTiles, bi, bj);
+    const f32x4 d = decays(g, bi, bj, t < kTiles), x = d * dot_tile<DP>(t < kTiles ? K : Q, K, bi, bj);
+    if (t < kTiles) store_tile(A, bi, bj, -rows_of(g.beta, 16 * bi) * x);
+    else store_tile(P, bi, bj, x);
+    return x;
+}
+// The inverse of a diagonal block of 1 + A, in its place: wavefront w takes block w, each lane a column (the four groups of 16 lanes the same).
+__device__ __forceinline__ void invert_block(float *A, int w)
+{
+    const int c = threadIdx.x & 15;
+    float *m = A + 16 * w * kLA + 16 * w;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float s = i == c ? 1.f : 0.f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) s = fmaf(m[i * kLA + j], x[j], s);
+        x[i] = s;
+    }
+    if ((threadIdx.x & 63) < 16)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m[i * kLA + c] = x[i];
+}
+// (1 + A) U = X, and (1 + A)^T U = X, in place for 16 columns.
+__device__ __forceinline__ void solve(const float *A, f32x4 (&X)[4])
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+#pragma unroll
+        for (int j = 0; j < b; ++j) X[b] = multiply(frag(A, kLA, 16 * b, 16 * j), X[j], X[b]);
+        X[b] = multiply(frag(A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
+    }
+}
+__device__ __forceinline__ void solve_t(const float *A, f32x4 (&X)[4])
+{
+#pragma unroll
+    for (int b = 3; b >= 0; --b) {
+#pragma unroll
+        for (int j = 3; j > b; --j) X[b] = multiply(frag_t(A, kLA, 16 * b, 16 * j), X[j], X[b]);
+        X[b] = multiply(frag_t(A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
+    }
+}
+
+// 16 columns of a state [D,Dv] in registers.
+template <int DT> __device__ __forceinline__ void load_state(const Sizes &z, const float *s, int col, f32x4 (&S)[DT])
+{
+    const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int k = 0; k < DT; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * k + 4 * g + r;
+            S[k][r] = s && d < z.D && col < z.Dv ? s[(size_t)d * z.Dv + col] : 0.f;
+        }
+}
+template <int DT> __device__ __forceinline__ void store_state(const Sizes &z, float *s, int col, const f32x4 (&S)[DT])
+{
+    const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int k = 0; k < DT; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * k + 4 * g + r;
+            if (d < z.D && col < z.Dv) s[(size_t)d * z.Dv + col] = S[k][r];
+        }
+}
+// 16 columns of the chunk's rows of v, o or their gradients; rows from `live` on are not read, and written as zeros.
+template <typename T> __device__ __forceinline__ void load_rows(const T *p, long long stride, int live, bool there, f32x4 (&X)[4])
+{
+    const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * b + 4 * g + r;
+            X[b][r] = there && i < live ? (float)p[i * stride] : 0.f;
+        }
+}
+template <typename T> __device__ __forceinline__ void store_rows(T *p, long long stride, int live, int rows, bool there, const f32x4 (&X)[4])
+{
+    const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * b + 4 * g + r;
+            if (there && i < rows) p[i * stride] = (T)(i < live ? X[b][r] : 0.f);
+        }
+}
+
+template <int DT> struct Shared {
+    static constexpr int DP = 16 * DT, LD = DP + 4;
+    float K[kC * LD], Q[kC * LD], A[kC * kLA], P[kC * kLA];
+    Gates g;
+};
+
+// ----------------------------------------------------------------------------- all steps
+// A block takes the columns of a state that its wavefronts hold, 16 each, through all chunks.
+template <typename T, int DT, int NW>
+__global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
+                                                            T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
+{
+    typedef Shared<DT> Lds;
+    constexpr int DP = Lds::DP, LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = (blockIdx.y * NW + wave) * 16 + (threadIdx.x & 15);
+    const bool there = col < z.Dv;
+    const int len = steps_of(z, lengths, n);
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 S[DT];
+    load_state(z, h0 ? h0 + own : nullptr, col, S);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < z.chunks; ++c) {
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
+        if (saved) store_state(z, saved + state_at(z, c, n, h), col, S);
+        T *out = o ? o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr;
+        f32x4 X[4] = {zero, zero, zero, zero};
+        if (live <= 0) {
+            if (o) store_rows(out, z.o_t, 0, rows, there, X);
+            continue;
+        }
+        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+        __syncthreads();
+        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+        if (wave == 0) load_gates(z, row0, bias, h, live, s.g);
+        __syncthreads();
+        load_rows(row0 + v_at(z, h) + col, z.gi_t, live, there, X);
+        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(t, s.g, s.K, s.Q, s.A, s.P);
+        __syncthreads();
+        if (wave < 4) invert_block(s.A, wave);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            f32x4 acc = zero;
+#pragma unroll
+            for (int k = 0; k < DT; ++k) acc = multiply(frag(s.K, LD, 16 * b, 16 * k), S[k], acc);
+            X[b] = rows_of(s.g.beta, 16 * b) * (X[b] - rows_of(s.g.in, 16 * b) * acc);
+        }
+        __syncthreads();
+        solve(s.A, X);
+        if (o) {
+            f32x4 O[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                O[b] = zero;
+#pragma unroll
+                for (int k = 0; k < DT; ++k) O[b] = multiply(frag(s.Q, LD, 16 * b, 16 * k), S[k], O[b]);
+                O[b] *= rows_of(s.g.in, 16 * b);
+#pragma unroll
+                for (int j = 0; j <= b; ++j) O[b] = multiply(frag(s.P, kLA, 16 * b, 16 * j), X[j], O[b]);
+            }
+            store_rows(out, z.o_t, live, rows, there, O);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) X[b] *= rows_of(s.g.out, 16 * b);
+        const float all = s.g.all;
+#pragma unroll
+        for (int k = 0; k < DT; ++k) {
+            S[k] *= all;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) S[k] = multiply(frag_t(s.K, LD, 16 * k, 16 * b), X[b], S[k]);
+        }
+    }
+    if (h_last) store_state(z, h_last + own, col, S);
+}
+
+// ----------------------------------------------------------------------------- backwards
+// The gradients of the states that leave the chunks, from the last to the first, and of the initial state.
+template <typename T, int DT, int NW>
+__global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
+                                                             const float *__restrict__ dh_last, float *__restrict__ dh0, float *__restrict__ ends)
+{
+    typedef Shared<DT> Lds;
+    constexpr int DP = Lds::DP, LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = (blockIdx.y * NW + wave) * 16 + (threadIdx.x & 15);
+    const bool there = col < z.Dv;
+    const int len = steps_of(z, lengths, n);
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 G[DT];
+    load_state(z, dh_last ? dh_last + own : nullptr, col, G);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    for (int c = (len + kC - 1) / kC - 1; c >= 0; --c) {
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
+        store_state(z, ends + state_at(z, c, n, h), col, G);
+        if (c == 0 && !dh0) break;
+        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+        __syncthreads();
+        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+        if (wave == 0) load_gates(z, row0, bias, h, live, s.g);
+        __syncthreads();
+        f32x4 dO[4];
+        load_rows(d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr, z.o_t, live, there && d_o, dO);
+        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(t, s.g, s.K, s.Q, s.A, s.P);
+        __syncthreads();
+        if (wave < 4) invert_block(s.A, wave);
+        f32x4 X[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            X[b] = zero;
+#pragma unroll
+            for (int k = 0; k < DT; ++k) X[b] = multiply(frag(s.K, LD, 16 * b, 16 * k), G[k], X[b]);
+            X[b] *= rows_of(s.g.out, 16 * b);
+#pragma unroll
+            for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(s.P, kLA, 16 * b, 16 * i), dO[i], X[b]);
+        }
+        __syncthreads();
+        solve_t(s.A, X);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 in = rows_of(s.g.in, 16 * b);
+            dO[b] *= in;
+            X[b] *= -in * rows_of(s.g.beta, 16 * b);
+        }
+        const float all = s.g.all;
+#pragma unroll
+        for (int k = 0; k < DT; ++k) {
+            G[k] *= all;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                G[k] = multiply(frag_t(s.Q, LD, 16 * k, 16 * b), dO[b], G[k]);
+                G[k] = multiply(frag_t(s.K, LD, 16 * k, 16 * b), X[b], G[k]);
+            }
+        }
+    }
+    if (dh0) store_state(z, dh0 + own, col, G);
+}
+
+// Four columns of a row in memory, as an operand's fragment: row row0 + l % 16, columns k0 + 4 (l / 16) and the next.
+template <typename T> __device__ __forceinline__ f32x4 frag_of(const T *m, long long ld, int row0, int rows, int k0, int columns, bool vec)
+{
+    const int l = threadIdx.x & 63, row = row0 + (l & 15), k = k0 + 4 * (l >> 4);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (row >= rows || k >= columns) return x;
+    const T *p = m + row * ld + k;
+    struct alignas(4 * sizeof(T)) Q {
+        T q[4];
+    };
+    if (vec) {
+        const Q q = *(const Q *)p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (float)q.q[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (k + e < columns) x[e] = (float)p[e];
+    }
+    return x;
+}
+
+// The gradients of a chunk's rows, given the states in front of and the gradients behind it.  A block takes a key head and the heads that share it, one after the other, so that
+// their gradients of q and k are summed in registers.  64 columns of the state at a time: four wavefronts make U, the other four X; then all make the products that reach over
+// the columns, each a tile column of dQ and dK and its tiles of dA and dP.
+constexpr int kGradWaves = 8;
+template <int DT> struct GradShared : Shared<DT> {
+    float X[kC * kLA], U[kC * kLA];
+    float inv_k[kC], inv_q[kC];
+    float row_a[4][kC], col_a[4][kC], row_p[4][kC], col_p[4][kC];       // of the tiles, by their other index
+    float dots[DT][kC], ends[DT][kC];
+    float xr[4][kC];
+    float states[DT];
+};
+template <typename T, int DT>
+__global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, int vec_do, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
+                                                                     const float *__restrict__ saved, const T *__restrict__ d_o, const float *__restrict__ ends, T *__restrict__ dgi)
+{
+    typedef GradShared<DT> Lds;
+    constexpr int DP = Lds::DP, LD = Lds::LD, NW = kGradWaves, RT = 4 * DT / NW, KEEP = (2 * kTiles + NW - 1) / NW;
+    static_assert(RT >= 1, "tiles of dQ for every wavefront");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int c = blockIdx.x / (z.N * z.Hk), rest = blockIdx.x - c * (z.N * z.Hk), n = rest / z.Hk, hk = rest - n * z.Hk, group = z.H / z.Hk;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, g4 = 4 * (l >> 4), lc = l & 15;
+    const int len = steps_of(z, lengths, n), t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
+    const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+    T *out0 = dgi + t0 * z.gi_t + n * z.gi_n;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (live <= 0) {
+        const int widths[4] = {z.D, z.D, group * z.Dv, group}, at[4] = {q_at(z, hk), k_at(z, hk), v_at(z, hk * group), a_at(z, hk * group)};
+        for (int i = wave; i < rows; i += NW) {
+            T *p = out0 + i * z.gi_t;
+            for (int k = 0; k < 4; ++k)
+                for (int e = l; e < widths[k]; e += 64) p[at[k] + e] = (T)0.f;
+            for (int e = l; e < group; e += 64) p[b_at(z, hk * group) + e] = (T)0.f;
+        }
+        return;
+    }
+    load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, s.inv_k, s.inv_q);
+    // this wavefront's tiles of dQ and dK
+    const int dt = wave % DT, rt0 = wave / DT * RT;
+    f32x4 dQ[RT], dK[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) dQ[i] = dK[i] = zero;
+    for (int h = hk * group; h < (hk + 1) * group; ++h) {
+        if (wave == 0) load_gates(z, row0, bias, h, live, s.g);
+        __syncthreads();
+        f32x4 tile[KEEP], acc[KEEP];
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            const int t = wave + i * NW;
+            tile[i] = acc[i] = zero;
+            if (t < 2 * kTiles) tile[i] = make_tile<DP>(t, s.g, s.K, s.Q, s.A, s.P);
+        }
+        __syncthreads();
+        if (wave < 4) invert_block(s.A, wave);
+        __syncthreads();
+        const float *S0 = saved + state_at(z, c, n, h), *G0 = ends + state_at(z, c, n, h);
+        const T *do0 = d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr;
+        f32x4 E1[RT], E2[RT], E3[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) E1[i] = E2[i] = E3[i] = zero;
+        float both = 0.f;               // sum of S * G
+        for (int v0 = 0; v0 < z.Dv; v0 += 64) {
+            const int mine = 16 * (wave & 3) + lc, col = v0 + mine;
+            const bool there = col < z.Dv;
+            f32x4 R[4], X[4], S[DT];
+            if (wave < 4) {
+                load_state(z, S0, col, S);
+                load_rows(row0 + v_at(z, h) + col, z.gi_t, live, there, R);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    X[b] = zero;
+#pragma unroll
+                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(s.K, LD, 16 * b, 16 * k), S[k], X[b]);
+                    R[b] -= rows_of(s.g.in, 16 * b) * X[b];
+                    X[b] = rows_of(s.g.beta, 16 * b) * R[b];
+                }
+                solve(s.A, X);
+            } else {
+                load_state(z, G0, col, S);
+                load_rows(do0 ? do0 + col : nullptr, z.o_t, live, there && do0, R);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    X[b] = zero;
+#pragma unroll
+                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(s.K, LD, 16 * b, 16 * k), S[k], X[b]);
+                    X[b] *= rows_of(s.g.out, 16 * b);
+#pragma unroll
+                    for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(s.P, kLA, 16 * b, 16 * i), R[i], X[b]);
+                }
+                solve_t(s.A, X);
+            }
+            float *put = (wave < 4 ? s.U : s.X) + g4 * kLA + mine;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) put[(16 * b + r) * kLA] = X[b][r];
+            __syncthreads();
+            if (wave < 4) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    f32x4 x;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = s.X[(16 * b + g4 + r) * kLA + mine] * R[b][r];
+                    x = sum_columns(x);
+                    if (lc == 0) {
+                        f32x4 *p = (f32x4 *)&s.xr[wave][16 * b + g4];
+                        *p = v0 ? *p + x : x;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) X[b] *= rows_of(s.g.beta, 16 * b);
+                store_rows(out0 + v_at(z, h) + col, z.gi_t, live, rows, there, X);
+            }
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) {
+                const int t = wave + i * NW;
+                int bi, bj;
+                if (t >= 2 * kTiles) break;
+                tile_at(t < kTiles ? t : t - kTiles, bi, bj);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const f32x4 a = t < kTiles ? frag(s.X, kLA, 16 * bi, 16 * k) : do0 ? frag_of(do0, z.o_t, 16 * bi, live, v0 + 16 * k, z.Dv, vec_do) : zero;
+                    acc[i] = multiply(a, frag(s.U, kLA, 16 * bj, 16 * k), acc[i]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool vec = z.Dv % 4 == 0;
+                const f32x4 sf = frag_of(S0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec), gf = frag_of(G0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec);
+                if (rt0 == 0) both += (sf[0] * gf[0] + sf[1] * gf[1]) + (sf[2] * gf[2] + sf[3] * gf[3]);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const int b = rt0 + i;
+                    E1[i] = multiply(frag(s.X, kLA, 16 * b, 16 * k), sf, E1[i]);
+                    if (do0) E2[i] = multiply(frag_of(do0, z.o_t, 16 * b, live, v0 + 16 * k, z.Dv, vec_do), sf, E2[i]);
+                    E3[i] = multiply(frag(s.U, kLA, 16 * b, 16 * k), gf, E3[i]);
+                }
+            }
+            __syncthreads();
+        }
+        // dA and dP, times L, in the place of A and P; the sums of dA A and dP P over rows and columns
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            const int t = wave + i * NW;
+            int bi, bj;
+            if (t >= 2 * kTiles) break;
+            const bool is_a = t < kTiles;
+            tile_at(is_a ? t : t - kTiles, bi, bj);
+            const f32x4 beta = rows_of(s.g.beta, 16 * bi), d = is_a ? -acc[i] : acc[i], L = decays(s.g, bi, bj, is_a);
+            const f32x4 by_row = d * tile[i], by_col = is_a ? beta * by_row : by_row;
+            float sum = (by_col[0] + by_col[1]) + (by_col[2] + by_col[3]);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (l < 16) (is_a ? s.col_a : s.col_p)[bi][16 * bj + l] = sum;
+            const f32x4 row = sum_columns(by_row);
+            if (lc == 0) *(f32x4 *)&(is_a ? s.row_a : s.row_p)[bj][16 * bi + g4] = row;
+            store_tile(is_a ? s.A : s.P, bi, bj, is_a ? beta * d * L : d * L);
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int b = rt0 + i;
+            const f32x4 in = rows_of(s.g.in, 16 * b), k1 = -in * rows_of(s.g.beta, 16 * b) * E1[i], q1 = in * E2[i], e = rows_of(s.g.out, 16 * b) * E3[i];
+            f32x4 k, q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                k[r] = s.K[(16 * b + g4 + r) * LD + 16 * dt + lc];
+                q[r] = s.Q[(16 * b + g4 + r) * LD + 16 * dt + lc];
+            }
+            const f32x4 ek = sum_columns(e * k), dot = sum_columns(k1 * k + q1 * q);
+            if (lc == 0) {
+                *(f32x4 *)&s.ends[dt][16 * b + g4] = ek;
+                *(f32x4 *)&s.dots[dt][16 * b + g4] = dot;
+            }
+            dQ[i] += q1;
+            dK[i] += k1 + e;
+        }
+        if (rt0 == 0) {
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) both += __shfl_xor(both, o, 64);
+            if (l == 0) s.states[dt] = both;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int b = rt0 + i;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 k = frag_t(s.K, LD, 16 * dt, 16 * j);
+                if (j <= b) {
+                    dK[i] = multiply(frag(s.A, kLA, 16 * b, 16 * j), k, dK[i]);
+                    dQ[i] = multiply(frag(s.P, kLA, 16 * b, 16 * j), k, dQ[i]);
+                }
+                if (j >= b) {
+                    dK[i] = multiply(frag_t(s.A, kLA, 16 * b, 16 * j), k, dK[i]);
+                    dK[i] = multiply(frag_t(s.P, kLA, 16 * b, 16 * j), frag_t(s.Q, LD, 16 * dt, 16 * j), dK[i]);
+                }
+            }
+        }
+        if (wave == NW - 1) {           // the gates, a step a lane
+            const int b = l >> 4;
+            double dc = 0., e = 0., both_all = 0.;
+#pragma unroll
+            for (int k = 0; k < DT; ++k) {
+                e += (double)s.ends[k][l];
+                dc += (double)s.dots[k][l];
+                both_all += (double)s.states[k];
+            }
+            dc -= e;
+            float ra = 0.f, xr = (s.xr[0][l] + s.xr[1][l]) + (s.xr[2][l] + s.xr[3][l]);
+            double p = 0.;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k <= b) {
+                    ra += s.row_a[k][l];
+                    p += (double)s.row_p[k][l];
+                }
+                if (k >= b) p -= (double)s.col_a[k][l] + (double)s.col_p[k][l];
+            }
+            const float beta = s.g.beta[l];
+            dc += (double)beta * ra + p;
+            // of log alpha: all c from this step on, and C
+            double up = dc, end = e;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const double x = __shfl_down(up, o, 64);
+                if (l + o < 64) up += x;
+                end += __shfl_xor(end, o, 64);
+            }
+            up += end + (double)s.g.all * both_all;
+            if (l < rows) {
+                T *q = out0 + l * z.gi_t;
+                q[a_at(z, h)] = (T)(l < live ? (float)up * s.g.rest_a[l] : 0.f);
+                q[b_at(z, h)] = (T)(l < live ? (xr + ra) * beta * s.g.rest_b[l] : 0.f);
+            }
+        }
+        __syncthreads();
+    }
+    // through the lengths: k^ = k / |k|, q^ = q / (sqrt(D) |q|)
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        f32x4 k, q;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            k[r] = s.K[(16 * (rt0 + i) + g4 + r) * LD + 16 * dt + lc];
+            q[r] = s.Q[(16 * (rt0 + i) + g4 + r) * LD + 16 * dt + lc];
+        }
+        const f32x4 kk = sum_columns(dK[i] * k), qq = sum_columns(dQ[i] * q);
+        if (lc == 0) {
+            *(f32x4 *)&s.ends[dt][16 * (rt0 + i) + g4] = kk;
+            *(f32x4 *)&s.dots[dt][16 * (rt0 + i) + g4] = qq;
+        }
+    }
+    __syncthreads();
+    const float width = (float)z.D, unit = 1.f / sqrtf(width);
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * (rt0 + i) + g4 + r, d = 16 * dt + lc;
+            float kk = 0.f, qq = 0.f;
+#pragma unroll
+            for (int k = 0; k < DT; ++k) {
+                kk += s.ends[k][row];
+                qq += s.dots[k][row];
+            }
+            if (row >= rows || d >= z.D) continue;
+            T *p = out0 + row * z.gi_t;
+            p[k_at(z, hk) + d] = (T)(row < live ? s.inv_k[row] * (dK[i][r] - s.K[row * LD + d] * kk) : 0.f);
+            p[q_at(z, hk) + d] = (T)(row < live ? s.inv_q[row] * unit * (dQ[i][r] - width * s.Q[row * LD + d] * qq) : 0.f);
+        }
+}
+
+// ----------------------------------------------------------------------------- one token
+// A block a head's state, which is read once and kept in registers: a thread has four columns of every (256 / GROUPS)th row.
+constexpr int kStepThreads = 256;
+template <typename T, int GROUPS>
+__global__ __launch_bounds__(kStepThreads) void delta_step_kernel(Sizes z, int S, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ slots,
+                                                                  float *__restrict__ state, T *__restrict__ o)
+{
+    constexpr int ROWS = kStepThreads / GROUPS, EACH = kMostWidth / ROWS;
+    __shared__ float K[kMostWidth], Q[kMostWidth];
+    __shared__ f32x4 part[2][ROWS][GROUPS];
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), cg = threadIdx.x % GROUPS, rg = threadIdx.x / GROUPS, col = 4 * cg;
+    const int slot = slots ? slots[n] : n;
+    const T *row = gi + n * z.gi_n;
+    T *out = o ? o + (size_t)n * z.H * z.Dv + h * z.Dv + col : nullptr;
+    if (slot < 0 || slot >= S) {
+        if (o && rg == 0)
+            for (int e = 0; e < 4; ++e)
+                if (col + e < z.Dv) out[e] = (T)0.f;
+        return;
+    }
+    float *own = state + ((size_t)slot * z.H + h) * z.D * z.Dv + col;
+    const bool vec = z.Dv % 4 == 0;
+    f32x4 s[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int d = rg + i * ROWS;
+        s[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (d >= z.D || col >= z.Dv) continue;
+        if (vec) s[i] = *(const f32x4 *)(own + (size_t)d * z.Dv);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < z.Dv) s[i][e] = own[(size_t)d * z.Dv + e];
+    }
+    const float alpha = sigmoid((float)row[a_at(z, h)] + (bias ? bias[h] : 0.f)), beta = sigmoid((float)row[b_at(z, h)] + (bias ? bias[z.H + h] : 0.f));
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = col + e < z.Dv ? (float)row[v_at(z, h) + col + e] : 0.f;
+    if (threadIdx.x < 128) {            // the first wavefront the key, the second the query
+        const int l = threadIdx.x & 63;
+        const bool key = threadIdx.x < 64;
+        const T *p = row + (key ? k_at(z, hk) : q_at(z, hk));
+        const float x0 = l < z.D ? (float)p[l] : 0.f, x1 = l + 64 < z.D ? (float)p[l + 64] : 0.f;
+        float sum = x0 * x0 + x1 * x1;
+#pragma unroll
+        for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w, 64);
+        const float by = (key ? 1.f : 1.f / sqrtf((float)z.D)) / sqrtf(sum + kEps);
+        float *to = key ? K : Q;
+        to[l] = x0 * by;
+        to[l + 64] = x1 * by;
+    }
+    __syncthreads();
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        s[i] *= alpha;
+        sum += K[rg + i * ROWS] * s[i];
+    }
+    part[0][rg][cg] = sum;
+    __syncthreads();
+    sum = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) sum += part[0][r][cg];
+    const f32x4 u = beta * (v - sum);
+    sum = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int d = rg + i * ROWS;
+        s[i] += K[d] * u;
+        sum += Q[d] * s[i];
+        if (d >= z.D || col >= z.Dv) continue;
+        if (vec) *(f32x4 *)(own + (size_t)d * z.Dv) = s[i];
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < z.Dv) own[(size_t)d * z.Dv + e] = s[i][e];
+    }
+    if (!o) return;
+    part[1][rg][cg] = sum;
+    __syncthreads();
+    if (rg) return;
+    sum = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) sum += part[1][r][cg];
+    for (int e = 0; e < 4; ++e)
+        if (col + e < z.Dv) out[e] = (T)sum[e];
+}
+
+// ----------------------------------------------------------------------------- host
+// Rows of `width` elements at t * st + n * sn that do not overlap, and do not lie between each other's; both strides 0: [T,N,width].
+bool rows_apart(int T, int N, long long width, long long &st, long long &sn)
+{
+    if (st == 0 && sn == 0) {
+        sn = width;
+        st = width * N;
+    }
+    const long long most = 1LL << 60;
+    if ((T > 1 && (st < width || st > most / T)) || (N > 1 && (sn < width || sn > most / N))) return false;
+    return T == 1 || N == 1 || st >= sn * (N - 1) + width || sn >= st * (T - 1) + width;
+}
+bool heads_ok(int H, int Hk, int D, int Dv) { return H > 0 && Hk > 0 && D > 0 && Dv > 0 && H <= 1 << 20 && D <= 1 << 20 && Dv <= 1 << 20 && H % Hk == 0; }
+long long width_of(int H, int Hk, int D, int Dv) { return 2LL * Hk * D + (long long)H * Dv + 2LL * H; }
+int check(const nsk_delta_desc_t *desc, Sizes &z)
+{
+    if (!desc) return NSK_ERR_NULL;
+    nsk_delta_desc_t d = *desc;
+    if (d.T <= 0 || d.N <= 0 || !heads_ok(d.H, d.Hk, d.D, d.Dv) || (d.dtype != NSK_F32 && d.dtype != NSK_BF16)) return NSK_ERR_BAD_DESC;
+    const long long width = width_of(d.H, d.Hk, d.D, d.Dv);
+    if (width > 1 << 30 || (long long)d.N * width > (1LL << 60) / d.T) return NSK_ERR_BAD_DESC;
+    if (!rows_apart(d.T, d.N, width, d.gi_t, d.gi_n) || !rows_apart(d.T, d.N, (long long)d.H * d.Dv, d.o_t, d.o_n)) return NSK_ERR_BAD_DESC;
+    // (a launch has fewer than 2^32 threads)
+    const long long chunks = ((long long)d.T + kC - 1) / kC;
+    if (d.D > kMostWidth || d.Dv > kMostWidth || d.T > 1 << 30 || (long long)d.N * d.H >= 1LL << 22 || chunks * d.N * d.Hk >= 1LL << 23) return NSK_ERR_UNSUPPORTED;
+    const int whole = d.dtype == NSK_BF16 ? 8 : 4;
+    const bool vec = d.D % whole == 0 && (d.T == 1 || d.gi_t % whole == 0) && (d.N == 1 || d.gi_n % whole == 0);
+    z = {d.T, d.N, d.H, d.Hk, d.D, d.Dv, (int)chunks, vec, d.T == 1 ? 0 : d.gi_t, d.N == 1 ? 0 : d.gi_n, d.T == 1 ? 0 : d.o_t, d.N == 1 ? 0 : d.o_n};
+    return NSK_OK;
+}
+size_t saved_of(const Sizes &z) { return (size_t)z.chunks * z.N * z.H * z.D * z.Dv * sizeof(float); }
+
+// A call with the tiles of D and the wavefronts' columns as constants.
+template <typename F> int with_sizes(const Sizes &z, F &&f)
+{
+    auto columns = [&](auto dt) { return z.Dv <= 64 ? f(dt, std::integral_constant<int, 4>{}) : f(dt, std::integral_constant<int, 8>{}); };
+    if (z.D <= 32) return columns(std::integral_constant<int, 2>{});
+    if (z.D <= 64) return columns(std::integral_constant<int, 4>{});
+    return columns(std::integral_constant<int, 8>{});
+}
+
+}  // namespace
+}  // namespace nsk
+
+using namespace nsk;
+
+extern "C" {
+
+size_t nsk_delta_saved_bytes(const nsk_delta_desc_t *desc)
+{
+    Sizes z;
+    return check(desc, z) == NSK_OK ? saved_of(z) : 0;
+}
+
+size_t nsk_delta_workspace_bytes(const nsk_delta_desc_t *desc, int pass)
+{
+    Sizes z;
+    return pass == NSK_PASS_DGRAD && check(desc, z) == NSK_OK ? saved_of(z) : 0;
+}
+
+int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0, void *o, float *h_last, float *saved, void *workspace,
+                  size_t workspace_bytes, void *stream)
+{
+    Sizes z;
+    const int status = check(desc, z);
+    if (status != NSK_OK) return status;
+    if (!gi || (!o && !h_last)) return NSK_ERR_NULL;
+    if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(h0) || unaligned16(o) || unaligned16(h_last) || unaligned16(saved) || unaligned16(workspace))
+        return NSK_ERR_ALIGNMENT;
+    (void)workspace_bytes;
+    hipStream_t st = (hipStream_t)stream;
+    auto launch = [&](auto one) {
+        typedef decltype(one) T;
+        return with_sizes(z, [&](auto dt, auto nw) {
+            constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
+            const size_t bytes = sizeof(Shared<DT>);
+            const int allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
+            if (allowed != NSK_OK) return allowed;
+            hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0, (T *)o,
+                               h_last, saved);
+            return check_launch();
+        });
+    };
+    return desc->dtype == NSK_BF16 ? launch(bf16_t{}) : launch(float{});
+}
+
+int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *saved, const void *d_o, const float *dh_last, void *dgi, float *dh0,
+                  void *workspace, size_t workspace_bytes, void *stream)
+{
+    Sizes z;
+    const int status = check(desc, z);
+    if (status != NSK_OK) return status;
+    if (!gi || !saved || (!d_o && !dh_last) || !dgi) return NSK_ERR_NULL;
+    if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(saved) || unaligned16(d_o) || unaligned16(dh_last) || unaligned16(dgi) || unaligned16(dh0) ||
+        unaligned16(workspace))
+        return NSK_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < saved_of(z)) return NSK_ERR_WORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    float *ends = (float *)workspace;
+    const int vec_do = z.Dv % 4 == 0 && z.o_t % 4 == 0 && z.o_n % 4 == 0;
+    auto launch = [&](auto one) {
+        typedef decltype(one) T;
+        return with_sizes(z, [&](auto dt, auto nw) {
+            constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
+            const size_t bytes = sizeof(Shared<DT>), grad_bytes = sizeof(GradShared<DT>);
+            static_assert(sizeof(GradShared<DT>) <= 160 * 1024, "what a compute unit has");
+            int allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
+            if (allowed == NSK_OK) allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);
+            if (allowed != NSK_OK) return allowed;
+            hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,
+                               (const T *)d_o, dh_last, dh0, ends);
+            hipLaunchKernelGGL((delta_grad_kernel<T, DT>), dim3((unsigned)(z.chunks * z.N * z.Hk)), dim3(kGradWaves * 64), grad_bytes, st, z, vec_do, (const T *)gi, bias, lengths, saved,
+                               (const T *)d_o, ends, (T *)dgi);
+            return check_launch();
+        });
+    };
+    return desc->dtype == NSK_BF16 ? launch(bf16_t{}) : launch(float{});
+}
+
+int nsk_delta_step(int dtype, int N, int H, int Hk, int D, int Dv, int S, const void *gi, const float *bias, const int *slots, float *state, void *o, void *stream)
+{
+    if (N <= 0 || S <= 0 || !heads_ok(H, Hk, D, Dv) || width_of(H, Hk, D, Dv) > 1 << 30 || (dtype != NSK_F32 && dtype != NSK_BF16)) return NSK_ERR_BAD_DESC;
+    if (!gi || !state) return NSK_ERR_NULL;
+    if (unaligned16(gi) || unaligned16(bias) || unaligned16(slots) || unaligned16(state) || unaligned16(o)) return NSK_ERR_ALIGNMENT;
+    if (D > kMostWidth || Dv > kMostWidth || (long long)N * H >= 1LL << 24) return NSK_ERR_UNSUPPORTED;     // (2^32 threads)
+    const Sizes z{1, N, H, Hk, D, Dv, 1, 0, 0, width_of(H, Hk, D, Dv), 0, 0};
+    auto launch = [&](auto one) {
+        typedef decltype(one) T;
+        if (Dv <= 64)
+            hipLaunchKernelGGL((delta_step_kernel<T, 16>), dim3((unsigned)(N * H)), dim3(kStepThreads), 0, (hipStream_t)stream, z, S, (const T *)gi, bias, slots, state, (T *)o);
+        else
+            hipLaunchKernelGGL((delta_step_kernel<T, 32>), dim3((unsigned)(N * H)), dim3(kStepThreads), 0, (hipStream_t)stream, z, S, (const T *)gi, bias, slots, state, (T *)o);
+    };
+    if (dtype == NSK_BF16) launch(bf16_t{});
+    else launch(float{});
+    return check_launch();
+}
+
+}  // extern "C"
