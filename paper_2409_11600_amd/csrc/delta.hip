@@ -53,16 +53,21 @@ __device__ __forceinline__ float sigmoid(float a)
 }
 
 // ----------------------------------------------------------------------------- products
+// This thread's lane, as a number that is made anew: what is computed from it is not kept in registers from one round of a loop to the next (LDS addresses alone would fill them).
+__device__ __forceinline__ int fresh_lane()
+{
+    int l = threadIdx.x & 63;
+    asm volatile("" : "+v"(l));
+    return l;
+}
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 // A left operand's rows row0..row0+15, columns k0..k0+15 of m, or of m transposed; also a right operand's columns and rows, of m transposed or of m.
-__device__ __forceinline__ f32x4 frag(const float *m, int ld, int row0, int k0)
+__device__ __forceinline__ f32x4 frag(int l, const float *m, int ld, int row0, int k0)
 {
-    const int l = threadIdx.x & 63;
     return *(const f32x4 *)(m + (row0 + (l & 15)) * ld + k0 + 4 * (l >> 4));
 }
-__device__ __forceinline__ f32x4 frag_t(const float *m, int ld, int row0, int k0)
+__device__ __forceinline__ f32x4 frag_t(int l, const float *m, int ld, int row0, int k0)
 {
-    const int l = threadIdx.x & 63;
     const float *p = m + (k0 + 4 * (l >> 4)) * ld + row0 + (l & 15);
     return (f32x4){p[0], p[ld], p[2 * ld], p[3 * ld]};
 }
@@ -74,7 +79,7 @@ __device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c)
 }
 // Nothing is moved across: the fragments of one row of tiles are in flight at a time, not those of a whole product, for which there are not enough registers.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
-__device__ __forceinline__ f32x4 rows_of(const float *v, int row0) { return *(const f32x4 *)(v + row0 + 4 * ((threadIdx.x >> 4) & 3)); }
+__device__ __forceinline__ f32x4 rows_of(int l, const float *v, int row0) { return *(const f32x4 *)(v + row0 + 4 * (l >> 4)); }
 // Sums over the 16 columns of a tile; all lanes have them.
 __device__ __forceinline__ f32x4 sum_columns(f32x4 v)
 {
@@ -93,16 +98,16 @@ struct alignas(16) Gates {
     float all;                  // exp(C)
 };
 // By one wavefront.  Steps from `live` on leave the state as it is.
-template <typename T> __device__ void load_gates(const Sizes &z, const T *row, const float *bias, int h, int live, Gates &g)
+template <typename T> __device__ void load_gates(int i, const Sizes &z, const T *row, const float *bias, int h, int live, Gates &g)
 {
-    const int i = threadIdx.x & 63;
     double la = 0.;
     float beta = 0.f, rest_a = 0.f, rest_b = 0.f;
     if (i < live) {
         const T *p = row + i * z.gi_t;
         const float a = (float)p[a_at(z, h)] + (bias ? bias[h] : 0.f), b = (float)p[b_at(z, h)] + (bias ? bias[z.H + h] : 0.f);
-        // log sigmoid(a); below -1000 alpha is 0 in any type, and a sum of infinities would have no differences
-        la = a < -1000.f ? -1000. : (a < 0.f ? (double)a : 0.) - log1p(exp(-fabs((double)a)));
+        // log sigmoid(a); below -1000 alpha is 0 in any type, and a sum of infinities would have no differences.  Its rounding, 2^-24 of it, is the more the less the product
+        // of gates counts: x exp(-x) is at most 0.37.  (NaN stays NaN: fminf of it and 0 would be 0, but not the sum's other part.)
+        la = a < -1000.f ? -1000.f : fminf(a, 0.f) - log1pf(expf(-fabsf(a)));
         beta = sigmoid(b);
         rest_a = sigmoid(-a);
         rest_b = sigmoid(-b);
@@ -197,79 +202,80 @@ __device__ __forceinline__ void tile_at(int t, int &bi, int &bj)
     bj = t - bi * (bi + 1) / 2;
 }
 // exp(c_i - c_j) for this lane's elements of a tile; 0 where j > i, or j = i in a strict one.
-__device__ __forceinline__ f32x4 decays(const Gates &g, int bi, int bj, bool strict)
+__device__ __forceinline__ f32x4 decays(int l, const Gates &g, int bi, int bj, bool strict)
 {
-    const int l = threadIdx.x & 63, i0 = 16 * bi + 4 * (l >> 4), j = 16 * bj + (l & 15);
+    const int i0 = 16 * bi + 4 * (l >> 4), j = 16 * bj + (l & 15);
     f32x4 d;
 #pragma unroll
     for (int r = 0; r < 4; ++r) d[r] = i0 + r > j || (!strict && i0 + r == j) ? expf((float)(g.c[i0 + r] - g.c[j])) : 0.f;
     return d;
 }
-template <int DP> __device__ __forceinline__ f32x4 dot_tile(const float *X, const float *K, int bi, int bj)
+template <int DP> __device__ __forceinline__ f32x4 dot_tile(int l, const float *X, const float *K, int bi, int bj)
 {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k0 = 0; k0 < DP; k0 += 16) acc = multiply(frag(X, DP + 4, 16 * bi, k0), frag(K, DP + 4, 16 * bj, k0), acc);
+    for (int k0 = 0; k0 < DP; k0 += 16) acc = multiply(frag(l, X, DP + 4, 16 * bi, k0), frag(l, K, DP + 4, 16 * bj, k0), acc);
     return acc;
 }
-__device__ __forceinline__ void store_tile(float *m, int bi, int bj, f32x4 v)
+__device__ __forceinline__ void store_tile(int l, float *m, int bi, int bj, f32x4 v)
 {
-    const int l = threadIdx.x & 63;
     float *p = m + (16 * bi + 4 * (l >> 4)) * kLA + 16 * bj + (l & 15);
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r * kLA] = v[r];
 }
 // -A and P by all wavefronts: tile t of 20, the first ten of A.  Returns the tile without beta (A) or as it is (P).
-template <int DP> __device__ __forceinline__ f32x4 make_tile(int t, const Gates &g, const float *K, const float *Q, float *A, float *P)
+template <int DP> __device__ __forceinline__ f32x4 make_tile(int l, int t, const Gates &g, const float *K, const float *Q, float *A, float *P)
 {
     int bi, bj;
     tile_at(t < kTiles ? t : t - kTiles, bi, bj);
-    const f32x4 d = decays(g, bi, bj, t < kTiles), x = d * dot_tile<DP>(t < kTiles ? K : Q, K, bi, bj);
-    if (t < kTiles) store_tile(A, bi, bj, -rows_of(g.beta, 16 * bi) * x);
-    else store_tile(P, bi, bj, x);
+    const f32x4 d = decays(l, g, bi, bj, t < kTiles), x = d * dot_tile<DP>(l, t < kTiles ? K : Q, K, bi, bj);
+    if (t < kTiles) store_tile(l, A, bi, bj, -rows_of(l, g.beta, 16 * bi) * x);
+    else store_tile(l, P, bi, bj, x);
     return x;
 }
 // The inverse of a diagonal block of 1 + A, in its place: wavefront w takes block w, each lane a column (the four groups of 16 lanes the same).
-__device__ __forceinline__ void invert_block(float *A, int w)
+__device__ __forceinline__ void invert_block(int l, float *A, int w)
 {
-    const int c = threadIdx.x & 15;
+    const int c = l & 15;
     float *m = A + 16 * w * kLA + 16 * w;
     float x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float s = i == c ? 1.f : 0.f;
+    for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.f : 0.f;
+    // a value is taken out of all rows below it at once: 15 steps that wait for each other, not 120
 #pragma unroll
-        for (int j = 0; j < i; ++j) s = fmaf(m[i * kLA + j], x[j], s);
-        x[i] = s;
-    }
-    if ((threadIdx.x & 63) < 16)
+    for (int j = 0; j < 15; ++j)
+#pragma unroll
+        for (int i = j + 1; i < 16; ++i) x[i] = fmaf(m[i * kLA + j], x[j], x[i]);
+    if (l < 16)
 #pragma unroll
         for (int i = 0; i < 16; ++i) m[i * kLA + c] = x[i];
 }
 // (1 + A) U = X, and (1 + A)^T U = X, in place for 16 columns.
-__device__ __forceinline__ void solve(const float *A, f32x4 (&X)[4])
+__device__ __forceinline__ void solve(int l, const float *A, f32x4 (&X)[4])
 {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
 #pragma unroll
-        for (int j = 0; j < b; ++j) X[b] = multiply(frag(A, kLA, 16 * b, 16 * j), X[j], X[b]);
-        X[b] = multiply(frag(A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
+        for (int j = 0; j < b; ++j) X[b] = multiply(frag(l, A, kLA, 16 * b, 16 * j), X[j], X[b]);
+        X[b] = multiply(frag(l, A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
+        fence();
     }
 }
-__device__ __forceinline__ void solve_t(const float *A, f32x4 (&X)[4])
+__device__ __forceinline__ void solve_t(int l, const float *A, f32x4 (&X)[4])
 {
 #pragma unroll
     for (int b = 3; b >= 0; --b) {
 #pragma unroll
-        for (int j = 3; j > b; --j) X[b] = multiply(frag_t(A, kLA, 16 * b, 16 * j), X[j], X[b]);
-        X[b] = multiply(frag_t(A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
+        for (int j = 3; j > b; --j) X[b] = multiply(frag_t(l, A, kLA, 16 * b, 16 * j), X[j], X[b]);
+        X[b] = multiply(frag_t(l, A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
+        fence();
     }
 }
 
 // 16 columns of a state [D,Dv] in registers.
-template <int DT> __device__ __forceinline__ void load_state(const Sizes &z, const float *s, int col, f32x4 (&S)[DT])
+template <int DT> __device__ __forceinline__ void load_state(int l, const Sizes &z, const float *s, int col, f32x4 (&S)[DT])
 {
-    const int g = (threadIdx.x >> 4) & 3;
+    const int g = l >> 4;
 #pragma unroll
     for (int k = 0; k < DT; ++k)
 #pragma unroll
@@ -278,9 +284,9 @@ template <int DT> __device__ __forceinline__ void load_state(const Sizes &z, con
             S[k][r] = s && d < z.D && col < z.Dv ? s[(size_t)d * z.Dv + col] : 0.f;
         }
 }
-template <int DT> __device__ __forceinline__ void store_state(const Sizes &z, float *s, int col, const f32x4 (&S)[DT])
+template <int DT> __device__ __forceinline__ void store_state(int l, const Sizes &z, float *s, int col, const f32x4 (&S)[DT])
 {
-    const int g = (threadIdx.x >> 4) & 3;
+    const int g = l >> 4;
 #pragma unroll
     for (int k = 0; k < DT; ++k)
 #pragma unroll
@@ -290,9 +296,9 @@ template <int DT> __device__ __forceinline__ void store_state(const Sizes &z, fl
         }
 }
 // 16 columns of the chunk's rows of v, o or their gradients; rows from `live` on are not read, and written as zeros.
-template <typename T> __device__ __forceinline__ void load_rows(const T *p, long long stride, int live, bool there, f32x4 (&X)[4])
+template <typename T> __device__ __forceinline__ void load_rows(int l, const T *p, long long stride, int live, bool there, f32x4 (&X)[4])
 {
-    const int g = (threadIdx.x >> 4) & 3;
+    const int g = l >> 4;
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -301,9 +307,9 @@ template <typename T> __device__ __forceinline__ void load_rows(const T *p, long
             X[b][r] = there && i < live ? (float)p[i * stride] : 0.f;
         }
 }
-template <typename T> __device__ __forceinline__ void store_rows(T *p, long long stride, int live, int rows, bool there, const f32x4 (&X)[4])
+template <typename T> __device__ __forceinline__ void store_rows(int l, T *p, long long stride, int live, int rows, bool there, const f32x4 (&X)[4])
 {
-    const int g = (threadIdx.x >> 4) & 3;
+    const int g = l >> 4;
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -313,151 +319,10 @@ template <typename T> __device__ __forceinline__ void store_rows(T *p, long long
         }
 }
 
-template <int DT> struct Shared {
-    static constexpr int DP = 16 * DT, LD = DP + 4;
-    float K[kC * LD], Q[kC * LD], A[kC * kLA], P[kC * kLA];
-    Gates g;
-};
-
-// ----------------------------------------------------------------------------- all steps
-// A block takes the columns of a state that its wavefronts hold, 16 each, through all chunks.
-template <typename T, int DT, int NW>
-__global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
-                                                            T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
-{
-    typedef Shared<DT> Lds;
-    constexpr int DP = Lds::DP, LD = Lds::LD;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    Lds &s = *(Lds *)lds;
-    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = (blockIdx.y * NW + wave) * 16 + (threadIdx.x & 15);
-    const bool there = col < z.Dv;
-    const int len = steps_of(z, lengths, n);
-    const size_t own = state_at(z, 0, n, h);
-    f32x4 S[DT];
-    load_state(z, h0 ? h0 + own : nullptr, col, S);
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < z.chunks; ++c) {
-        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
-        if (saved) store_state(z, saved + state_at(z, c, n, h), col, S);
-        T *out = o ? o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr;
-        f32x4 X[4] = {zero, zero, zero, zero};
-        if (live <= 0) {
-            if (o) store_rows(out, z.o_t, 0, rows, there, X);
-            continue;
-        }
-        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-        __syncthreads();
-        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
-        if (wave == 0) load_gates(z, row0, bias, h, live, s.g);
-        __syncthreads();
-        load_rows(row0 + v_at(z, h) + col, z.gi_t, live, there, X);
-        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(t, s.g, s.K, s.Q, s.A, s.P);
-        __syncthreads();
-        if (wave < 4) invert_block(s.A, wave);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            f32x4 acc = zero;
-#pragma unroll
-            for (int k = 0; k < DT; ++k) acc = multiply(frag(s.K, LD, 16 * b, 16 * k), S[k], acc);
-            X[b] = rows_of(s.g.beta, 16 * b) * (X[b] - rows_of(s.g.in, 16 * b) * acc);
-        }
-        __syncthreads();
-        solve(s.A, X);
-        if (o) {
-            f32x4 O[4];
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                O[b] = zero;
-#pragma unroll
-                for (int k = 0; k < DT; ++k) O[b] = multiply(frag(s.Q, LD, 16 * b, 16 * k), S[k], O[b]);
-                O[b] *= rows_of(s.g.in, 16 * b);
-#pragma unroll
-                for (int j = 0; j <= b; ++j) O[b] = multiply(frag(s.P, kLA, 16 * b, 16 * j), X[j], O[b]);
-            }
-            store_rows(out, z.o_t, live, rows, there, O);
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) X[b] *= rows_of(s.g.out, 16 * b);
-        const float all = s.g.all;
-#pragma unroll
-        for (int k = 0; k < DT; ++k) {
-            S[k] *= all;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) S[k] = multiply(frag_t(s.K, LD, 16 * k, 16 * b), X[b], S[k]);
-        }
-    }
-    if (h_last) store_state(z, h_last + own, col, S);
-}
-
-// ----------------------------------------------------------------------------- backwards
-// The gradients of the states that leave the chunks, from the last to the first, and of the initial state.
-template <typename T, int DT, int NW>
-__global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
-                                                             const float *__restrict__ dh_last, float *__restrict__ dh0, float *__restrict__ ends)
-{
-    typedef Shared<DT> Lds;
-    constexpr int DP = Lds::DP, LD = Lds::LD;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    Lds &s = *(Lds *)lds;
-    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = (blockIdx.y * NW + wave) * 16 + (threadIdx.x & 15);
-    const bool there = col < z.Dv;
-    const int len = steps_of(z, lengths, n);
-    const size_t own = state_at(z, 0, n, h);
-    f32x4 G[DT];
-    load_state(z, dh_last ? dh_last + own : nullptr, col, G);
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    for (int c = (len + kC - 1) / kC - 1; c >= 0; --c) {
-        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
-        store_state(z, ends + state_at(z, c, n, h), col, G);
-        if (c == 0 && !dh0) break;
-        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-        __syncthreads();
-        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
-        if (wave == 0) load_gates(z, row0, bias, h, live, s.g);
-        __syncthreads();
-        f32x4 dO[4];
-        load_rows(d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr, z.o_t, live, there && d_o, dO);
-        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(t, s.g, s.K, s.Q, s.A, s.P);
-        __syncthreads();
-        if (wave < 4) invert_block(s.A, wave);
-        f32x4 X[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            X[b] = zero;
-#pragma unroll
-            for (int k = 0; k < DT; ++k) X[b] = multiply(frag(s.K, LD, 16 * b, 16 * k), G[k], X[b]);
-            X[b] *= rows_of(s.g.out, 16 * b);
-#pragma unroll
-            for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(s.P, kLA, 16 * b, 16 * i), dO[i], X[b]);
-        }
-        __syncthreads();
-        solve_t(s.A, X);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const f32x4 in = rows_of(s.g.in, 16 * b);
-            dO[b] *= in;
-            X[b] *= -in * rows_of(s.g.beta, 16 * b);
-        }
-        const float all = s.g.all;
-#pragma unroll
-        for (int k = 0; k < DT; ++k) {
-            G[k] *= all;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                G[k] = multiply(frag_t(s.Q, LD, 16 * k, 16 * b), dO[b], G[k]);
-                G[k] = multiply(frag_t(s.K, LD, 16 * k, 16 * b), X[b], G[k]);
-            }
-        }
-    }
-    if (dh0) store_state(z, dh0 + own, col, G);
-}
-
 // Four columns of a row in memory, as an operand's fragment: row row0 + l % 16, columns k0 + 4 (l / 16) and the next.
-template <typename T> __device__ __forceinline__ f32x4 frag_of(const T *m, long long ld, int row0, int rows, int k0, int columns, bool vec)
+template <typename T> __device__ __forceinline__ f32x4 frag_of(int l, const T *m, long long ld, int row0, int rows, int k0, int columns, bool vec)
 {
-    const int l = threadIdx.x & 63, row = row0 + (l & 15), k = k0 + 4 * (l >> 4);
+    const int row = row0 + (l & 15), k = k0 + 4 * (l >> 4);
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     if (row >= rows || k >= columns) return x;
     const T *p = m + row * ld + k;
@@ -474,6 +339,326 @@ template <typename T> __device__ __forceinline__ f32x4 frag_of(const T *m, long 
             if (k + e < columns) x[e] = (float)p[e];
     }
     return x;
+}
+
+template <int DT> struct Shared {
+    static constexpr int DP = 16 * DT, LD = DP + 4;
+    float K[kC * LD], Q[kC * LD], A[kC * kLA], P[kC * kLA];
+    Gates g;
+};
+
+// beta (V - exp(c) K S), in place of V
+template <int DT> __device__ __forceinline__ void below_state(int l, const Shared<DT> &s, const f32x4 (&S)[DT], f32x4 (&X)[4])
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < DT; ++k) acc = multiply(frag(l, s.K, s.LD, 16 * b, 16 * k), S[k], acc);
+        X[b] = rows_of(l, s.g.beta, 16 * b) * (X[b] - rows_of(l, s.g.in, 16 * b) * acc);
+        fence();
+    }
+}
+// exp(c) Q S + P U
+template <int DT> __device__ __forceinline__ void answers(int l, const Shared<DT> &s, const f32x4 (&S)[DT], const f32x4 (&U)[4], f32x4 (&O)[4])
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        O[b] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < DT; ++k) O[b] = multiply(frag(l, s.Q, s.LD, 16 * b, 16 * k), S[k], O[b]);
+        O[b] *= rows_of(l, s.g.in, 16 * b);
+#pragma unroll
+        for (int j = 0; j <= b; ++j) O[b] = multiply(frag(l, s.P, kLA, 16 * b, 16 * j), U[j], O[b]);
+        fence();
+    }
+}
+
+// ----------------------------------------------------------------------------- all steps
+// A block takes the columns of a state that its wavefronts hold, 16 each, through all chunks.
+template <typename T, int DT, int NW>
+__global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
+                                                            T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
+{
+    typedef Shared<DT> Lds;
+    constexpr int DP = Lds::DP, LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int l = fresh_lane();
+    const int col = (blockIdx.y * NW + wave) * 16 + (l & 15);
+    const bool there = col < z.Dv;
+    const int len = steps_of(z, lengths, n);
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 S[DT];
+    load_state(l, z, h0 ? h0 + own : nullptr, col, S);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < z.chunks; ++c) {
+        l = fresh_lane();
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
+        if (saved) store_state(l, z, saved + state_at(z, c, n, h), col, S);
+        T *out = o ? o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr;
+        f32x4 X[4] = {zero, zero, zero, zero};
+        if (live <= 0) {
+            if (o) store_rows(l, out, z.o_t, 0, rows, there, X);
+            continue;
+        }
+        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+        __syncthreads();
+        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+        if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
+        __syncthreads();
+        load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, X);
+        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+        __syncthreads();
+        if (wave < 4) invert_block(l, s.A, wave);
+        below_state<DT>(l, s, S, X);
+        __syncthreads();
+        solve(l, s.A, X);
+        if (o) {
+            f32x4 O[4];
+            answers<DT>(l, s, S, X, O);
+            store_rows(l, out, z.o_t, live, rows, there, O);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) X[b] *= rows_of(l, s.g.out, 16 * b);
+        const float all = s.g.all;
+#pragma unroll
+        for (int k = 0; k < DT; ++k) {
+            S[k] *= all;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) S[k] = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], S[k]);
+            fence();
+        }
+    }
+    if (h_last) store_state(l, z, h_last + own, col, S);
+}
+
+// ----------------------------------------------------------------------------- all chunks at once
+// A chunk takes S to M S + B, and the gradient behind it to M^T G + B'.  Where heads are few, the chunks' M and B are made beside each other (the products above for a state of
+// D + Dv columns, the unit matrix and zeros), then a small product a chunk goes through the sequence, and then everything else is done for all chunks beside each other.
+__host__ __device__ inline size_t matrices_at(const Sizes &z, int chunk, int n, int h) { return (((size_t)chunk * z.N + n) * z.H + h) * z.D * (z.D + z.Dv); }
+
+template <typename T, int DT, int NW, bool BACK>
+__global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
+                                                                 float *__restrict__ matrices)
+{
+    typedef Shared<DT> Lds;
+    constexpr int DP = Lds::DP, LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int c = blockIdx.x / (z.N * z.H), rest = blockIdx.x - c * (z.N * z.H), n = rest / z.H, h = rest - n * z.H, hk = h / (z.H / z.Hk);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = fresh_lane(), lc = l & 15, g4 = 4 * (l >> 4);
+    const int t0 = c * kC, len = steps_of(z, lengths, n), live = len - t0 < kC ? len - t0 : kC;
+    if (live <= 0) return;
+    // this wavefront's columns: of the unit matrix in front, or of v (or the gradient of o)
+    const int units = (z.D + 15) / 16, tile = blockIdx.y * NW + wave;
+    const bool unit = tile < units;
+    const int col = (unit ? tile : tile - units) * 16 + lc;
+    const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+    load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+    if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 V[4];
+    const bool there = !unit && col < z.Dv;
+    if (!BACK) load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, V);
+    else load_rows(l, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr, z.o_t, live, there && d_o, V);
+    __syncthreads();
+    for (int t = wave; t < (BACK ? 2 : 1) * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+    __syncthreads();
+    if (wave < 4) invert_block(l, s.A, wave);
+    __syncthreads();
+    f32x4 X[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        if (unit) {                     // the product of K and the unit matrix
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[b][r] = s.K[(16 * b + g4 + r) * LD + col];
+            X[b] *= BACK ? rows_of(l, s.g.out, 16 * b) : -rows_of(l, s.g.in, 16 * b) * rows_of(l, s.g.beta, 16 * b);
+        } else if (!BACK) {
+            X[b] = rows_of(l, s.g.beta, 16 * b) * V[b];
+        } else {
+            X[b] = zero;
+#pragma unroll
+            for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), V[i], X[b]);
+        }
+    }
+    if (BACK) solve_t(l, s.A, X);
+    else solve(l, s.A, X);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const f32x4 in = rows_of(l, s.g.in, 16 * b);
+        if (BACK) V[b] *= in;
+        X[b] *= BACK ? -in * rows_of(l, s.g.beta, 16 * b) : rows_of(l, s.g.out, 16 * b);
+    }
+    const float all = s.g.all;
+    const int width = unit ? z.D : z.Dv;
+    float *m = matrices + matrices_at(z, c, n, h) + (unit ? 0 : (size_t)z.D * z.D) + col;
+#pragma unroll
+    for (int k = 0; k < DT; ++k) {
+        f32x4 acc;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] = unit && 16 * k + g4 + r == col ? all : 0.f;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            if (BACK && !unit) acc = multiply(frag_t(l, s.Q, LD, 16 * k, 16 * b), V[b], acc);
+            acc = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], acc);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (16 * k + g4 + r < z.D && col < width) m[(size_t)(16 * k + g4 + r) * width] = acc[r];
+        fence();
+    }
+}
+
+// States in front of the chunks (BACK: gradients behind them) to `states`, and the last one to `last`.  A block takes 16 columns of a state, a wavefront 16 rows; the state goes round
+// through LDS, a column in a row.  What the next chunk needs is on its way meanwhile.
+template <int DT, bool BACK>
+__global__ __launch_bounds__(DT * 64) void delta_scan_kernel(Sizes z, const int *__restrict__ lengths, const float *__restrict__ matrices, const float *__restrict__ first,
+                                                             float *__restrict__ states, float *__restrict__ last)
+{
+    constexpr int DP = 16 * DT, LD = DP + 4;
+    __shared__ __attribute__((aligned(16))) float lds[2][16 * LD];
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = fresh_lane(), lc = l & 15, g4 = 4 * (l >> 4);
+    const int col = blockIdx.y * 16 + lc, row = 16 * wave + g4, len = steps_of(z, lengths, n), used = (len + kC - 1) / kC;
+    const bool vec = z.D % 4 == 0;
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 S, M[DT], B;
+    auto get = [&](const float *p, f32x4 &x) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = p && row + r < z.D && col < z.Dv ? p[(size_t)(row + r) * z.Dv + col] : 0.f;
+    };
+    auto put = [&](float *p) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (row + r < z.D && col < z.Dv) p[(size_t)(row + r) * z.Dv + col] = S[r];
+    };
+    auto fetch = [&](int i) {
+        const float *m = matrices + matrices_at(z, BACK ? used - 1 - i : i, n, h);
+#pragma unroll
+        for (int k = 0; k < DT; ++k) M[k] = frag_of(l, m, z.D, 16 * wave, z.D, 16 * k, z.D, vec);
+        get(m + (size_t)z.D * z.D, B);
+    };
+    get(first ? first + own : nullptr, S);
+    const int steps = last ? used : used - 1;       // products: the one behind the last state only if that is wanted
+    if (steps > 0) fetch(0);
+    for (int i = 0; i < used; ++i) {
+        put(states + state_at(z, BACK ? used - 1 - i : i, n, h));
+        if (i >= steps) break;
+        float *to = lds[i & 1];
+        *(f32x4 *)(to + lc * LD + row) = S;
+        lds_barrier();
+        f32x4 acc[2] = {B, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int k = 0; k < DT; ++k) acc[k & 1] = multiply(M[k], *(const f32x4 *)(to + lc * LD + 16 * k + g4), acc[k & 1]);
+        S = acc[0] + acc[1];
+        if (i + 1 < steps) fetch(i + 1);
+    }
+    if (!BACK)
+        for (int c = used; c < z.chunks; ++c) put(states + state_at(z, c, n, h));
+    if (last) put(last + own);
+}
+
+// What the chunks answer, given the states in front of them.
+template <typename T, int DT, int NW>
+__global__ __launch_bounds__(NW * 64) void delta_out_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ states,
+                                                            T *__restrict__ o)
+{
+    typedef Shared<DT> Lds;
+    constexpr int DP = Lds::DP;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int c = blockIdx.x / (z.N * z.H), rest = blockIdx.x - c * (z.N * z.H), n = rest / z.H, h = rest - n * z.H, hk = h / (z.H / z.Hk);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = fresh_lane(), col = (blockIdx.y * NW + wave) * 16 + (l & 15);
+    const bool there = col < z.Dv;
+    const int t0 = c * kC, len = steps_of(z, lengths, n), live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
+    T *out = o + t0 * z.o_t + n * z.o_n + h * z.Dv + col;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 X[4] = {zero, zero, zero, zero}, S[DT];
+    if (live <= 0) return store_rows(l, out, z.o_t, 0, rows, there, X);
+    const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+    load_state(l, z, states + state_at(z, c, n, h), col, S);
+    load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, X);
+    load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+    if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
+    __syncthreads();
+    for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+    __syncthreads();
+    if (wave < 4) invert_block(l, s.A, wave);
+    below_state<DT>(l, s, S, X);
+    __syncthreads();
+    solve(l, s.A, X);
+    f32x4 O[4];
+    answers<DT>(l, s, S, X, O);
+    store_rows(l, out, z.o_t, live, rows, there, O);
+}
+
+// ----------------------------------------------------------------------------- backwards
+// The gradients of the states that leave the chunks, from the last to the first, and of the initial state.
+template <typename T, int DT, int NW>
+__global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
+                                                             const float *__restrict__ dh_last, float *__restrict__ dh0, float *__restrict__ ends)
+{
+    typedef Shared<DT> Lds;
+    constexpr int DP = Lds::DP, LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds &s = *(Lds *)lds;
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int l = fresh_lane();
+    const int col = (blockIdx.y * NW + wave) * 16 + (l & 15);
+    const bool there = col < z.Dv;
+    const int len = steps_of(z, lengths, n);
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 G[DT];
+    load_state(l, z, dh_last ? dh_last + own : nullptr, col, G);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    for (int c = (len + kC - 1) / kC - 1; c >= 0; --c) {
+        l = fresh_lane();
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
+        store_state(l, z, ends + state_at(z, c, n, h), col, G);
+        if (c == 0 && !dh0) break;
+        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+        __syncthreads();
+        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+        if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
+        __syncthreads();
+        f32x4 dO[4];
+        load_rows(l, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr, z.o_t, live, there && d_o, dO);
+        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+        __syncthreads();
+        if (wave < 4) invert_block(l, s.A, wave);
+        f32x4 X[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            X[b] = zero;
+#pragma unroll
+            for (int k = 0; k < DT; ++k) X[b] = multiply(frag(l, s.K, LD, 16 * b, 16 * k), G[k], X[b]);
+            X[b] *= rows_of(l, s.g.out, 16 * b);
+#pragma unroll
+            for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), dO[i], X[b]);
+            fence();
+        }
+        __syncthreads();
+        solve_t(l, s.A, X);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 in = rows_of(l, s.g.in, 16 * b);
+            dO[b] *= in;
+            X[b] *= -in * rows_of(l, s.g.beta, 16 * b);
+        }
+        const float all = s.g.all;
+#pragma unroll
+        for (int k = 0; k < DT; ++k) {
+            G[k] *= all;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                G[k] = multiply(frag_t(l, s.Q, LD, 16 * k, 16 * b), dO[b], G[k]);
+                G[k] = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], G[k]);
+            }
+            fence();
+        }
+    }
+    if (dh0) store_state(l, z, dh0 + own, col, G);
 }
 
 // The gradients of a chunk's rows, given the states in front of and the gradients behind it.  A block takes a key head and the heads that share it, one after the other, so that
@@ -498,7 +683,13 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Lds &s = *(Lds *)lds;
     const int c = blockIdx.x / (z.N * z.Hk), rest = blockIdx.x - c * (z.N * z.Hk), n = rest / z.Hk, hk = rest - n * z.Hk, group = z.H / z.Hk;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, g4 = 4 * (l >> 4), lc = l & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int l = fresh_lane(), g4 = 4 * (l >> 4), lc = l & 15;
+    auto anew = [&] {
+        l = fresh_lane();
+        g4 = 4 * (l >> 4);
+        lc = l & 15;
+    };
     const int len = steps_of(z, lengths, n), t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
     const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
     T *out0 = dgi + t0 * z.gi_t + n * z.gi_n;
@@ -520,17 +711,18 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
 #pragma unroll
     for (int i = 0; i < RT; ++i) dQ[i] = dK[i] = zero;
     for (int h = hk * group; h < (hk + 1) * group; ++h) {
-        if (wave == 0) load_gates(z, row0, bias, h, live, s.g);
+        anew();
+        if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
         __syncthreads();
         f32x4 tile[KEEP], acc[KEEP];
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
             const int t = wave + i * NW;
             tile[i] = acc[i] = zero;
-            if (t < 2 * kTiles) tile[i] = make_tile<DP>(t, s.g, s.K, s.Q, s.A, s.P);
+            if (t < 2 * kTiles) tile[i] = make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
         }
         __syncthreads();
-        if (wave < 4) invert_block(s.A, wave);
+        if (wave < 4) invert_block(l, s.A, wave);
         __syncthreads();
         const float *S0 = saved + state_at(z, c, n, h), *G0 = ends + state_at(z, c, n, h);
         const T *do0 = d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr;
@@ -539,35 +731,39 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
         for (int i = 0; i < RT; ++i) E1[i] = E2[i] = E3[i] = zero;
         float both = 0.f;               // sum of S * G
         for (int v0 = 0; v0 < z.Dv; v0 += 64) {
+            anew();
             const int mine = 16 * (wave & 3) + lc, col = v0 + mine;
             const bool there = col < z.Dv;
             f32x4 R[4], X[4], S[DT];
             if (wave < 4) {
-                load_state(z, S0, col, S);
-                load_rows(row0 + v_at(z, h) + col, z.gi_t, live, there, R);
+                load_state(l, z, S0, col, S);
+                load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, R);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     X[b] = zero;
 #pragma unroll
-                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(s.K, LD, 16 * b, 16 * k), S[k], X[b]);
-                    R[b] -= rows_of(s.g.in, 16 * b) * X[b];
-                    X[b] = rows_of(s.g.beta, 16 * b) * R[b];
+                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(l, s.K, LD, 16 * b, 16 * k), S[k], X[b]);
+                    R[b] -= rows_of(l, s.g.in, 16 * b) * X[b];
+                    X[b] = rows_of(l, s.g.beta, 16 * b) * R[b];
+                    fence();
                 }
-                solve(s.A, X);
+                solve(l, s.A, X);
             } else {
-                load_state(z, G0, col, S);
-                load_rows(do0 ? do0 + col : nullptr, z.o_t, live, there && do0, R);
+                load_state(l, z, G0, col, S);
+                load_rows(l, do0 ? do0 + col : nullptr, z.o_t, live, there && do0, R);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     X[b] = zero;
 #pragma unroll
-                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(s.K, LD, 16 * b, 16 * k), S[k], X[b]);
-                    X[b] *= rows_of(s.g.out, 16 * b);
+                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(l, s.K, LD, 16 * b, 16 * k), S[k], X[b]);
+                    X[b] *= rows_of(l, s.g.out, 16 * b);
 #pragma unroll
-                    for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(s.P, kLA, 16 * b, 16 * i), R[i], X[b]);
+                    for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), R[i], X[b]);
+                    fence();
                 }
-                solve_t(s.A, X);
+                solve_t(l, s.A, X);
             }
+            anew();
             float *put = (wave < 4 ? s.U : s.X) + g4 * kLA + mine;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
@@ -588,33 +784,37 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
                 }
             } else {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) X[b] *= rows_of(s.g.beta, 16 * b);
-                store_rows(out0 + v_at(z, h) + col, z.gi_t, live, rows, there, X);
+                for (int b = 0; b < 4; ++b) X[b] *= rows_of(l, s.g.beta, 16 * b);
+                store_rows(l, out0 + v_at(z, h) + col, z.gi_t, live, rows, there, X);
             }
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) {
                 const int t = wave + i * NW;
                 int bi, bj;
+                anew();
                 if (t >= 2 * kTiles) break;
                 tile_at(t < kTiles ? t : t - kTiles, bi, bj);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const f32x4 a = t < kTiles ? frag(s.X, kLA, 16 * bi, 16 * k) : do0 ? frag_of(do0, z.o_t, 16 * bi, live, v0 + 16 * k, z.Dv, vec_do) : zero;
-                    acc[i] = multiply(a, frag(s.U, kLA, 16 * bj, 16 * k), acc[i]);
+                    const f32x4 a = t < kTiles ? frag(l, s.X, kLA, 16 * bi, 16 * k) : do0 ? frag_of(l, do0, z.o_t, 16 * bi, live, v0 + 16 * k, z.Dv, vec_do) : zero;
+                    acc[i] = multiply(a, frag(l, s.U, kLA, 16 * bj, 16 * k), acc[i]);
                 }
+                fence();
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const bool vec = z.Dv % 4 == 0;
-                const f32x4 sf = frag_of(S0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec), gf = frag_of(G0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec);
+                anew();
+                const f32x4 sf = frag_of(l, S0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec), gf = frag_of(l, G0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec);
                 if (rt0 == 0) both += (sf[0] * gf[0] + sf[1] * gf[1]) + (sf[2] * gf[2] + sf[3] * gf[3]);
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
                     const int b = rt0 + i;
-                    E1[i] = multiply(frag(s.X, kLA, 16 * b, 16 * k), sf, E1[i]);
-                    if (do0) E2[i] = multiply(frag_of(do0, z.o_t, 16 * b, live, v0 + 16 * k, z.Dv, vec_do), sf, E2[i]);
-                    E3[i] = multiply(frag(s.U, kLA, 16 * b, 16 * k), gf, E3[i]);
+                    E1[i] = multiply(frag(l, s.X, kLA, 16 * b, 16 * k), sf, E1[i]);
+                    if (do0) E2[i] = multiply(frag_of(l, do0, z.o_t, 16 * b, live, v0 + 16 * k, z.Dv, vec_do), sf, E2[i]);
+                    E3[i] = multiply(frag(l, s.U, kLA, 16 * b, 16 * k), gf, E3[i]);
                 }
+                fence();
             }
             __syncthreads();
         }
@@ -625,8 +825,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             int bi, bj;
             if (t >= 2 * kTiles) break;
             const bool is_a = t < kTiles;
+            anew();
             tile_at(is_a ? t : t - kTiles, bi, bj);
-            const f32x4 beta = rows_of(s.g.beta, 16 * bi), d = is_a ? -acc[i] : acc[i], L = decays(s.g, bi, bj, is_a);
+            const f32x4 beta = rows_of(l, s.g.beta, 16 * bi), d = is_a ? -acc[i] : acc[i], L = decays(l, s.g, bi, bj, is_a);
             const f32x4 by_row = d * tile[i], by_col = is_a ? beta * by_row : by_row;
             float sum = (by_col[0] + by_col[1]) + (by_col[2] + by_col[3]);
             sum += __shfl_xor(sum, 16, 64);
@@ -634,12 +835,14 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             if (l < 16) (is_a ? s.col_a : s.col_p)[bi][16 * bj + l] = sum;
             const f32x4 row = sum_columns(by_row);
             if (lc == 0) *(f32x4 *)&(is_a ? s.row_a : s.row_p)[bj][16 * bi + g4] = row;
-            store_tile(is_a ? s.A : s.P, bi, bj, is_a ? beta * d * L : d * L);
+            store_tile(l, is_a ? s.A : s.P, bi, bj, is_a ? beta * d * L : d * L);
+            fence();
         }
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int b = rt0 + i;
-            const f32x4 in = rows_of(s.g.in, 16 * b), k1 = -in * rows_of(s.g.beta, 16 * b) * E1[i], q1 = in * E2[i], e = rows_of(s.g.out, 16 * b) * E3[i];
+            anew();
+            const f32x4 in = rows_of(l, s.g.in, 16 * b), k1 = -in * rows_of(l, s.g.beta, 16 * b) * E1[i], q1 = in * E2[i], e = rows_of(l, s.g.out, 16 * b) * E3[i];
             f32x4 k, q;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -653,6 +856,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             }
             dQ[i] += q1;
             dK[i] += k1 + e;
+            fence();
         }
         if (rt0 == 0) {
 #pragma unroll
@@ -663,17 +867,19 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int b = rt0 + i;
+            anew();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x4 k = frag_t(s.K, LD, 16 * dt, 16 * j);
+                const f32x4 k = frag_t(l, s.K, LD, 16 * dt, 16 * j);
                 if (j <= b) {
-                    dK[i] = multiply(frag(s.A, kLA, 16 * b, 16 * j), k, dK[i]);
-                    dQ[i] = multiply(frag(s.P, kLA, 16 * b, 16 * j), k, dQ[i]);
+                    dK[i] = multiply(frag(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
+                    dQ[i] = multiply(frag(l, s.P, kLA, 16 * b, 16 * j), k, dQ[i]);
                 }
                 if (j >= b) {
-                    dK[i] = multiply(frag_t(s.A, kLA, 16 * b, 16 * j), k, dK[i]);
-                    dK[i] = multiply(frag_t(s.P, kLA, 16 * b, 16 * j), frag_t(s.Q, LD, 16 * dt, 16 * j), dK[i]);
+                    dK[i] = multiply(frag_t(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
+                    dK[i] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), frag_t(l, s.Q, LD, 16 * dt, 16 * j), dK[i]);
                 }
+                fence();
             }
         }
         if (wave == NW - 1) {           // the gates, a step a lane
@@ -862,12 +1068,15 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
     if (!rows_apart(d.T, d.N, width, d.gi_t, d.gi_n) || !rows_apart(d.T, d.N, (long long)d.H * d.Dv, d.o_t, d.o_n)) return NSK_ERR_BAD_DESC;
     // (a launch has fewer than 2^32 threads)
     const long long chunks = ((long long)d.T + kC - 1) / kC;
-    if (d.D > kMostWidth || d.Dv > kMostWidth || d.T > 1 << 30 || (long long)d.N * d.H >= 1LL << 22 || chunks * d.N * d.Hk >= 1LL << 23) return NSK_ERR_UNSUPPORTED;
+    if (d.D > kMostWidth || d.Dv > kMostWidth || d.T > 1 << 30 || (long long)d.N * d.H >= 1LL << 22 || chunks * d.N * d.H >= 1LL << 22) return NSK_ERR_UNSUPPORTED;
     const int whole = d.dtype == NSK_BF16 ? 8 : 4;
     const bool vec = d.D % whole == 0 && (d.T == 1 || d.gi_t % whole == 0) && (d.N == 1 || d.gi_n % whole == 0);
     z = {d.T, d.N, d.H, d.Hk, d.D, d.Dv, (int)chunks, vec, d.T == 1 ? 0 : d.gi_t, d.N == 1 ? 0 : d.gi_n, d.T == 1 ? 0 : d.o_t, d.N == 1 ? 0 : d.o_n};
     return NSK_OK;
 }
+// The states (or gradients) of all chunks, and behind them their matrices where the chunks are taken all at once.
+bool at_once(const Sizes &z) { return z.chunks > 2 && (long long)z.N * z.H < 192; }
+size_t matrices_of(const Sizes &z) { return at_once(z) ? matrices_at(z, z.chunks, 0, 0) * sizeof(float) : 0; }
 size_t saved_of(const Sizes &z) { return (size_t)z.chunks * z.N * z.H * z.D * z.Dv * sizeof(float); }
 
 // A call with the tiles of D and the wavefronts' columns as constants.
@@ -895,7 +1104,8 @@ size_t nsk_delta_saved_bytes(const nsk_delta_desc_t *desc)
 size_t nsk_delta_workspace_bytes(const nsk_delta_desc_t *desc, int pass)
 {
     Sizes z;
-    return pass == NSK_PASS_DGRAD && check(desc, z) == NSK_OK ? saved_of(z) : 0;
+    if ((pass != NSK_PASS_FWD && pass != NSK_PASS_DGRAD) || check(desc, z) != NSK_OK) return 0;
+    return pass == NSK_PASS_DGRAD || at_once(z) ? align_up(saved_of(z)) + matrices_of(z) : 0;
 }
 
 int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0, void *o, float *h_last, float *saved, void *workspace,
@@ -907,15 +1117,27 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (!gi || (!o && !h_last)) return NSK_ERR_NULL;
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(h0) || unaligned16(o) || unaligned16(h_last) || unaligned16(saved) || unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    (void)workspace_bytes;
+    if (at_once(z) && (!workspace || workspace_bytes < align_up(saved_of(z)) + matrices_of(z))) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
+    float *matrices = (float *)((char *)workspace + align_up(saved_of(z))), *states = saved ? saved : (float *)workspace;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
         return with_sizes(z, [&](auto dt, auto nw) {
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
             const size_t bytes = sizeof(Shared<DT>);
-            const int allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
+            int allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
+            if (allowed == NSK_OK) allowed = allow_lds<delta_matrices_kernel<T, DT, NW, false>>(bytes);
+            if (allowed == NSK_OK) allowed = allow_lds<delta_out_kernel<T, DT, NW>>(bytes);
             if (allowed != NSK_OK) return allowed;
+            if (at_once(z)) {
+                const unsigned all = (unsigned)(z.chunks * z.N * z.H);
+                hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, false>), dim3(all, (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)), dim3(NW * 64), bytes, st, z,
+                                   (const T *)gi, bias, lengths, (const T *)nullptr, matrices);
+                hipLaunchKernelGGL((delta_scan_kernel<DT, false>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16)), dim3(DT * 64), 0, st, z, lengths, matrices, h0, states, h_last);
+                if (o)
+                    hipLaunchKernelGGL((delta_out_kernel<T, DT, NW>), dim3(all, (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, states, (T *)o);
+                return check_launch();
+            }
             hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0, (T *)o,
                                h_last, saved);
             return check_launch();
@@ -934,9 +1156,9 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(saved) || unaligned16(d_o) || unaligned16(dh_last) || unaligned16(dgi) || unaligned16(dh0) ||
         unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    if (!workspace || workspace_bytes < saved_of(z)) return NSK_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < align_up(saved_of(z)) + matrices_of(z)) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    float *ends = (float *)workspace;
+    float *ends = (float *)workspace, *matrices = (float *)((char *)workspace + align_up(saved_of(z)));
     const int vec_do = z.Dv % 4 == 0 && z.o_t % 4 == 0 && z.o_n % 4 == 0;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
@@ -945,10 +1167,17 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             const size_t bytes = sizeof(Shared<DT>), grad_bytes = sizeof(GradShared<DT>);
             static_assert(sizeof(GradShared<DT>) <= 160 * 1024, "what a compute unit has");
             int allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
+            if (allowed == NSK_OK) allowed = allow_lds<delta_matrices_kernel<T, DT, NW, true>>(bytes);
             if (allowed == NSK_OK) allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);
             if (allowed != NSK_OK) return allowed;
-            hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,
-                               (const T *)d_o, dh_last, dh0, ends);
+            if (at_once(z)) {
+                hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, true>), dim3((unsigned)(z.chunks * z.N * z.H), (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)),
+                                   dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, (const T *)d_o, matrices);
+                hipLaunchKernelGGL((delta_scan_kernel<DT, true>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16)), dim3(DT * 64), 0, st, z, lengths, matrices, dh_last, ends, dh0);
+            } else {
+                hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,
+                                   (const T *)d_o, dh_last, dh0, ends);
+            }
             hipLaunchKernelGGL((delta_grad_kernel<T, DT>), dim3((unsigned)(z.chunks * z.N * z.Hk)), dim3(kGradWaves * 64), grad_bytes, st, z, vec_do, (const T *)gi, bias, lengths, saved,
                                (const T *)d_o, ends, (T *)dgi);
             return check_launch();
