@@ -79,6 +79,15 @@ __device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c)
 }
 // Nothing is moved across: the fragments of one row of tiles are in flight at a time, not those of a whole product, for which there are not enough registers.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+// Sums that are read behind a branch or in a loop's next round.  A matrix instruction's result may be read 11 wait states after it at the earliest; within a block of instructions the
+// compiler sees to that, but where a branch ended with one and a block of a jump alone lay between, it left no wait, and what was read was the sum before the last products.
+template <int N> __device__ __forceinline__ void settle(f32x4 (&x)[N])
+{
+    fence();
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("s_nop 15" : "+v"(x[i]));
+    fence();
+}
 __device__ __forceinline__ f32x4 rows_of(int l, const float *v, int row0) { return *(const f32x4 *)(v + row0 + 4 * (l >> 4)); }
 // Sums over the 16 columns of a tile; all lanes have them.
 __device__ __forceinline__ f32x4 sum_columns(f32x4 v)
@@ -92,40 +101,57 @@ __device__ __forceinline__ f32x4 sum_columns(f32x4 v)
 
 // ----------------------------------------------------------------------------- what a chunk starts with
 struct alignas(16) Gates {
-    double c[kC];               // sums of log alpha: differences of far ones keep what matters
+    double c[kC];               // sums of log alpha to the base of two: differences of far ones keep what matters
     float beta[kC], in[kC], out[kC];        // beta, exp(c), exp(C - c)
     float rest_a[kC], rest_b[kC];           // 1 - alpha, 1 - beta
     float all;                  // exp(C)
 };
-// By one wavefront.  Steps from `live` on leave the state as it is.
-template <typename T> __device__ void load_gates(int i, const Sizes &z, const T *row, const float *bias, int h, int live, Gates &g)
-{
-    double la = 0.;
-    float beta = 0.f, rest_a = 0.f, rest_b = 0.f;
-    if (i < live) {
+// By one wavefront, a step a lane.  Steps from `live` on leave the state as it is.
+__device__ __forceinline__ float exp_of(double c) { return __builtin_amdgcn_exp2f((float)c); }
+template <typename T> struct GateParts {
+    float a, b;
+    __device__ __forceinline__ void load(int i, const Sizes &z, const T *row, int h, int live)
+    {
+        a = b = 0.f;
+        if (i >= live) return;
         const T *p = row + i * z.gi_t;
-        const float a = (float)p[a_at(z, h)] + (bias ? bias[h] : 0.f), b = (float)p[b_at(z, h)] + (bias ? bias[z.H + h] : 0.f);
-        // log sigmoid(a); below -1000 alpha is 0 in any type, and a sum of infinities would have no differences.  Its rounding, 2^-24 of it, is the more the less the product
-        // of gates counts: x exp(-x) is at most 0.37.  (NaN stays NaN: fminf of it and 0 would be 0, but not the sum's other part.)
-        la = a < -1000.f ? -1000.f : fminf(a, 0.f) - log1pf(expf(-fabsf(a)));
-        beta = sigmoid(b);
-        rest_a = sigmoid(-a);
-        rest_b = sigmoid(-b);
+        a = (float)p[a_at(z, h)];
+        b = (float)p[b_at(z, h)];
     }
-    double c = la;
+    __device__ __forceinline__ void finish(int i, const Sizes &z, const float *bias, int h, int live, Gates &g) const
+    {
+        double la = 0.;
+        float beta = 0.f, rest_a = 0.f, rest_b = 0.f;
+        if (i < live) {
+            const float x = a + (bias ? bias[h] : 0.f), y = b + (bias ? bias[z.H + h] : 0.f);
+            // log sigmoid(x); below -1000 alpha is 0 in any type, and a sum of infinities would have no differences.  Its rounding, 2^-24 of it, is the more the less the product
+            // of gates counts: t exp(-t) is at most 0.37.  (NaN stays NaN: fminf of it and 0 would be 0, but not the sum's other part.)
+            la = x < -1000.f ? -1000.f : fminf(x, 0.f) - log1pf(expf(-fabsf(x)));
+            beta = sigmoid(y);
+            rest_a = sigmoid(-x);
+            rest_b = sigmoid(-y);
+        }
+        double c = la * 1.4426950408889634;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double up = __shfl_up(c, o, 64);
-        if (i >= o) c += up;
+        for (int o = 1; o < 64; o <<= 1) {
+            const double up = __shfl_up(c, o, 64);
+            if (i >= o) c += up;
+        }
+        const double C = __shfl(c, 63, 64);
+        g.c[i] = c;
+        g.beta[i] = beta;
+        g.in[i] = exp_of(c);
+        g.out[i] = exp_of(C - c);
+        g.rest_a[i] = rest_a;
+        g.rest_b[i] = rest_b;
+        if (i == 0) g.all = exp_of(C);
     }
-    const double C = __shfl(c, 63, 64);
-    g.c[i] = c;
-    g.beta[i] = beta;
-    g.in[i] = expf((float)c);
-    g.out[i] = expf((float)(C - c));
-    g.rest_a[i] = rest_a;
-    g.rest_b[i] = rest_b;
-    if (i == 0) g.all = expf((float)C);
+};
+template <typename T> __device__ __forceinline__ void load_gates(int l, const Sizes &z, const T *row, const float *bias, int h, int live, Gates &g)
+{
+    GateParts<T> p;
+    p.load(l, z, row, h, live);
+    p.finish(l, z, bias, h, live, g);
 }
 
 // A row of q or k: kThreads / 64 neighbouring lanes take vectors of 16 bytes in turn.
@@ -175,24 +201,29 @@ template <typename T, int DP, int THREADS> struct RowPart {
         }
     }
 };
-// Normalised keys and queries of a chunk into LDS, [64][DP + 4]; lengths: NULL, or where 1 / |k| and 1 / |q| go.
-template <typename T, int DP, int THREADS>
-__device__ __forceinline__ void load_keys(const Sizes &z, const T *row0, int hk, int live, float *K, float *Q, float *inv_k, float *inv_q)
-{
+// Normalised keys and queries of a chunk into LDS, [64][DP + 4]; inv_k, inv_q: NULL, or where 1 / |k| and 1 / |q| go.
+template <typename T, int DP, int THREADS> struct KeyParts {
     typedef RowPart<T, DP, THREADS> Part;
-    const int r = threadIdx.x / Part::LANES;
-    const T *row = row0 + r * z.gi_t;
     Part k, q;
-    k.load(row + k_at(z, hk), z.D, r < live, z.vec);
-    q.load(row + q_at(z, hk), z.D, r < live, z.vec);
-    const float ik = k.inverse_length(), iq = q.inverse_length();
-    k.store(K + r * (DP + 4), ik);
-    q.store(Q + r * (DP + 4), iq / sqrtf((float)z.D));
-    if (inv_k && threadIdx.x % Part::LANES == 0) {
-        inv_k[r] = ik;
-        inv_q[r] = iq;
+    __device__ __forceinline__ void load(const Sizes &z, const T *row0, int hk, int live)
+    {
+        const int r = threadIdx.x / Part::LANES;
+        const T *row = row0 + r * z.gi_t;
+        k.load(row + k_at(z, hk), z.D, r < live, z.vec);
+        q.load(row + q_at(z, hk), z.D, r < live, z.vec);
     }
-}
+    __device__ __forceinline__ void finish(const Sizes &z, float *K, float *Q, float *inv_k, float *inv_q) const
+    {
+        const int r = threadIdx.x / Part::LANES;
+        const float ik = k.inverse_length(), iq = q.inverse_length();
+        k.store(K + r * (DP + 4), ik);
+        q.store(Q + r * (DP + 4), iq / sqrtf((float)z.D));
+        if (inv_k && threadIdx.x % Part::LANES == 0) {
+            inv_k[r] = ik;
+            inv_q[r] = iq;
+        }
+    }
+};
 
 // The tiles of 16 x 16 of A and P that are not zero: 10 each.
 constexpr int kTiles = 10;
@@ -207,7 +238,7 @@ __device__ __forceinline__ f32x4 decays(int l, const Gates &g, int bi, int bj, b
     const int i0 = 16 * bi + 4 * (l >> 4), j = 16 * bj + (l & 15);
     f32x4 d;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) d[r] = i0 + r > j || (!strict && i0 + r == j) ? expf((float)(g.c[i0 + r] - g.c[j])) : 0.f;
+    for (int r = 0; r < 4; ++r) d[r] = bi > bj || i0 + r > j || (!strict && i0 + r == j) ? exp_of(g.c[i0 + r] - g.c[j]) : 0.f;
     return d;
 }
 template <int DP> __device__ __forceinline__ f32x4 dot_tile(int l, const float *X, const float *K, int bi, int bj)
@@ -228,7 +259,9 @@ template <int DP> __device__ __forceinline__ f32x4 make_tile(int l, int t, const
 {
     int bi, bj;
     tile_at(t < kTiles ? t : t - kTiles, bi, bj);
-    const f32x4 d = decays(l, g, bi, bj, t < kTiles), x = d * dot_tile<DP>(l, t < kTiles ? K : Q, K, bi, bj);
+    f32x4 dot[1] = {dot_tile<DP>(l, t < kTiles ? K : Q, K, bi, bj)};
+    settle(dot);
+    const f32x4 x = decays(l, g, bi, bj, t < kTiles) * dot[0];
     if (t < kTiles) store_tile(l, A, bi, bj, -rows_of(l, g.beta, 16 * bi) * x);
     else store_tile(l, P, bi, bj, x);
     return x;
@@ -240,12 +273,17 @@ __device__ __forceinline__ void invert_block(int l, float *A, int w)
     float *m = A + 16 * w * kLA + 16 * w;
     float x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i == c ? 1.f : 0.f;
-    // a value is taken out of all rows below it at once: 15 steps that wait for each other, not 120
+    for (int i = 0; i < 16; ++i) {
+        float sum[2] = {i == c ? 1.f : 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 15; ++j)
+        for (int j = 0; j < i; j += 4) {
+            const f32x4 a = *(const f32x4 *)(m + i * kLA + j);
 #pragma unroll
-        for (int i = j + 1; i < 16; ++i) x[i] = fmaf(m[i * kLA + j], x[j], x[i]);
+            for (int e = 0; e < 4; ++e)
+                if (j + e < i) sum[e & 1] = fmaf(a[e], x[j + e], sum[e & 1]);
+        }
+        x[i] = sum[0] + sum[1];
+    }
     if (l < 16)
 #pragma unroll
         for (int i = 0; i < 16; ++i) m[i * kLA + c] = x[i];
@@ -272,72 +310,88 @@ __device__ __forceinline__ void solve_t(int l, const float *A, f32x4 (&X)[4])
     }
 }
 
+// Rows are reached through buffer descriptors: what lies at or behind `bytes` reads as zero and is not written, and so is a lane's offset of kNowhere plus anything below 2^31.  An access is
+// a lane's offset plus a uniform one: one instruction, where 64-bit addresses and conditions took six.
+constexpr unsigned kNowhere = 0x80000000u;
+constexpr long long kMostStride = 1LL << 25;       // elements from a step to the next: 16 steps within 2^31 bytes
+template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const T *p, long long bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)bytes, 0x00020000); }
+template <typename T> __device__ __forceinline__ unsigned load_raw(__amdgpu_buffer_rsrc_t b, unsigned at)
+{
+    if constexpr (sizeof(T) == 2) return (unsigned)__builtin_amdgcn_raw_buffer_load_b16(b, at, 0, 0);
+    else return (unsigned)__builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0);
+}
+template <typename T> __device__ __forceinline__ float value_of(unsigned raw) { return __builtin_bit_cast(float, sizeof(T) == 2 ? raw << 16 : raw); }
+template <typename T> __device__ __forceinline__ void store(float v, __amdgpu_buffer_rsrc_t b, unsigned at)
+{
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (T)v), b, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), b, at, 0, 0);
+}
+
 // 16 columns of a state [D,Dv] in registers.
 template <int DT> __device__ __forceinline__ void load_state(int l, const Sizes &z, const float *s, int col, f32x4 (&S)[DT])
 {
-    const int g = l >> 4;
+    const __amdgpu_buffer_rsrc_t b = buffer(s, s ? z.D * z.Dv * 4 : 0);
+    const unsigned at = col < z.Dv ? (unsigned)(4 * (l >> 4) * z.Dv + col) * 4 : kNowhere;
 #pragma unroll
     for (int k = 0; k < DT; ++k)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = 16 * k + 4 * g + r;
-            S[k][r] = s && d < z.D && col < z.Dv ? s[(size_t)d * z.Dv + col] : 0.f;
-        }
+        for (int r = 0; r < 4; ++r) S[k][r] = value_of<float>(load_raw<float>(b, at + (16 * k + r) * z.Dv * 4));
 }
 template <int DT> __device__ __forceinline__ void store_state(int l, const Sizes &z, float *s, int col, const f32x4 (&S)[DT])
 {
-    const int g = l >> 4;
+    const __amdgpu_buffer_rsrc_t b = buffer(s, z.D * z.Dv * 4);
+    const unsigned at = col < z.Dv ? (unsigned)(4 * (l >> 4) * z.Dv + col) * 4 : kNowhere;
 #pragma unroll
     for (int k = 0; k < DT; ++k)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = 16 * k + 4 * g + r;
-            if (d < z.D && col < z.Dv) s[(size_t)d * z.Dv + col] = S[k][r];
-        }
+        for (int r = 0; r < 4; ++r) store<float>(S[k][r], b, at + (16 * k + r) * z.Dv * 4);
 }
-// 16 columns of the chunk's rows of v, o or their gradients; rows from `live` on are not read, and written as zeros.
-template <typename T> __device__ __forceinline__ void load_rows(int l, const T *p, long long stride, int live, bool there, f32x4 (&X)[4])
+// 16 columns of the chunk's rows of v, o or their gradients, [.., Dv] from p on; rows from `live` on are not read, and written as zeros.
+struct Raw {
+    unsigned x[4][4];
+};
+template <typename T> __device__ __forceinline__ unsigned row_bytes(const Sizes &z, long long stride, int rows)
 {
-    const int g = l >> 4;
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * b + 4 * g + r;
-            X[b][r] = there && i < live ? (float)p[i * stride] : 0.f;
-        }
+    return rows <= 0 ? 0 : (unsigned)(((rows < 16 ? rows : 16) - 1) * stride + z.Dv) * (unsigned)sizeof(T);
 }
-template <typename T> __device__ __forceinline__ void store_rows(int l, T *p, long long stride, int live, int rows, bool there, const f32x4 (&X)[4])
+template <typename T> __device__ __forceinline__ void load_rows(int l, const Sizes &z, const T *p, long long stride, int live, int col, Raw &X)
 {
-    const int g = l >> 4;
+    const unsigned by = (unsigned)stride * (unsigned)sizeof(T), at = col < z.Dv ? 4 * (l >> 4) * by + col * (unsigned)sizeof(T) : kNowhere;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 4; ++b) {
+        const __amdgpu_buffer_rsrc_t m = buffer(p + 16 * b * stride, p ? row_bytes<T>(z, stride, live - 16 * b) : 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * b + 4 * g + r;
-            if (there && i < rows) p[i * stride] = (T)(i < live ? X[b][r] : 0.f);
-        }
-}
-
-// Four columns of a row in memory, as an operand's fragment: row row0 + l % 16, columns k0 + 4 (l / 16) and the next.
-template <typename T> __device__ __forceinline__ f32x4 frag_of(int l, const T *m, long long ld, int row0, int rows, int k0, int columns, bool vec)
-{
-    const int row = row0 + (l & 15), k = k0 + 4 * (l >> 4);
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (row >= rows || k >= columns) return x;
-    const T *p = m + row * ld + k;
-    struct alignas(4 * sizeof(T)) Q {
-        T q[4];
-    };
-    if (vec) {
-        const Q q = *(const Q *)p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (float)q.q[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (k + e < columns) x[e] = (float)p[e];
+        for (int r = 0; r < 4; ++r) X.x[b][r] = load_raw<T>(m, at + r * by);
     }
+}
+template <typename T> __device__ __forceinline__ void values_of(const Raw &raw, f32x4 (&X)[4])
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) X[b][r] = value_of<T>(raw.x[b][r]);
+}
+template <typename T> __device__ __forceinline__ void store_rows(int l, const Sizes &z, T *p, long long stride, int live, int rows, int col, const f32x4 (&X)[4])
+{
+    const unsigned by = (unsigned)stride * (unsigned)sizeof(T), at = col < z.Dv ? 4 * (l >> 4) * by + col * (unsigned)sizeof(T) : kNowhere;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const __amdgpu_buffer_rsrc_t m = buffer(p + 16 * b * stride, row_bytes<T>(z, stride, rows - 16 * b));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) store<T>(16 * b + 4 * (l >> 4) + r < live ? X[b][r] : 0.f, m, at + r * by);
+    }
+}
+// Four columns of a row of a matrix [rows, columns] in memory, as an operand's fragment: row row0 + l % 16, columns k0 + 4 (l / 16) and the next.
+__device__ __forceinline__ f32x4 frag_of(int l, const float *m, int rows, int row0, int columns, int k0, bool vec)
+{
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    const __amdgpu_buffer_rsrc_t b = buffer(m, rows * columns * 4);
+    const int k = k0 + 4 * (l >> 4);
+    const unsigned at = (unsigned)((row0 + (l & 15)) * columns + k) * 4;
+    if (vec) return __builtin_bit_cast(f32x4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, k < columns ? at : kNowhere, 0, 0));
+    f32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = value_of<float>(load_raw<float>(b, k + e < columns ? at + 4 * e : kNowhere));
     return x;
 }
 
@@ -387,38 +441,49 @@ __global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__
     const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int l = fresh_lane();
     const int col = (blockIdx.y * NW + wave) * 16 + (l & 15);
-    const bool there = col < z.Dv;
     const int len = steps_of(z, lengths, n);
     const size_t own = state_at(z, 0, n, h);
     f32x4 S[DT];
     load_state(l, z, h0 ? h0 + own : nullptr, col, S);
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    // a chunk's rows are on their way while the chunk in front of it is worked on
+    KeyParts<T, DP, NW * 64> keys;
+    GateParts<T> gates;
+    Raw v;
+    auto fetch = [&](int c) {
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
+        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+        keys.load(z, row0, hk, live);
+        if (wave == 0) gates.load(l, z, row0, h, live);
+        load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, col, v);
+    };
+    if (len > 0) fetch(0);
     for (int c = 0; c < z.chunks; ++c) {
         l = fresh_lane();
         const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
         if (saved) store_state(l, z, saved + state_at(z, c, n, h), col, S);
-        T *out = o ? o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr;
-        f32x4 X[4] = {zero, zero, zero, zero};
+        T *out = o ? o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr;
+        f32x4 X[4] = {};
         if (live <= 0) {
-            if (o) store_rows(l, out, z.o_t, 0, rows, there, X);
+            if (o) store_rows(l, z, out, z.o_t, 0, rows, col, X);
             continue;
         }
-        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-        __syncthreads();
-        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
-        if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-        __syncthreads();
-        load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, X);
+        lds_barrier();
+        keys.finish(z, s.K, s.Q, nullptr, nullptr);
+        if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
+        values_of<T>(v, X);
+        if (t0 + kC < len) fetch(c + 1);
+        fence();
+        lds_barrier();
         for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
-        __syncthreads();
+        lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
         below_state<DT>(l, s, S, X);
-        __syncthreads();
+        lds_barrier();
         solve(l, s.A, X);
         if (o) {
             f32x4 O[4];
             answers<DT>(l, s, S, X, O);
-            store_rows(l, out, z.o_t, live, rows, there, O);
+            store_rows(l, z, out, z.o_t, live, rows, col, O);
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) X[b] *= rows_of(l, s.g.out, 16 * b);
@@ -430,6 +495,7 @@ __global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__
             for (int b = 0; b < 4; ++b) S[k] = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], S[k]);
             fence();
         }
+        settle(S);
     }
     if (h_last) store_state(l, z, h_last + own, col, S);
 }
@@ -456,32 +522,40 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
     const bool unit = tile < units;
     const int col = (unit ? tile : tile - units) * 16 + lc;
     const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-    load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
+    KeyParts<T, DP, NW * 64> keys;
+    keys.load(z, row0, hk, live);
+    Raw raw;
+    if (BACK) load_rows(l, z, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr, z.o_t, live, unit ? z.Dv : col, raw);
+    else load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, unit ? z.Dv : col, raw);
     if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
+    keys.finish(z, s.K, s.Q, nullptr, nullptr);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    f32x4 V[4];
-    const bool there = !unit && col < z.Dv;
-    if (!BACK) load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, V);
-    else load_rows(l, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr, z.o_t, live, there && d_o, V);
-    __syncthreads();
+    lds_barrier();
     for (int t = wave; t < (BACK ? 2 : 1) * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
-    __syncthreads();
+    lds_barrier();
     if (wave < 4) invert_block(l, s.A, wave);
-    __syncthreads();
+    lds_barrier();
+    f32x4 V[4];
+    values_of<T>(raw, V);
     f32x4 X[4];
+    if (unit) {                         // the product of K and the unit matrix
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        if (unit) {                     // the product of K and the unit matrix
+        for (int b = 0; b < 4; ++b) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) X[b][r] = s.K[(16 * b + g4 + r) * LD + col];
             X[b] *= BACK ? rows_of(l, s.g.out, 16 * b) : -rows_of(l, s.g.in, 16 * b) * rows_of(l, s.g.beta, 16 * b);
-        } else if (!BACK) {
-            X[b] = rows_of(l, s.g.beta, 16 * b) * V[b];
-        } else {
+        }
+    } else if (!BACK) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) X[b] = rows_of(l, s.g.beta, 16 * b) * V[b];
+    } else {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
             X[b] = zero;
 #pragma unroll
             for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), V[i], X[b]);
         }
+        settle(X);
     }
     if (BACK) solve_t(l, s.A, X);
     else solve(l, s.A, X);
@@ -501,7 +575,7 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
         for (int r = 0; r < 4; ++r) acc[r] = unit && 16 * k + g4 + r == col ? all : 0.f;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            if (BACK && !unit) acc = multiply(frag_t(l, s.Q, LD, 16 * k, 16 * b), V[b], acc);
+            if (BACK) acc = multiply(frag_t(l, s.Q, LD, 16 * k, 16 * b), V[b], acc);       // (zeros in the unit matrix's columns)
             acc = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], acc);
         }
 #pragma unroll
@@ -523,36 +597,47 @@ __global__ __launch_bounds__(DT * 64) void delta_scan_kernel(Sizes z, const int 
     const int col = blockIdx.y * 16 + lc, row = 16 * wave + g4, len = steps_of(z, lengths, n), used = (len + kC - 1) / kC;
     const bool vec = z.D % 4 == 0;
     const size_t own = state_at(z, 0, n, h);
-    f32x4 S, M[DT], B;
+    f32x4 S;
+    struct Chunk {
+        f32x4 M[DT], B;
+    };
+    Chunk chunk[2];
+    const unsigned at = col < z.Dv ? (unsigned)(row * z.Dv + col) * 4 : kNowhere;
     auto get = [&](const float *p, f32x4 &x) {
+        const __amdgpu_buffer_rsrc_t b = buffer(p, p ? z.D * z.Dv * 4 : 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = p && row + r < z.D && col < z.Dv ? p[(size_t)(row + r) * z.Dv + col] : 0.f;
+        for (int r = 0; r < 4; ++r) x[r] = value_of<float>(load_raw<float>(b, at + r * z.Dv * 4));
     };
     auto put = [&](float *p) {
+        const __amdgpu_buffer_rsrc_t b = buffer(p, z.D * z.Dv * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (row + r < z.D && col < z.Dv) p[(size_t)(row + r) * z.Dv + col] = S[r];
+        for (int r = 0; r < 4; ++r) store<float>(S[r], b, at + r * z.Dv * 4);
     };
-    auto fetch = [&](int i) {
+    auto fetch = [&](int i, Chunk &x) {
         const float *m = matrices + matrices_at(z, BACK ? used - 1 - i : i, n, h);
 #pragma unroll
-        for (int k = 0; k < DT; ++k) M[k] = frag_of(l, m, z.D, 16 * wave, z.D, 16 * k, z.D, vec);
-        get(m + (size_t)z.D * z.D, B);
+        for (int k = 0; k < DT; ++k) x.M[k] = frag_of(l, m, z.D, 16 * wave, z.D, 16 * k, vec);
+        get(m + (size_t)z.D * z.D, x.B);
     };
     get(first ? first + own : nullptr, S);
     const int steps = last ? used : used - 1;       // products: the one behind the last state only if that is wanted
-    if (steps > 0) fetch(0);
-    for (int i = 0; i < used; ++i) {
+    auto step = [&](int i, const Chunk &now, Chunk &next) {
         put(states + state_at(z, BACK ? used - 1 - i : i, n, h));
-        if (i >= steps) break;
+        if (i >= steps) return;
+        if (i + 1 < steps) fetch(i + 1, next);
         float *to = lds[i & 1];
         *(f32x4 *)(to + lc * LD + row) = S;
         lds_barrier();
-        f32x4 acc[2] = {B, {0.f, 0.f, 0.f, 0.f}};
+        f32x4 acc[2] = {now.B, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int k = 0; k < DT; ++k) acc[k & 1] = multiply(M[k], *(const f32x4 *)(to + lc * LD + 16 * k + g4), acc[k & 1]);
+        for (int k = 0; k < DT; ++k) acc[k & 1] = multiply(now.M[k], *(const f32x4 *)(to + lc * LD + 16 * k + g4), acc[k & 1]);
+        settle(acc);
         S = acc[0] + acc[1];
-        if (i + 1 < steps) fetch(i + 1);
+    };
+    if (steps > 0) fetch(0, chunk[0]);
+    for (int i = 0; i < used; i += 2) {
+        step(i, chunk[0], chunk[1]);
+        if (i + 1 < used) step(i + 1, chunk[1], chunk[0]);
     }
     if (!BACK)
         for (int c = used; c < z.chunks; ++c) put(states + state_at(z, c, n, h));
@@ -570,27 +655,30 @@ __global__ __launch_bounds__(NW * 64) void delta_out_kernel(Sizes z, const T *__
     Lds &s = *(Lds *)lds;
     const int c = blockIdx.x / (z.N * z.H), rest = blockIdx.x - c * (z.N * z.H), n = rest / z.H, h = rest - n * z.H, hk = h / (z.H / z.Hk);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = fresh_lane(), col = (blockIdx.y * NW + wave) * 16 + (l & 15);
-    const bool there = col < z.Dv;
     const int t0 = c * kC, len = steps_of(z, lengths, n), live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
-    T *out = o + t0 * z.o_t + n * z.o_n + h * z.Dv + col;
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    f32x4 X[4] = {zero, zero, zero, zero}, S[DT];
-    if (live <= 0) return store_rows(l, out, z.o_t, 0, rows, there, X);
+    T *out = o + t0 * z.o_t + n * z.o_n + h * z.Dv;
+    f32x4 X[4] = {}, S[DT];
+    if (live <= 0) return store_rows(l, z, out, z.o_t, 0, rows, col, X);
     const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+    KeyParts<T, DP, NW * 64> keys;
+    keys.load(z, row0, hk, live);
+    Raw raw;
+    load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, col, raw);
     load_state(l, z, states + state_at(z, c, n, h), col, S);
-    load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, X);
-    load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
     if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-    __syncthreads();
+    keys.finish(z, s.K, s.Q, nullptr, nullptr);
+    lds_barrier();
     for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
-    __syncthreads();
+    lds_barrier();
     if (wave < 4) invert_block(l, s.A, wave);
+    values_of<T>(raw, X);
     below_state<DT>(l, s, S, X);
-    __syncthreads();
+    lds_barrier();
     solve(l, s.A, X);
     f32x4 O[4];
     answers<DT>(l, s, S, X, O);
-    store_rows(l, out, z.o_t, live, rows, there, O);
+    settle(O);
+    store_rows(l, z, out, z.o_t, live, rows, col, O);
 }
 
 // ----------------------------------------------------------------------------- backwards
@@ -606,26 +694,38 @@ __global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *_
     const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int l = fresh_lane();
     const int col = (blockIdx.y * NW + wave) * 16 + (l & 15);
-    const bool there = col < z.Dv;
     const int len = steps_of(z, lengths, n);
     const size_t own = state_at(z, 0, n, h);
     f32x4 G[DT];
     load_state(l, z, dh_last ? dh_last + own : nullptr, col, G);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    for (int c = (len + kC - 1) / kC - 1; c >= 0; --c) {
+    KeyParts<T, DP, NW * 64> keys;
+    GateParts<T> gates;
+    Raw raw;
+    auto fetch = [&](int c) {
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
+        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
+        keys.load(z, row0, hk, live);
+        if (wave == 0) gates.load(l, z, row0, h, live);
+        load_rows(l, z, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr, z.o_t, live, col, raw);
+    };
+    const int used = (len + kC - 1) / kC;
+    if (used > 0) fetch(used - 1);
+    for (int c = used - 1; c >= 0; --c) {
         l = fresh_lane();
         const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
         store_state(l, z, ends + state_at(z, c, n, h), col, G);
         if (c == 0 && !dh0) break;
-        const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-        __syncthreads();
-        load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, nullptr, nullptr);
-        if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-        __syncthreads();
+        lds_barrier();
+        keys.finish(z, s.K, s.Q, nullptr, nullptr);
+        if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
         f32x4 dO[4];
-        load_rows(l, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv + col : nullptr, z.o_t, live, there && d_o, dO);
+        values_of<T>(raw, dO);
+        if (c > 0) fetch(c - 1);
+        fence();
+        lds_barrier();
         for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
-        __syncthreads();
+        lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
         f32x4 X[4];
 #pragma unroll
@@ -638,7 +738,7 @@ __global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *_
             for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), dO[i], X[b]);
             fence();
         }
-        __syncthreads();
+        lds_barrier();
         solve_t(l, s.A, X);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -657,6 +757,7 @@ __global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *_
             }
             fence();
         }
+        settle(G);
     }
     if (dh0) store_state(l, z, dh0 + own, col, G);
 }
@@ -666,15 +767,24 @@ __global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *_
 // the columns, each a tile column of dQ and dK and its tiles of dA and dP.
 constexpr int kGradWaves = 8;
 template <int DT> struct GradShared : Shared<DT> {
-    float X[kC * kLA], U[kC * kLA];
+    struct Columns {
+        float X[kC * kLA], U[kC * kLA], O[kC * kLA];
+    };
+    // (after the columns)
+    struct Sums {
+        float row_a[4][kC], col_a[4][kC], row_p[4][kC], col_p[4][kC];       // of the tiles, by their other index
+        float dots[DT][kC], ends[DT][kC];
+        float states[DT];
+    };
+    union {
+        Columns v;
+        Sums t;
+    };
     float inv_k[kC], inv_q[kC];
-    float row_a[4][kC], col_a[4][kC], row_p[4][kC], col_p[4][kC];       // of the tiles, by their other index
-    float dots[DT][kC], ends[DT][kC];
     float xr[4][kC];
-    float states[DT];
 };
 template <typename T, int DT>
-__global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, int vec_do, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
+__global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
                                                                      const float *__restrict__ saved, const T *__restrict__ d_o, const float *__restrict__ ends, T *__restrict__ dgi)
 {
     typedef GradShared<DT> Lds;
@@ -704,16 +814,33 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
         }
         return;
     }
-    load_keys<T, DP, NW * 64>(z, row0, hk, live, s.K, s.Q, s.inv_k, s.inv_q);
+    {
+        KeyParts<T, DP, NW * 64> keys;
+        keys.load(z, row0, hk, live);
+        keys.finish(z, s.K, s.Q, s.inv_k, s.inv_q);
+    }
     // this wavefront's tiles of dQ and dK
     const int dt = wave % DT, rt0 = wave / DT * RT;
+    const bool vec = z.Dv % 4 == 0;
     f32x4 dQ[RT], dK[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) dQ[i] = dK[i] = zero;
     for (int h = hk * group; h < (hk + 1) * group; ++h) {
         anew();
+        const float *S0 = saved + state_at(z, c, n, h), *G0 = ends + state_at(z, c, n, h);
+        const T *do0 = d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr;
+        // 16 columns: v and the state in front for U, the gradients of o and of the state behind for X
+        Raw raw;
+        f32x4 S[DT];
+        auto fetch = [&](int v0) {
+            const int col = v0 + 16 * (wave & 3) + lc;
+            if (wave < 4) load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, col, raw);
+            else load_rows(l, z, do0, z.o_t, live, col, raw);
+            load_state(l, z, wave < 4 ? S0 : G0, col, S);
+        };
+        fetch(0);
         if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-        __syncthreads();
+        lds_barrier();
         f32x4 tile[KEEP], acc[KEEP];
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
@@ -721,11 +848,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             tile[i] = acc[i] = zero;
             if (t < 2 * kTiles) tile[i] = make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
         }
-        __syncthreads();
+        lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
-        __syncthreads();
-        const float *S0 = saved + state_at(z, c, n, h), *G0 = ends + state_at(z, c, n, h);
-        const T *do0 = d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr;
+        lds_barrier();
         f32x4 E1[RT], E2[RT], E3[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) E1[i] = E2[i] = E3[i] = zero;
@@ -733,11 +858,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
         for (int v0 = 0; v0 < z.Dv; v0 += 64) {
             anew();
             const int mine = 16 * (wave & 3) + lc, col = v0 + mine;
-            const bool there = col < z.Dv;
-            f32x4 R[4], X[4], S[DT];
+            f32x4 R[4], X[4];
+            values_of<T>(raw, R);
             if (wave < 4) {
-                load_state(l, z, S0, col, S);
-                load_rows(l, row0 + v_at(z, h) + col, z.gi_t, live, there, R);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     X[b] = zero;
@@ -748,9 +871,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
                     fence();
                 }
                 solve(l, s.A, X);
+                settle(X);
             } else {
-                load_state(l, z, G0, col, S);
-                load_rows(l, do0 ? do0 + col : nullptr, z.o_t, live, there && do0, R);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     X[b] = zero;
@@ -762,20 +884,32 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
                     fence();
                 }
                 solve_t(l, s.A, X);
+                settle(X);
             }
             anew();
-            float *put = (wave < 4 ? s.U : s.X) + g4 * kLA + mine;
+            auto put = [&](float *to, const f32x4 (&x)[4]) {
+                to += g4 * kLA + mine;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) put[(16 * b + r) * kLA] = X[b][r];
-            __syncthreads();
+                    for (int r = 0; r < 4; ++r) to[(16 * b + r) * kLA] = x[b][r];
+            };
+            put(wave < 4 ? s.v.U : s.v.X, X);
+            if (wave >= 4) put(s.v.O, R);
+            // rows of this wavefront's tile column of S and G
+            f32x4 sf[4], gf[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sf[k] = frag_of(l, S0, z.D, 16 * dt, z.Dv, v0 + 16 * k, vec);
+                gf[k] = frag_of(l, G0, z.D, 16 * dt, z.Dv, v0 + 16 * k, vec);
+            }
+            lds_barrier();
             if (wave < 4) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     f32x4 x;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = s.X[(16 * b + g4 + r) * kLA + mine] * R[b][r];
+                    for (int r = 0; r < 4; ++r) x[r] = s.v.X[(16 * b + g4 + r) * kLA + mine] * R[b][r];
                     x = sum_columns(x);
                     if (lc == 0) {
                         f32x4 *p = (f32x4 *)&s.xr[wave][16 * b + g4];
@@ -785,8 +919,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             } else {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) X[b] *= rows_of(l, s.g.beta, 16 * b);
-                store_rows(l, out0 + v_at(z, h) + col, z.gi_t, live, rows, there, X);
+                store_rows(l, z, out0 + v_at(z, h), z.gi_t, live, rows, col, X);
             }
+            if (v0 + 64 < z.Dv) fetch(v0 + 64);
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) {
                 const int t = wave + i * NW;
@@ -794,29 +929,29 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
                 anew();
                 if (t >= 2 * kTiles) break;
                 tile_at(t < kTiles ? t : t - kTiles, bi, bj);
+                const float *left = t < kTiles ? s.v.X : s.v.O;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const f32x4 a = t < kTiles ? frag(l, s.X, kLA, 16 * bi, 16 * k) : do0 ? frag_of(l, do0, z.o_t, 16 * bi, live, v0 + 16 * k, z.Dv, vec_do) : zero;
-                    acc[i] = multiply(a, frag(l, s.U, kLA, 16 * bj, 16 * k), acc[i]);
-                }
+                for (int k = 0; k < 4; ++k) acc[i] = multiply(frag(l, left, kLA, 16 * bi, 16 * k), frag(l, s.v.U, kLA, 16 * bj, 16 * k), acc[i]);
                 fence();
             }
+            anew();
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const bool vec = z.Dv % 4 == 0;
-                anew();
-                const f32x4 sf = frag_of(l, S0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec), gf = frag_of(l, G0, z.Dv, 16 * dt, z.D, v0 + 16 * k, z.Dv, vec);
-                if (rt0 == 0) both += (sf[0] * gf[0] + sf[1] * gf[1]) + (sf[2] * gf[2] + sf[3] * gf[3]);
+                if (rt0 == 0) both += (sf[k][0] * gf[k][0] + sf[k][1] * gf[k][1]) + (sf[k][2] * gf[k][2] + sf[k][3] * gf[k][3]);
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
                     const int b = rt0 + i;
-                    E1[i] = multiply(frag(l, s.X, kLA, 16 * b, 16 * k), sf, E1[i]);
-                    if (do0) E2[i] = multiply(frag_of(l, do0, z.o_t, 16 * b, live, v0 + 16 * k, z.Dv, vec_do), sf, E2[i]);
-                    E3[i] = multiply(frag(l, s.U, kLA, 16 * b, 16 * k), gf, E3[i]);
+                    E1[i] = multiply(frag(l, s.v.X, kLA, 16 * b, 16 * k), sf[k], E1[i]);
+                    E2[i] = multiply(frag(l, s.v.O, kLA, 16 * b, 16 * k), sf[k], E2[i]);
+                    E3[i] = multiply(frag(l, s.v.U, kLA, 16 * b, 16 * k), gf[k], E3[i]);
                 }
                 fence();
             }
-            __syncthreads();
+            settle(acc);
+            settle(E1);
+            settle(E2);
+            settle(E3);
+            lds_barrier();
         }
         // dA and dP, times L, in the place of A and P; the sums of dA A and dP P over rows and columns
 #pragma unroll
@@ -832,9 +967,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             float sum = (by_col[0] + by_col[1]) + (by_col[2] + by_col[3]);
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            if (l < 16) (is_a ? s.col_a : s.col_p)[bi][16 * bj + l] = sum;
+            if (l < 16) (is_a ? s.t.col_a : s.t.col_p)[bi][16 * bj + l] = sum;
             const f32x4 row = sum_columns(by_row);
-            if (lc == 0) *(f32x4 *)&(is_a ? s.row_a : s.row_p)[bj][16 * bi + g4] = row;
+            if (lc == 0) *(f32x4 *)&(is_a ? s.t.row_a : s.t.row_p)[bj][16 * bi + g4] = row;
             store_tile(l, is_a ? s.A : s.P, bi, bj, is_a ? beta * d * L : d * L);
             fence();
         }
@@ -851,8 +986,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             }
             const f32x4 ek = sum_columns(e * k), dot = sum_columns(k1 * k + q1 * q);
             if (lc == 0) {
-                *(f32x4 *)&s.ends[dt][16 * b + g4] = ek;
-                *(f32x4 *)&s.dots[dt][16 * b + g4] = dot;
+                *(f32x4 *)&s.t.ends[dt][16 * b + g4] = ek;
+                *(f32x4 *)&s.t.dots[dt][16 * b + g4] = dot;
             }
             dQ[i] += q1;
             dK[i] += k1 + e;
@@ -861,9 +996,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
         if (rt0 == 0) {
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) both += __shfl_xor(both, o, 64);
-            if (l == 0) s.states[dt] = both;
+            if (l == 0) s.t.states[dt] = both;
         }
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int b = rt0 + i;
@@ -882,14 +1017,16 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
                 fence();
             }
         }
+        settle(dQ);
+        settle(dK);
         if (wave == NW - 1) {           // the gates, a step a lane
             const int b = l >> 4;
             double dc = 0., e = 0., both_all = 0.;
 #pragma unroll
             for (int k = 0; k < DT; ++k) {
-                e += (double)s.ends[k][l];
-                dc += (double)s.dots[k][l];
-                both_all += (double)s.states[k];
+                e += (double)s.t.ends[k][l];
+                dc += (double)s.t.dots[k][l];
+                both_all += (double)s.t.states[k];
             }
             dc -= e;
             float ra = 0.f, xr = (s.xr[0][l] + s.xr[1][l]) + (s.xr[2][l] + s.xr[3][l]);
@@ -897,10 +1034,10 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k <= b) {
-                    ra += s.row_a[k][l];
-                    p += (double)s.row_p[k][l];
+                    ra += s.t.row_a[k][l];
+                    p += (double)s.t.row_p[k][l];
                 }
-                if (k >= b) p -= (double)s.col_a[k][l] + (double)s.col_p[k][l];
+                if (k >= b) p -= (double)s.t.col_a[k][l] + (double)s.t.col_p[k][l];
             }
             const float beta = s.g.beta[l];
             dc += (double)beta * ra + p;
@@ -919,9 +1056,10 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
                 q[b_at(z, h)] = (T)(l < live ? (xr + ra) * beta * s.g.rest_b[l] : 0.f);
             }
         }
-        __syncthreads();
+        lds_barrier();
     }
     // through the lengths: k^ = k / |k|, q^ = q / (sqrt(D) |q|)
+    anew();
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         f32x4 k, q;
@@ -932,11 +1070,11 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
         }
         const f32x4 kk = sum_columns(dK[i] * k), qq = sum_columns(dQ[i] * q);
         if (lc == 0) {
-            *(f32x4 *)&s.ends[dt][16 * (rt0 + i) + g4] = kk;
-            *(f32x4 *)&s.dots[dt][16 * (rt0 + i) + g4] = qq;
+            *(f32x4 *)&s.t.ends[dt][16 * (rt0 + i) + g4] = kk;
+            *(f32x4 *)&s.t.dots[dt][16 * (rt0 + i) + g4] = qq;
         }
     }
-    __syncthreads();
+    lds_barrier();
     const float width = (float)z.D, unit = 1.f / sqrtf(width);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -946,8 +1084,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, in
             float kk = 0.f, qq = 0.f;
 #pragma unroll
             for (int k = 0; k < DT; ++k) {
-                kk += s.ends[k][row];
-                qq += s.dots[k][row];
+                kk += s.t.ends[k][row];
+                qq += s.t.dots[k][row];
             }
             if (row >= rows || d >= z.D) continue;
             T *p = out0 + row * z.gi_t;
@@ -1069,9 +1207,15 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
     // (a launch has fewer than 2^32 threads)
     const long long chunks = ((long long)d.T + kC - 1) / kC;
     if (d.D > kMostWidth || d.Dv > kMostWidth || d.T > 1 << 30 || (long long)d.N * d.H >= 1LL << 22 || chunks * d.N * d.H >= 1LL << 22) return NSK_ERR_UNSUPPORTED;
+    // (a single step's stride says nothing)
+    if (d.T == 1) {
+        d.gi_t = width;
+        d.o_t = (long long)d.H * d.Dv;
+    }
+    if (d.gi_t >= kMostStride || d.o_t >= kMostStride) return NSK_ERR_UNSUPPORTED;
     const int whole = d.dtype == NSK_BF16 ? 8 : 4;
     const bool vec = d.D % whole == 0 && (d.T == 1 || d.gi_t % whole == 0) && (d.N == 1 || d.gi_n % whole == 0);
-    z = {d.T, d.N, d.H, d.Hk, d.D, d.Dv, (int)chunks, vec, d.T == 1 ? 0 : d.gi_t, d.N == 1 ? 0 : d.gi_n, d.T == 1 ? 0 : d.o_t, d.N == 1 ? 0 : d.o_n};
+    z = {d.T, d.N, d.H, d.Hk, d.D, d.Dv, (int)chunks, vec, d.gi_t, d.N == 1 ? 0 : d.gi_n, d.o_t, d.N == 1 ? 0 : d.o_n};
     return NSK_OK;
 }
 // The states (or gradients) of all chunks, and behind them their matrices where the chunks are taken all at once.
@@ -1159,7 +1303,6 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (!workspace || workspace_bytes < align_up(saved_of(z)) + matrices_of(z)) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     float *ends = (float *)workspace, *matrices = (float *)((char *)workspace + align_up(saved_of(z)));
-    const int vec_do = z.Dv % 4 == 0 && z.o_t % 4 == 0 && z.o_n % 4 == 0;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
         return with_sizes(z, [&](auto dt, auto nw) {
@@ -1178,7 +1321,7 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
                 hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,
                                    (const T *)d_o, dh_last, dh0, ends);
             }
-            hipLaunchKernelGGL((delta_grad_kernel<T, DT>), dim3((unsigned)(z.chunks * z.N * z.Hk)), dim3(kGradWaves * 64), grad_bytes, st, z, vec_do, (const T *)gi, bias, lengths, saved,
+            hipLaunchKernelGGL((delta_grad_kernel<T, DT>), dim3((unsigned)(z.chunks * z.N * z.Hk)), dim3(kGradWaves * 64), grad_bytes, st, z, (const T *)gi, bias, lengths, saved,
                                (const T *)d_o, ends, (T *)dgi);
             return check_launch();
         });
