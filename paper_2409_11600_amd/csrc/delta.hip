@@ -89,14 +89,34 @@ template <int N> __device__ __forceinline__ void settle(f32x4 (&x)[N])
     fence();
 }
 __device__ __forceinline__ f32x4 rows_of(int l, const float *v, int row0) { return *(const f32x4 *)(v + row0 + 4 * (l >> 4)); }
-// Sums over the 16 columns of a tile; all lanes have them.
+// Sums over the 16 columns of a tile; all lanes have them: rows of 16 lanes turned by 8, 4, 2 and 1.
+template <int BY> __device__ __forceinline__ float add_turned(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + BY, 0xf, 0xf, true));
+}
 __device__ __forceinline__ f32x4 sum_columns(f32x4 v)
 {
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] += __shfl_xor(v[r], o, 64);
+    for (int r = 0; r < 4; ++r) v[r] = add_turned<1>(add_turned<2>(add_turned<4>(add_turned<8>(v[r]))));
     return v;
+}
+
+// ----------------------------------------------------------------------------- memory
+// Rows are reached through buffer descriptors: what lies at or behind `bytes` reads as zero and is not written, and so is a lane's offset of kNowhere plus anything below 2^31.  An access is
+// a lane's offset plus a uniform one: one instruction, where 64-bit addresses and conditions took six.
+constexpr unsigned kNowhere = 0x80000000u;
+constexpr long long kMostStride = 1LL << 25;       // elements from a step to the next: 16 steps within 2^31 bytes
+template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const T *p, long long bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)bytes, 0x00020000); }
+template <typename T> __device__ __forceinline__ unsigned load_raw(__amdgpu_buffer_rsrc_t b, unsigned at)
+{
+    if constexpr (sizeof(T) == 2) return (unsigned)__builtin_amdgcn_raw_buffer_load_b16(b, at, 0, 0);
+    else return (unsigned)__builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0);
+}
+template <typename T> __device__ __forceinline__ float value_of(unsigned raw) { return __builtin_bit_cast(float, sizeof(T) == 2 ? raw << 16 : raw); }
+template <typename T> __device__ __forceinline__ void store(float v, __amdgpu_buffer_rsrc_t b, unsigned at)
+{
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (T)v), b, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), b, at, 0, 0);
 }
 
 // ----------------------------------------------------------------------------- what a chunk starts with
@@ -108,22 +128,41 @@ struct alignas(16) Gates {
 };
 // By one wavefront, a step a lane.  Steps from `live` on leave the state as it is.
 __device__ __forceinline__ float exp_of(double c) { return __builtin_amdgcn_exp2f((float)c); }
+// c plus the sums of the lanes in front: within 16 lanes, then over the rows of 16.
+template <int CTRL, int ROWS> __device__ __forceinline__ double add_moved(double c)
+{
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, c);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, true), hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, true);
+    return c + __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+__device__ __forceinline__ double sums_up_to(double c)
+{
+    c = add_moved<0x111, 0xf>(c);       // a row moved by 1, 2, 4 and 8 lanes
+    c = add_moved<0x112, 0xf>(c);
+    c = add_moved<0x114, 0xf>(c);
+    c = add_moved<0x118, 0xf>(c);
+    c = add_moved<0x142, 0xa>(c);       // the last lane of a row to the next one (rows 1 and 3), then of the second to the last two
+    return add_moved<0x143, 0xc>(c);
+}
 template <typename T> struct GateParts {
-    float a, b;
+    unsigned a, b;
     __device__ __forceinline__ void load(int i, const Sizes &z, const T *row, int h, int live)
     {
-        a = b = 0.f;
-        if (i >= live) return;
-        const T *p = row + i * z.gi_t;
-        a = (float)p[a_at(z, h)];
-        b = (float)p[b_at(z, h)];
+        const T *p = row + (i < live ? i : 0) * z.gi_t;
+        a = raw_of(p + a_at(z, h));
+        b = raw_of(p + b_at(z, h));
+    }
+    static __device__ __forceinline__ unsigned raw_of(const T *p)
+    {
+        if constexpr (sizeof(T) == 2) return *(const unsigned short *)p;
+        else return *(const unsigned *)p;
     }
     __device__ __forceinline__ void finish(int i, const Sizes &z, const float *bias, int h, int live, Gates &g) const
     {
         double la = 0.;
         float beta = 0.f, rest_a = 0.f, rest_b = 0.f;
         if (i < live) {
-            const float x = a + (bias ? bias[h] : 0.f), y = b + (bias ? bias[z.H + h] : 0.f);
+            const float x = value_of<T>(a) + (bias ? bias[h] : 0.f), y = value_of<T>(b) + (bias ? bias[z.H + h] : 0.f);
             // log sigmoid(x); below -1000 alpha is 0 in any type, and a sum of infinities would have no differences.  Its rounding, 2^-24 of it, is the more the less the product
             // of gates counts: t exp(-t) is at most 0.37.  (NaN stays NaN: fminf of it and 0 would be 0, but not the sum's other part.)
             la = x < -1000.f ? -1000.f : fminf(x, 0.f) - log1pf(expf(-fabsf(x)));
@@ -131,13 +170,10 @@ template <typename T> struct GateParts {
             rest_a = sigmoid(-x);
             rest_b = sigmoid(-y);
         }
-        double c = la * 1.4426950408889634;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const double up = __shfl_up(c, o, 64);
-            if (i >= o) c += up;
-        }
-        const double C = __shfl(c, 63, 64);
+        const double c = sums_up_to(la * 1.4426950408889634);
+        const unsigned long long last = __builtin_bit_cast(unsigned long long, c);
+        const double C = __builtin_bit_cast(double, (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(last >> 32), 63) << 32 |
+                                                        (unsigned)__builtin_amdgcn_readlane((int)(unsigned)last, 63));
         g.c[i] = c;
         g.beta[i] = beta;
         g.in[i] = exp_of(c);
@@ -154,27 +190,46 @@ template <typename T> __device__ __forceinline__ void load_gates(int l, const Si
     p.finish(l, z, bias, h, live, g);
 }
 
-// A row of q or k: kThreads / 64 neighbouring lanes take vectors of 16 bytes in turn.
+// A row of q or k: THREADS / 64 neighbouring lanes take vectors of 16 bytes in turn.  They stay as they were loaded until they are used, so that nothing waits for them before.
 template <typename T, int DP, int THREADS> struct RowPart {
-    static constexpr int LANES = THREADS / 64, V = 16 / sizeof(T), VECTORS = DP / V, EACH = (VECTORS + LANES - 1) / LANES;
-    struct alignas(16) Vec {
-        T v[V];
-    };
-    Vec x[EACH];
-    __device__ __forceinline__ void load(const T *row, int D, bool live, bool vec)
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    static constexpr int LANES = THREADS / 64, V = 16 / sizeof(T), VECTORS = DP / V, EACH = (VECTORS + LANES - 1) / LANES, ROWS = 64 / LANES;     // ROWS: of a wavefront
+    u32x4 x[EACH];
+    // p: the chunk's first row
+    __device__ __forceinline__ void load(int l, int wave, const T *p, long long stride, int D, int live, bool vec)
     {
-        const int p = threadIdx.x % LANES;
+        int left = live - wave * ROWS;
+        left = left < ROWS ? left : ROWS;
+        const __amdgpu_buffer_rsrc_t b = buffer(p + wave * ROWS * stride, left <= 0 ? 0 : ((left - 1) * stride + D) * (long long)sizeof(T));
+        const unsigned at = (unsigned)(l / LANES) * (unsigned)stride * (unsigned)sizeof(T);
+        const int first = l % LANES * V;
+        if (vec) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int e = first + i * LANES * V;
+                x[i] = (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, e < D ? at + e * (unsigned)sizeof(T) : kNowhere, 0, 0);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            x[i] = {};
-            const int e0 = (p + i * LANES) * V;
-            if (!live || e0 >= D) continue;
-            if (vec) x[i] = *(const Vec *)(row + e0);
-            else
+            unsigned raw[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (e0 + e < D) x[i].v[e] = row[e0 + e];
+            for (int k = 0; k < V; ++k) {
+                const int e = first + i * LANES * V + k;
+                raw[k] = load_raw<T>(b, e < D ? at + e * (unsigned)sizeof(T) : kNowhere);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (V == 8) x[i][k] = raw[2 * k] | raw[2 * k + 1] << 16;
+                else x[i][k] = raw[k];
+            }
         }
+    }
+    __device__ __forceinline__ float value(int i, int e) const
+    {
+        const unsigned u = V == 4 ? x[i][e] : e & 1 ? x[i][e / 2] & 0xffff0000u : x[i][e / 2] << 16;
+        return __builtin_bit_cast(float, u);
     }
     // 1 / sqrt(|row|^2 + eps)
     __device__ __forceinline__ float inverse_length() const
@@ -183,21 +238,20 @@ template <typename T, int DP, int THREADS> struct RowPart {
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += (float)x[i].v[e] * (float)x[i].v[e];
-#pragma unroll
-        for (int o = 1; o < LANES; o <<= 1) s += __shfl_xor(s, o, 64);
+            for (int e = 0; e < V; ++e) s = fmaf(value(i, e), value(i, e), s);
+        s += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, s), 0xb1, 0xf, 0xf, true));      // of lane ^ 1
+        s += lane_xor<2>(s);
+        if (LANES == 8) s += lane_xor<4>(s);
         return 1.f / sqrtf(s + kEps);
     }
-    __device__ __forceinline__ void store(float *row, float by) const
+    __device__ __forceinline__ void store(int l, float *row, float by) const
     {
-        const int p = threadIdx.x % LANES;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int v = p + i * LANES;
-            if (v >= VECTORS) continue;
+            const int v = l % LANES + i * LANES;
+            if (VECTORS % LANES && v >= VECTORS) continue;
 #pragma unroll
-            for (int e = 0; e < V; e += 4)
-                *(f32x4 *)(row + v * V + e) = (f32x4){(float)x[i].v[e] * by, (float)x[i].v[e + 1] * by, (float)x[i].v[e + 2] * by, (float)x[i].v[e + 3] * by};
+            for (int e = 0; e < V; e += 4) *(f32x4 *)(row + v * V + e) = (f32x4){value(i, e) * by, value(i, e + 1) * by, value(i, e + 2) * by, value(i, e + 3) * by};
         }
     }
 };
@@ -205,20 +259,18 @@ template <typename T, int DP, int THREADS> struct RowPart {
 template <typename T, int DP, int THREADS> struct KeyParts {
     typedef RowPart<T, DP, THREADS> Part;
     Part k, q;
-    __device__ __forceinline__ void load(const Sizes &z, const T *row0, int hk, int live)
+    __device__ __forceinline__ void load(int l, int wave, const Sizes &z, const T *row0, int hk, int live)
     {
-        const int r = threadIdx.x / Part::LANES;
-        const T *row = row0 + r * z.gi_t;
-        k.load(row + k_at(z, hk), z.D, r < live, z.vec);
-        q.load(row + q_at(z, hk), z.D, r < live, z.vec);
+        k.load(l, wave, row0 + k_at(z, hk), z.gi_t, z.D, live, z.vec);
+        q.load(l, wave, row0 + q_at(z, hk), z.gi_t, z.D, live, z.vec);
     }
-    __device__ __forceinline__ void finish(const Sizes &z, float *K, float *Q, float *inv_k, float *inv_q) const
+    __device__ __forceinline__ void finish(int l, int wave, const Sizes &z, float *K, float *Q, float *inv_k, float *inv_q) const
     {
-        const int r = threadIdx.x / Part::LANES;
+        const int r = wave * Part::ROWS + l / Part::LANES;
         const float ik = k.inverse_length(), iq = q.inverse_length();
-        k.store(K + r * (DP + 4), ik);
-        q.store(Q + r * (DP + 4), iq / sqrtf((float)z.D));
-        if (inv_k && threadIdx.x % Part::LANES == 0) {
+        k.store(l, K + r * (DP + 4), ik);
+        q.store(l, Q + r * (DP + 4), iq / sqrtf((float)z.D));
+        if (inv_k && l % Part::LANES == 0) {
             inv_k[r] = ik;
             inv_q[r] = iq;
         }
@@ -236,17 +288,14 @@ __device__ __forceinline__ void tile_at(int t, int &bi, int &bj)
 __device__ __forceinline__ f32x4 decays(int l, const Gates &g, int bi, int bj, bool strict)
 {
     const int i0 = 16 * bi + 4 * (l >> 4), j = 16 * bj + (l & 15);
+    const double cj = g.c[j];
     f32x4 d;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) d[r] = bi > bj || i0 + r > j || (!strict && i0 + r == j) ? exp_of(g.c[i0 + r] - g.c[j]) : 0.f;
+    for (int r = 0; r < 4; ++r) {
+        const float e = exp_of(g.c[i0 + r] - cj);       // (taken everywhere, without a branch)
+        d[r] = i0 + r > j - !strict ? e : 0.f;
+    }
     return d;
-}
-template <int DP> __device__ __forceinline__ f32x4 dot_tile(int l, const float *X, const float *K, int bi, int bj)
-{
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k0 = 0; k0 < DP; k0 += 16) acc = multiply(frag(l, X, DP + 4, 16 * bi, k0), frag(l, K, DP + 4, 16 * bj, k0), acc);
-    return acc;
 }
 __device__ __forceinline__ void store_tile(int l, float *m, int bi, int bj, f32x4 v)
 {
@@ -254,17 +303,44 @@ __device__ __forceinline__ void store_tile(int l, float *m, int bi, int bj, f32x
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r * kLA] = v[r];
 }
-// -A and P by all wavefronts: tile t of 20, the first ten of A.  Returns the tile without beta (A) or as it is (P).
-template <int DP> __device__ __forceinline__ f32x4 make_tile(int l, int t, const Gates &g, const float *K, const float *Q, float *A, float *P)
+// -A and P by NW wavefronts, the first TILES tiles of 20, of which the first ten are A's: every NW-th tile from this wavefront's number on.  All of a wavefront's tiles go through the products
+// together: one after the other they would wait for LDS four times each.  Returns the tiles without beta (A) or as they are (P), zeros where a wavefront has one less.
+template <int DP, int NW, int TILES, int EACH = (TILES + NW - 1) / NW>
+__device__ __forceinline__ void make_tiles(int l, int wave, const Gates &g, const float *K, const float *Q, float *A, float *P, f32x4 (&x)[EACH])
 {
-    int bi, bj;
-    tile_at(t < kTiles ? t : t - kTiles, bi, bj);
-    f32x4 dot[1] = {dot_tile<DP>(l, t < kTiles ? K : Q, K, bi, bj)};
-    settle(dot);
-    const f32x4 x = decays(l, g, bi, bj, t < kTiles) * dot[0];
-    if (t < kTiles) store_tile(l, A, bi, bj, -rows_of(l, g.beta, 16 * bi) * x);
-    else store_tile(l, P, bi, bj, x);
-    return x;
+    constexpr int LD = DP + 4;
+    int bi[EACH], bj[EACH];
+    const float *left[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int t = wave + i * NW < TILES ? wave + i * NW : TILES - 1;
+        tile_at(t < kTiles ? t : t - kTiles, bi[i], bj[i]);
+        left[i] = t < kTiles ? K : Q;
+        x[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int k0 = 0; k0 < DP; k0 += 16) {
+        f32x4 a[EACH], b[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            a[i] = frag(l, left[i], LD, 16 * bi[i], k0);
+            b[i] = frag(l, K, LD, 16 * bj[i], k0);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) x[i] = mfma(a[i][s], b[i][s], x[i]);
+    }
+    settle(x);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int t = wave + i * NW;
+        const bool is_a = t < kTiles;
+        x[i] *= decays(l, g, bi[i], bj[i], is_a);
+        const f32x4 by = -rows_of(l, g.beta, 16 * bi[i]);
+        if (t >= TILES) x[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        else store_tile(l, is_a ? A : P, bi[i], bj[i], is_a ? by * x[i] : x[i]);
+    }
 }
 // The inverse of a diagonal block of 1 + A, in its place: wavefront w takes block w, each lane a column (the four groups of 16 lanes the same).
 __device__ __forceinline__ void invert_block(int l, float *A, int w)
@@ -296,7 +372,6 @@ __device__ __forceinline__ void solve(int l, const float *A, f32x4 (&X)[4])
 #pragma unroll
         for (int j = 0; j < b; ++j) X[b] = multiply(frag(l, A, kLA, 16 * b, 16 * j), X[j], X[b]);
         X[b] = multiply(frag(l, A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
-        fence();
     }
 }
 __device__ __forceinline__ void solve_t(int l, const float *A, f32x4 (&X)[4])
@@ -306,25 +381,7 @@ __device__ __forceinline__ void solve_t(int l, const float *A, f32x4 (&X)[4])
 #pragma unroll
         for (int j = 3; j > b; --j) X[b] = multiply(frag_t(l, A, kLA, 16 * b, 16 * j), X[j], X[b]);
         X[b] = multiply(frag_t(l, A, kLA, 16 * b, 16 * b), X[b], (f32x4){0.f, 0.f, 0.f, 0.f});
-        fence();
     }
-}
-
-// Rows are reached through buffer descriptors: what lies at or behind `bytes` reads as zero and is not written, and so is a lane's offset of kNowhere plus anything below 2^31.  An access is
-// a lane's offset plus a uniform one: one instruction, where 64-bit addresses and conditions took six.
-constexpr unsigned kNowhere = 0x80000000u;
-constexpr long long kMostStride = 1LL << 25;       // elements from a step to the next: 16 steps within 2^31 bytes
-template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const T *p, long long bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)bytes, 0x00020000); }
-template <typename T> __device__ __forceinline__ unsigned load_raw(__amdgpu_buffer_rsrc_t b, unsigned at)
-{
-    if constexpr (sizeof(T) == 2) return (unsigned)__builtin_amdgcn_raw_buffer_load_b16(b, at, 0, 0);
-    else return (unsigned)__builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0);
-}
-template <typename T> __device__ __forceinline__ float value_of(unsigned raw) { return __builtin_bit_cast(float, sizeof(T) == 2 ? raw << 16 : raw); }
-template <typename T> __device__ __forceinline__ void store(float v, __amdgpu_buffer_rsrc_t b, unsigned at)
-{
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (T)v), b, at, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), b, at, 0, 0);
 }
 
 // 16 columns of a state [D,Dv] in registers.
@@ -431,7 +488,8 @@ template <int DT> __device__ __forceinline__ void answers(int l, const Shared<DT
 // ----------------------------------------------------------------------------- all steps
 // A block takes the columns of a state that its wavefronts hold, 16 each, through all chunks.
 template <typename T, int DT, int NW>
-__global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
+
+__global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
                                                             T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
 {
     typedef Shared<DT> Lds;
@@ -452,7 +510,7 @@ __global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__
     auto fetch = [&](int c) {
         const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
         const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-        keys.load(z, row0, hk, live);
+        keys.load(l, wave, z, row0, hk, live);
         if (wave == 0) gates.load(l, z, row0, h, live);
         load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, col, v);
     };
@@ -468,13 +526,16 @@ __global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__
             continue;
         }
         lds_barrier();
-        keys.finish(z, s.K, s.Q, nullptr, nullptr);
+        keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
         if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
         values_of<T>(v, X);
         if (t0 + kC < len) fetch(c + 1);
         fence();
         lds_barrier();
-        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+        {
+            f32x4 tiles[(2 * kTiles + NW - 1) / NW];
+            make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+        }
         lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
         below_state<DT>(l, s, S, X);
@@ -493,7 +554,7 @@ __global__ __launch_bounds__(NW * 64) void delta_fwd_kernel(Sizes z, const T *__
             S[k] *= all;
 #pragma unroll
             for (int b = 0; b < 4; ++b) S[k] = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], S[k]);
-            fence();
+            if (k & 1) fence();
         }
         settle(S);
     }
@@ -523,15 +584,19 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
     const int col = (unit ? tile : tile - units) * 16 + lc;
     const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
     KeyParts<T, DP, NW * 64> keys;
-    keys.load(z, row0, hk, live);
+    keys.load(l, wave, z, row0, hk, live);
     Raw raw;
     if (BACK) load_rows(l, z, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr, z.o_t, live, unit ? z.Dv : col, raw);
     else load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, unit ? z.Dv : col, raw);
     if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-    keys.finish(z, s.K, s.Q, nullptr, nullptr);
+    keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     lds_barrier();
-    for (int t = wave; t < (BACK ? 2 : 1) * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+    {
+        constexpr int TILES = (BACK ? 2 : 1) * kTiles;
+        f32x4 tiles[(TILES + NW - 1) / NW];
+        make_tiles<DP, NW, TILES>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+    }
     lds_barrier();
     if (wave < 4) invert_block(l, s.A, wave);
     lds_barrier();
@@ -661,14 +726,17 @@ __global__ __launch_bounds__(NW * 64) void delta_out_kernel(Sizes z, const T *__
     if (live <= 0) return store_rows(l, z, out, z.o_t, 0, rows, col, X);
     const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
     KeyParts<T, DP, NW * 64> keys;
-    keys.load(z, row0, hk, live);
+    keys.load(l, wave, z, row0, hk, live);
     Raw raw;
     load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, col, raw);
     load_state(l, z, states + state_at(z, c, n, h), col, S);
     if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-    keys.finish(z, s.K, s.Q, nullptr, nullptr);
+    keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
     lds_barrier();
-    for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+    {
+        f32x4 tiles[(2 * kTiles + NW - 1) / NW];
+        make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+    }
     lds_barrier();
     if (wave < 4) invert_block(l, s.A, wave);
     values_of<T>(raw, X);
@@ -684,7 +752,7 @@ __global__ __launch_bounds__(NW * 64) void delta_out_kernel(Sizes z, const T *__
 // ----------------------------------------------------------------------------- backwards
 // The gradients of the states that leave the chunks, from the last to the first, and of the initial state.
 template <typename T, int DT, int NW>
-__global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
+__global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
                                                              const float *__restrict__ dh_last, float *__restrict__ dh0, float *__restrict__ ends)
 {
     typedef Shared<DT> Lds;
@@ -705,7 +773,7 @@ __global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *_
     auto fetch = [&](int c) {
         const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC;
         const T *row0 = gi + t0 * z.gi_t + n * z.gi_n;
-        keys.load(z, row0, hk, live);
+        keys.load(l, wave, z, row0, hk, live);
         if (wave == 0) gates.load(l, z, row0, h, live);
         load_rows(l, z, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr, z.o_t, live, col, raw);
     };
@@ -717,14 +785,17 @@ __global__ __launch_bounds__(NW * 64) void delta_ends_kernel(Sizes z, const T *_
         store_state(l, z, ends + state_at(z, c, n, h), col, G);
         if (c == 0 && !dh0) break;
         lds_barrier();
-        keys.finish(z, s.K, s.Q, nullptr, nullptr);
+        keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
         if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
         f32x4 dO[4];
         values_of<T>(raw, dO);
         if (c > 0) fetch(c - 1);
         fence();
         lds_barrier();
-        for (int t = wave; t < 2 * kTiles; t += NW) make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
+        {
+            f32x4 tiles[(2 * kTiles + NW - 1) / NW];
+            make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+        }
         lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
         f32x4 X[4];
@@ -816,8 +887,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
     }
     {
         KeyParts<T, DP, NW * 64> keys;
-        keys.load(z, row0, hk, live);
-        keys.finish(z, s.K, s.Q, s.inv_k, s.inv_q);
+        keys.load(l, wave, z, row0, hk, live);
+        keys.finish(l, wave, z, s.K, s.Q, s.inv_k, s.inv_q);
     }
     // this wavefront's tiles of dQ and dK
     const int dt = wave % DT, rt0 = wave / DT * RT;
@@ -842,15 +913,11 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
         if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
         lds_barrier();
         f32x4 tile[KEEP], acc[KEEP];
+        make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tile);
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) {
-            const int t = wave + i * NW;
-            tile[i] = acc[i] = zero;
-            if (t < 2 * kTiles) tile[i] = make_tile<DP>(l, t, s.g, s.K, s.Q, s.A, s.P);
-        }
+        for (int i = 0; i < KEEP; ++i) acc[i] = zero;
         lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
-        lds_barrier();
         f32x4 E1[RT], E2[RT], E3[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) E1[i] = E2[i] = E3[i] = zero;
@@ -870,8 +937,6 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
                     X[b] = rows_of(l, s.g.beta, 16 * b) * R[b];
                     fence();
                 }
-                solve(l, s.A, X);
-                settle(X);
             } else {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
@@ -883,6 +948,14 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
                     for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), R[i], X[b]);
                     fence();
                 }
+                settle(X);
+            }
+            if (v0 == 0) lds_barrier();         // (the inverses)
+            anew();
+            if (wave < 4) {
+                solve(l, s.A, X);
+                settle(X);
+            } else {
                 solve_t(l, s.A, X);
                 settle(X);
             }
@@ -1014,7 +1087,6 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
                     dK[i] = multiply(frag_t(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
                     dK[i] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), frag_t(l, s.Q, LD, 16 * dt, 16 * j), dK[i]);
                 }
-                fence();
             }
         }
         settle(dQ);
