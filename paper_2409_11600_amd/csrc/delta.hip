@@ -44,7 +44,7 @@ __device__ __forceinline__ int steps_of(const Sizes &z, const int *lengths, int 
     const int l = lengths ? lengths[n] : z.T;
     return l < 0 ? 0 : l < z.T ? l : z.T;
 }
-__device__ __forceinline__ size_t state_at(const Sizes &z, int chunk, int n, int h) { return (((size_t)chunk * z.N + n) * z.H + h) * z.D * z.Dv; }
+__host__ __device__ __forceinline__ size_t state_at(const Sizes &z, int chunk, int n, int h) { return (((size_t)chunk * z.N + n) * z.H + h) * z.D * z.Dv; }
 
 __device__ __forceinline__ float sigmoid(float a)
 {
@@ -564,7 +564,7 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T 
 // ----------------------------------------------------------------------------- all chunks at once
 // A chunk takes S to M S + B, and the gradient behind it to M^T G + B'.  Where heads are few, the chunks' M and B are made beside each other (the products above for a state of
 // D + Dv columns, the unit matrix and zeros), then a small product a chunk goes through the sequence, and then everything else is done for all chunks beside each other.
-__host__ __device__ inline size_t matrices_at(const Sizes &z, int chunk, int n, int h) { return (((size_t)chunk * z.N + n) * z.H + h) * z.D * (z.D + z.Dv); }
+__host__ __device__ __forceinline__ size_t matrices_at(const Sizes &z, int chunk, int n, int h) { return (((size_t)chunk * z.N + n) * z.H + h) * z.D * (z.D + z.Dv); }
 
 template <typename T, int DT, int NW, bool BACK>
 __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
@@ -650,60 +650,80 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
     }
 }
 
-// States in front of the chunks (BACK: gradients behind them) to `states`, and the last one to `last`.  A block takes 16 columns of a state, a wavefront 16 rows; the state goes round
-// through LDS, a column in a row.  What the next chunk needs is on its way meanwhile.
-template <int DT, bool BACK>
+// States in front of the chunks (BACK: gradients behind them, from the last chunk on) to `states`, and the last one to `last`.  A block takes 16 columns of a state, a wavefront 16
+// rows; the state goes round through LDS, a column in a row.  What the next chunk needs is on its way meanwhile.
+// A chunk takes 2 us, which nothing hides where the blocks are few and the sequence long.  Then it is cut into segments (blockIdx.z): Compose makes the M and B of each, the columns of the
+// unit matrix and of no state; Jump goes from segment to segment; Fill goes through each from the state that enters it.
+enum class Scan { Whole, Compose, Jump, Fill };
+template <int DT, bool BACK, Scan MODE>
 __global__ __launch_bounds__(DT * 64) void delta_scan_kernel(Sizes z, const int *__restrict__ lengths, const float *__restrict__ matrices, const float *__restrict__ first,
-                                                             float *__restrict__ states, float *__restrict__ last)
+                                                             float *__restrict__ states, float *__restrict__ last, int segment)
 {
     constexpr int DP = 16 * DT, LD = DP + 4;
     __shared__ __attribute__((aligned(16))) float lds[2][16 * LD];
     const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = fresh_lane(), lc = l & 15, g4 = 4 * (l >> 4);
-    const int col = blockIdx.y * 16 + lc, row = 16 * wave + g4, len = steps_of(z, lengths, n), used = (len + kC - 1) / kC;
-    const bool vec = z.D % 4 == 0;
+    const int units = (z.D + 15) / 16, tile = blockIdx.y, len = steps_of(z, lengths, n), used = (len + kC - 1) / kC;
+    const bool vec = z.D % 4 == 0, unit = MODE == Scan::Compose && tile < units;
+    const int col = (MODE == Scan::Compose && !unit ? tile - units : tile) * 16 + lc, row = 16 * wave + g4, width = unit ? z.D : z.Dv;
+    // the items of the sequence (chunks, or segments) that this block goes through
+    const int items = MODE == Scan::Jump ? (used + segment - 1) / segment : used, number = (MODE == Scan::Compose || MODE == Scan::Fill) ? blockIdx.z : 0;
+    const int from = number * segment * (MODE == Scan::Compose || MODE == Scan::Fill), to = MODE == Scan::Compose || MODE == Scan::Fill ? (items - from < segment ? items : from + segment) : items;
+    const bool ends = to >= items;
+    if (from >= items && (MODE == Scan::Compose || from > 0)) return;
+    if (MODE == Scan::Compose && ends) return;          // (nothing comes behind it)
     const size_t own = state_at(z, 0, n, h);
     f32x4 S;
     struct Chunk {
         f32x4 M[DT], B;
     };
     Chunk chunk[2];
-    const unsigned at = col < z.Dv ? (unsigned)(row * z.Dv + col) * 4 : kNowhere;
+    const unsigned at = col < width ? (unsigned)(row * width + col) * 4 : kNowhere;
     auto get = [&](const float *p, f32x4 &x) {
-        const __amdgpu_buffer_rsrc_t b = buffer(p, p ? z.D * z.Dv * 4 : 0);
+        const __amdgpu_buffer_rsrc_t b = buffer(p, p ? z.D * width * 4 : 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = value_of<float>(load_raw<float>(b, at + r * z.Dv * 4));
+        for (int r = 0; r < 4; ++r) x[r] = value_of<float>(load_raw<float>(b, at + r * width * 4));
     };
     auto put = [&](float *p) {
-        const __amdgpu_buffer_rsrc_t b = buffer(p, z.D * z.Dv * 4);
+        const __amdgpu_buffer_rsrc_t b = buffer(p, z.D * width * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) store<float>(S[r], b, at + r * z.Dv * 4);
+        for (int r = 0; r < 4; ++r) store<float>(S[r], b, at + r * width * 4);
     };
+    auto item = [&](int i) { return BACK && MODE != Scan::Jump ? used - 1 - i : i; };
     auto fetch = [&](int i, Chunk &x) {
-        const float *m = matrices + matrices_at(z, BACK ? used - 1 - i : i, n, h);
+        const float *m = matrices + matrices_at(z, item(i), n, h);
 #pragma unroll
         for (int k = 0; k < DT; ++k) x.M[k] = frag_of(l, m, z.D, 16 * wave, z.D, 16 * k, vec);
-        get(m + (size_t)z.D * z.D, x.B);
+        get(unit ? nullptr : m + (size_t)z.D * z.D, x.B);
     };
-    get(first ? first + own : nullptr, S);
-    const int steps = last ? used : used - 1;       // products: the one behind the last state only if that is wanted
+    if (MODE == Scan::Compose) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[r] = unit && row + r == col ? 1.f : 0.f;
+    } else {
+        get(MODE == Scan::Fill ? first + state_at(z, number, n, h) : first ? first + own : nullptr, S);
+    }
+    // the last product only if what it makes is wanted
+    const int stop = MODE == Scan::Compose || (ends && last) ? to : to - 1;
     auto step = [&](int i, const Chunk &now, Chunk &next) {
-        put(states + state_at(z, BACK ? used - 1 - i : i, n, h));
-        if (i >= steps) return;
-        if (i + 1 < steps) fetch(i + 1, next);
-        float *to = lds[i & 1];
-        *(f32x4 *)(to + lc * LD + row) = S;
+        if (MODE != Scan::Compose) put(states + state_at(z, item(i), n, h));
+        if (i >= stop) return;
+        if (i + 1 < stop) fetch(i + 1, next);
+        float *to_lds = lds[i & 1];
+        *(f32x4 *)(to_lds + lc * LD + row) = S;
         lds_barrier();
         f32x4 acc[2] = {now.B, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int k = 0; k < DT; ++k) acc[k & 1] = multiply(now.M[k], *(const f32x4 *)(to + lc * LD + 16 * k + g4), acc[k & 1]);
+        for (int k = 0; k < DT; ++k) acc[k & 1] = multiply(now.M[k], *(const f32x4 *)(to_lds + lc * LD + 16 * k + g4), acc[k & 1]);
         settle(acc);
         S = acc[0] + acc[1];
     };
-    if (steps > 0) fetch(0, chunk[0]);
-    for (int i = 0; i < used; i += 2) {
+    if (stop > from) fetch(from, chunk[0]);
+    for (int i = from; i < to; i += 2) {
         step(i, chunk[0], chunk[1]);
-        if (i + 1 < used) step(i + 1, chunk[1], chunk[0]);
+        if (i + 1 < to) step(i + 1, chunk[1], chunk[0]);
     }
+    if (MODE == Scan::Compose) return put(states + matrices_at(z, number, n, h) + (unit ? 0 : (size_t)z.D * z.D));
+    if (MODE == Scan::Jump && items == 0) put(states + state_at(z, 0, n, h));        // (a sequence of no step: what enters it leaves it)
+    if (MODE == Scan::Jump || !ends) return;
     if (!BACK)
         for (int c = used; c < z.chunks; ++c) put(states + state_at(z, c, n, h));
     if (last) put(last + own);
@@ -1290,9 +1310,41 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
     z = {d.T, d.N, d.H, d.Hk, d.D, d.Dv, (int)chunks, vec, d.gi_t, d.N == 1 ? 0 : d.gi_n, d.o_t, d.N == 1 ? 0 : d.o_n};
     return NSK_OK;
 }
-// The states (or gradients) of all chunks, and behind them their matrices where the chunks are taken all at once.
+// The workspace: the states (or gradients) of all chunks; where the chunks are taken all at once their matrices; where the sequence is cut into segments theirs, and the states between them.
 bool at_once(const Sizes &z) { return z.chunks > 2 && (long long)z.N * z.H < 192; }
-size_t matrices_of(const Sizes &z) { return at_once(z) ? matrices_at(z, z.chunks, 0, 0) * sizeof(float) : 0; }
+int segment_of(const Sizes &z) { return z.chunks >= 48 && (long long)z.N * z.H * ceil_div(z.Dv, 16) <= 256 ? z.chunks > 512 ? 32 : 16 : 0; }
+size_t saved_of(const Sizes &z);
+struct Plan {
+    int segment, segments;
+    size_t matrices, composed, between, bytes;
+};
+Plan plan_of(const Sizes &z, bool states)
+{
+    Plan p{};
+    const bool all = at_once(z);
+    p.segment = all ? segment_of(z) : 0;
+    p.segments = p.segment ? ceil_div(z.chunks, p.segment) : 0;
+    p.matrices = states || all ? align_up(saved_of(z)) : 0;
+    p.composed = p.matrices + (all ? align_up(matrices_at(z, z.chunks, 0, 0) * sizeof(float)) : 0);
+    p.between = p.composed + align_up(matrices_at(z, p.segments, 0, 0) * sizeof(float));
+    p.bytes = p.between + align_up(state_at(z, p.segments, 0, 0) * sizeof(float));
+    return p;
+}
+template <int DT, bool BACK> void scan(const Sizes &z, const Plan &p, const int *lengths, char *workspace, const float *first, float *states, float *last, hipStream_t st)
+{
+    const float *matrices = (const float *)(workspace + p.matrices);
+    const unsigned heads = (unsigned)(z.N * z.H), columns = (unsigned)ceil_div(z.Dv, 16), both = columns + (unsigned)ceil_div(z.D, 16);
+    const dim3 block(DT * 64);
+    if (!p.segment) {
+        hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Whole>), dim3(heads, columns), block, 0, st, z, lengths, matrices, first, states, last, 0);
+        return;
+    }
+    float *composed = (float *)(workspace + p.composed), *between = (float *)(workspace + p.between);
+    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Compose>), dim3(heads, both, (unsigned)p.segments), block, 0, st, z, lengths, matrices, (const float *)nullptr, composed,
+                       (float *)nullptr, p.segment);
+    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Jump>), dim3(heads, columns), block, 0, st, z, lengths, composed, first, between, (float *)nullptr, p.segment);
+    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Fill>), dim3(heads, columns, (unsigned)p.segments), block, 0, st, z, lengths, matrices, between, states, last, p.segment);
+}
 size_t saved_of(const Sizes &z) { return (size_t)z.chunks * z.N * z.H * z.D * z.Dv * sizeof(float); }
 
 // A call with the tiles of D and the wavefronts' columns as constants.
@@ -1321,7 +1373,7 @@ size_t nsk_delta_workspace_bytes(const nsk_delta_desc_t *desc, int pass)
 {
     Sizes z;
     if ((pass != NSK_PASS_FWD && pass != NSK_PASS_DGRAD) || check(desc, z) != NSK_OK) return 0;
-    return pass == NSK_PASS_DGRAD || at_once(z) ? align_up(saved_of(z)) + matrices_of(z) : 0;
+    return plan_of(z, pass == NSK_PASS_DGRAD).bytes;
 }
 
 int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0, void *o, float *h_last, float *saved, void *workspace,
@@ -1333,9 +1385,10 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (!gi || (!o && !h_last)) return NSK_ERR_NULL;
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(h0) || unaligned16(o) || unaligned16(h_last) || unaligned16(saved) || unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    if (at_once(z) && (!workspace || workspace_bytes < align_up(saved_of(z)) + matrices_of(z))) return NSK_ERR_WORKSPACE;
+    const Plan p = plan_of(z, false);
+    if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    float *matrices = (float *)((char *)workspace + align_up(saved_of(z))), *states = saved ? saved : (float *)workspace;
+    float *matrices = (float *)((char *)workspace + p.matrices), *states = saved ? saved : (float *)workspace;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
         return with_sizes(z, [&](auto dt, auto nw) {
@@ -1349,7 +1402,7 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
                 const unsigned all = (unsigned)(z.chunks * z.N * z.H);
                 hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, false>), dim3(all, (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)), dim3(NW * 64), bytes, st, z,
                                    (const T *)gi, bias, lengths, (const T *)nullptr, matrices);
-                hipLaunchKernelGGL((delta_scan_kernel<DT, false>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16)), dim3(DT * 64), 0, st, z, lengths, matrices, h0, states, h_last);
+                scan<DT, false>(z, p, lengths, (char *)workspace, h0, states, h_last, st);
                 if (o)
                     hipLaunchKernelGGL((delta_out_kernel<T, DT, NW>), dim3(all, (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, states, (T *)o);
                 return check_launch();
@@ -1372,9 +1425,10 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(saved) || unaligned16(d_o) || unaligned16(dh_last) || unaligned16(dgi) || unaligned16(dh0) ||
         unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    if (!workspace || workspace_bytes < align_up(saved_of(z)) + matrices_of(z)) return NSK_ERR_WORKSPACE;
+    const Plan p = plan_of(z, true);
+    if (!workspace || workspace_bytes < p.bytes) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    float *ends = (float *)workspace, *matrices = (float *)((char *)workspace + align_up(saved_of(z)));
+    float *ends = (float *)workspace, *matrices = (float *)((char *)workspace + p.matrices);
     auto launch = [&](auto one) {
         typedef decltype(one) T;
         return with_sizes(z, [&](auto dt, auto nw) {
@@ -1388,7 +1442,7 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             if (at_once(z)) {
                 hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, true>), dim3((unsigned)(z.chunks * z.N * z.H), (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)),
                                    dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, (const T *)d_o, matrices);
-                hipLaunchKernelGGL((delta_scan_kernel<DT, true>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16)), dim3(DT * 64), 0, st, z, lengths, matrices, dh_last, ends, dh0);
+                scan<DT, true>(z, p, lengths, (char *)workspace, dh_last, ends, dh0, st);
             } else {
                 hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,
                                    (const T *)d_o, dh_last, dh0, ends);

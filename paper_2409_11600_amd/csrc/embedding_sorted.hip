@@ -64,46 +64,32 @@ __device__ __forceinline__ void fill(float *table, size_t elements, unsigned blo
 
 // Keys are compared as unsigned numbers, so what is no token (negative, or V and more) comes behind all tokens.
 
-// Few positions: the place of one is the number of those in front of it, counted by comparing it with all.  A block has 64 positions; its wavefronts share
-// the others, whose keys are the same for all lanes: scalar loads, and two vector instructions a comparison.
-constexpr int kRankWaves = 16, kRankMost = 16384;
-__global__ __launch_bounds__(kRankWaves * 64) void rank_kernel(const unsigned *__restrict__ tokens, int n, unsigned *__restrict__ keys, int *__restrict__ order, unsigned ranking, float *table,
-                                                               size_t elements)
-{
-    if (blockIdx.x >= ranking) return fill(table, elements, blockIdx.x - ranking, gridDim.x - ranking);
-    __shared__ int counts[kRankWaves][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int base = blockIdx.x * 64, i = base + lane;
-    const unsigned mine = i < n ? tokens[i] : 0;
-    const int each = (n + kRankWaves - 1) / kRankWaves, from = wave * each, to = n - from < each ? n : from + each;
-    int count = 0;
-    // in front of the block's positions an equal key comes first, behind them it does not
-    const int before = to < base ? to : base, after = from > base + 64 ? from : base + 64;
-#pragma unroll 16
-    for (int j = from; j < before; ++j) count += tokens[j] <= mine;
-    for (int j = from > base ? from : base; j < to && j < base + 64; ++j) {
-        const unsigned k = tokens[j];
-        count += k < mine || (k == mine && j < i);
-    }
-#pragma unroll 16
-    for (int j = after; j < to; ++j) count += tokens[j] < mine;
-    counts[wave][lane] = count;
-    __syncthreads();
-    if (wave || i >= n) return;
-    int place = 0;
-#pragma unroll
-    for (int w = 0; w < kRankWaves; ++w) place += counts[w][lane];
-    keys[place] = mine;
-    order[place] = i;
-}
-
-// Many positions: passes over digits of the key, the lowest first, each stable.  A block takes kTile positions, each of its wavefronts a quarter of them in order.
-constexpr int kBits = 9, kDigits = 1 << kBits, kTile = 4096, kWaves = kThreads / 64;
+// Passes over digits of the key, the lowest first, each stable.  A block takes kTile positions, each of its wavefronts a quarter of them in order.
+constexpr int kBits = 9, kDigits = 1 << kBits, kTile = 1024, kWaves = kThreads / 64;
 __device__ __forceinline__ int digit_of(unsigned key, int shift) { return (int)(key >> shift) & (kDigits - 1); }
+// Where this lane's position goes, in order of the lanes of equal digits; `next`: the wavefront's next place of each digit.
+__device__ __forceinline__ int place_of(int digit, bool there, int *next)
+{
+    unsigned long long same = __ballot(there);
+#pragma unroll
+    for (int b = 0; b < kBits; ++b) {
+        const unsigned long long set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+    }
+    const int rank = lanes_below(same);
+    int at = 0;
+    if (there) at = next[digit] + rank;
+    __builtin_amdgcn_wave_barrier();
+    if (there && rank == 0) next[digit] = at + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    return at;
+}
 // (What is no token is V here: as few digits as there can be.)
 __device__ __forceinline__ unsigned key_at(const unsigned *from, int i, unsigned V) { return from[i] < V ? from[i] : V; }
-__global__ __launch_bounds__(kThreads) void digits_kernel(const unsigned *__restrict__ from, int n, unsigned V, int shift, int tiles, int *__restrict__ counts, float *table, size_t elements)
+__global__ __launch_bounds__(kThreads) void digits_kernel(const unsigned *__restrict__ from, int n, unsigned V, int shift, int tiles, int *__restrict__ counts, float *table, size_t elements,
+                                                        int *__restrict__ list)
 {
+    if (blockIdx.x == 0 && threadIdx.x == 0) list[0] = 0;
     if ((int)blockIdx.x >= tiles) return fill(table, elements, blockIdx.x - tiles, gridDim.x - tiles);
     __shared__ int found[kDigits];
     for (int d = threadIdx.x; d < kDigits; d += kThreads) found[d] = 0;
@@ -173,20 +159,8 @@ __global__ __launch_bounds__(kThreads) void scatter_kernel(const unsigned *__res
     for (int r = 0; r < kTile / kThreads; ++r) {
         const int i = base + r * 64 + lane;
         const bool there = i < n;
-        const int d = there ? digit_of(key[r], shift) : 0;
-        unsigned long long same = __ballot(there);
-        if (!same) break;
-#pragma unroll
-        for (int b = 0; b < kBits; ++b) {
-            const unsigned long long set = __ballot((d >> b) & 1);
-            same &= (d >> b) & 1 ? set : ~set;
-        }
-        const int rank = lanes_below(same);
-        int at = 0;
-        if (there) at = next[wave][d] + rank;
-        __builtin_amdgcn_wave_barrier();
-        if (there && rank == 0) next[wave][d] = at + __popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        if (!__ballot(there)) break;
+        const int at = place_of(digit_of(key[r], shift), there, next[wave]);
         if (there) {
             keys[at] = key[r];
             order[at] = from_order ? from_order[i] : i;
@@ -194,9 +168,78 @@ __global__ __launch_bounds__(kThreads) void scatter_kernel(const unsigned *__res
     }
 }
 
+// Few positions: the place of one is the number of those in front of it, counted by comparing it with all, in one launch (six launches of the kernels above wait for each other longer than they
+// work; all passes in one block of 16 wavefronts took 29 us for 10000 positions).  A block has 64 positions; its wavefronts share the others, whose keys are the same for all
+// lanes: scalar loads.  A comparison is min(a - b, 1) without wrapping, two keys at a time where they have 16 bits: three vector instructions a pair, which is what bounds it.
+constexpr int kRankWaves = 16, kFew = 16384;
+template <bool NARROW>
+__global__ __launch_bounds__(kRankWaves * 64) void rank_kernel(const unsigned *__restrict__ tokens, int n, unsigned V, unsigned *__restrict__ keys, int *__restrict__ order, unsigned ranking,
+                                                               float *table, size_t elements, int *__restrict__ list)
+{
+    if (blockIdx.x == 0 && threadIdx.x == 0) list[0] = 0;
+    if (blockIdx.x >= ranking) return fill(table, elements, blockIdx.x - ranking, gridDim.x - ranking);
+    typedef unsigned u32x16 __attribute__((ext_vector_type(16), aligned(4)));
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    __shared__ int counts[kRankWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int base = blockIdx.x * 64, i = base + lane;
+    const unsigned mine = i < n ? key_at(tokens, i, V) : 0;
+    const int groups = n / 64, each = (groups + kRankWaves - 1) / kRankWaves, first = wave * each, last = groups - first < each ? groups : first + each;
+    int count = 0;
+    // whole groups of 64 keys: in front of the block's positions equal keys come first, behind them they do not.  (The subtractions are written out: of min(a - b, 1) the compiler makes a
+    // comparison, a selection and a wait between them, four times as long.)
+    auto below = [&](int from, int to, unsigned border) {
+        unsigned pair = 0;
+        const unsigned borders = border | border << 16;
+        for (int g = from; g < to; ++g) {
+            u32x16 k[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) k[q] = *(const u32x16 *)(tokens + 64 * g + 16 * q);
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) {
+                const unsigned x = k[e / 16][e % 16], y = k[e / 16][e % 16 + 1], a = x < V ? x : V, b = y < V ? y : V;
+                if constexpr (NARROW) {
+                    unsigned over;
+                    asm("v_pk_sub_u16 %0, %1, %2 clamp" : "=v"(over) : "v"(borders), "s"(a | b << 16));
+                    asm("v_pk_min_u16 %0, %1, %2" : "=v"(over) : "v"(over), "s"(0x00010001));
+                    pair = __builtin_bit_cast(unsigned, __builtin_bit_cast(u16x2, pair) + __builtin_bit_cast(u16x2, over));
+                } else {
+                    unsigned over[2];
+                    asm("v_sub_u32 %0, %1, %2 clamp" : "=v"(over[0]) : "v"(border), "s"(a));
+                    asm("v_sub_u32 %0, %1, %2 clamp" : "=v"(over[1]) : "v"(border), "s"(b));
+                    count += (over[0] < 1u ? over[0] : 1u) + (over[1] < 1u ? over[1] : 1u);
+                }
+            }
+        }
+        count += (pair & 0xffff) + (pair >> 16);
+    };
+    const int own = blockIdx.x;
+    auto least = [](int a, int b) { return a < b ? a : b; };
+    auto most = [](int a, int b) { return a > b ? a : b; };
+    below(first, least(last, own), mine + 1);
+    below(most(first, own + 1), last, mine);
+    // the block's own positions, and those behind the last whole group: a key a lane
+    if (wave < 2) {
+        const int at = wave ? 64 * groups : base, there = wave ? n - at : own < groups ? 64 : 0;
+        const unsigned key = lane < there ? key_at(tokens, at + lane, V) : 0;
+        for (int e = 0; e < there; ++e) {
+            const unsigned k = __builtin_amdgcn_readlane(key, e);
+            count += k < mine || (k == mine && at + e < i);
+        }
+    }
+    counts[wave][lane] = count;
+    __syncthreads();
+    if (wave || i >= n) return;
+    int place = 0;
+#pragma unroll
+    for (int w = 0; w < kRankWaves; ++w) place += counts[w][lane];
+    keys[place] = mine;
+    order[place] = i;
+}
+
 // ----------------------------------------------------------------------------- sums of runs
-// A wavefront takes kRun sorted positions and 256 columns.  A token whose positions all lie in its stretch is written; what it has of one that goes on in front of or behind the stretch
-// is left in memory (at most two rows), and join_kernel adds those up.
+// A wavefront takes a stretch of sorted positions and 256 columns.  A token whose positions begin in it and end in it or the next stretch it adds up as a whole.  Of a longer one, what lies in
+// its stretch is left in memory (at most two rows), and the wavefront in whose stretch the token begins puts it on a list; join_kernel adds the parts up in order.
 constexpr int kCols = 256;
 constexpr int kMostRun = 32;
 struct Runs {
@@ -249,7 +292,7 @@ template <bool VEC> __device__ __forceinline__ void finish(const Runs &z, float 
 }
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void runs_kernel(Runs z, const unsigned *__restrict__ keys, const int *__restrict__ order, const T *__restrict__ dout, float *__restrict__ dtable,
-                                                        float *__restrict__ left_over)
+                                                        float *__restrict__ left_over, int *__restrict__ list)
 {
     const int lane = threadIdx.x & 63;
     const long long task = (long long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -259,107 +302,118 @@ __global__ __launch_bounds__(kThreads) void runs_kernel(Runs z, const unsigned *
     const int col = chunk * kCols + Row<T, VEC>::column(lane), left = z.E - col;
     // the stretch's keys and positions, one a lane; the neighbours' keys behind them
     const int at = from + lane;
-    const unsigned my_key = at < to ? keys[at] : z.V, key_before = from ? keys[from - 1] : z.V, key_behind = to < z.n ? keys[to] : z.V;
-    const int my_pos = at < to ? order[at] : 0;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const int end = z.n - from < 2 * z.run ? z.n : from + 2 * z.run;
+    const unsigned my_key = at < end ? keys[at] : z.V, key_before = from ? keys[from - 1] : z.V, key_behind = end < z.n ? keys[end] : z.V;
+    const int my_pos = at < end ? order[at] : 0;
+    const int count = to - from, all = end - from;      // positions of the stretch, and of it and the next
+    // the token that goes on from the stretch in front: taken there, as a whole, if it began in it and ends here
+    const unsigned first_key = __builtin_amdgcn_readlane(my_key, 0), last_key = __builtin_amdgcn_readlane(my_key, count - 1);
+    const bool goes_on = from && key_before == first_key;
+    const bool began_before = goes_on && from > z.run && keys[from - z.run - 1] == first_key;           // further than one stretch in front
+    auto key_of = [&](int i) { return i < all ? (unsigned)__builtin_amdgcn_readlane(my_key, i) : key_behind; };
+    const bool whole_stretch = first_key == key_of(count);      // it goes on behind this stretch too
     int begin = 0;
-    const int count = to - from;
+    if (goes_on && !began_before && !whole_stretch)
+        while (begin < count && key_of(begin) == first_key) ++begin;
+    // the last token, if it began here: on to its end, or left as a part
+    const bool last_goes_on = key_of(count) == last_key, last_whole = last_goes_on && !(goes_on && first_key == last_key) && (all < 2 * z.run || key_behind != last_key);
+    int stop = count;
+    if (last_whole)
+        while (stop < all && key_of(stop) == last_key) ++stop;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
     constexpr int U = 8;
-    for (int base = 0; base < count; base += U) {
+    for (int base = begin; base < stop; base += U) {
         Row<T, VEC> x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const unsigned k = __builtin_amdgcn_readlane(my_key, base + u);      // (V behind the last)
-            const long long pos = __builtin_amdgcn_readlane(my_pos, base + u);
-            x[u].load(dout + pos * z.E + col, k < z.V && k != z.pad ? left : 0);
+            const int i = base + u < stop ? base + u : base;
+            const unsigned k = __builtin_amdgcn_readlane(my_key, i);
+            const long long pos = __builtin_amdgcn_readlane(my_pos, i);
+            x[u].load(dout + pos * z.E + col, base + u < stop && k < z.V && k != z.pad ? left : 0);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = base + u;
-            if (i >= count) break;
+            if (i >= stop) break;
             const unsigned k = __builtin_amdgcn_readlane(my_key, i);
             if (k >= z.V) return;               // only what is no token comes behind
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[e] += x[u].v[e];
-            const bool last = i + 1 == count;
-            const unsigned next = last ? key_behind : (unsigned)__builtin_amdgcn_readlane(my_key, i + 1);
-            if (next == k && !last) continue;
-            if (k == z.pad) {
-                begin = i + 1;
-                continue;
+            if (i + 1 < stop && key_of(i + 1) == k) continue;
+            const bool head = goes_on && k == first_key, tail = i + 1 == stop && last_goes_on && !last_whole;
+            if (k != z.pad) {
+                if (head || tail) Row<float, VEC>::store(left_over + ((size_t)stretch * 2 + (head ? 0 : 1)) * z.E + col, left, sum);
+                else finish<VEC>(z, dtable + (size_t)k * z.E + col, left, sum);
+                if (tail && !head && chunk == 0 && lane == 0) list[1 + atomicAdd(list, 1)] = stretch;
             }
-            const bool head = begin == 0 && key_before == k, tail = next == k;
-            if (head || tail)
-                Row<float, VEC>::store(left_over + ((size_t)stretch * 2 + (head ? 0 : 1)) * z.E + col, left, sum);
-            else
-                finish<VEC>(z, dtable + (size_t)k * z.E + col, left, sum);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[e] = 0.f;
-            begin = i + 1;
         }
     }
 }
-// A token that begins in a stretch and goes on behind it: its parts, in order.  The wavefronts take as many stretches each, one after the other.
-constexpr int kJoinWaves = 8;
+// The tokens of the list (whose order says nothing: each is a row of its own): their parts, in order.  The wavefronts of a block take as many stretches each, one after the other.
+constexpr int kJoinWaves = 8, kJoinBlocks = 512;
 template <bool VEC>
-__global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(Runs z, const unsigned *__restrict__ keys, float *__restrict__ dtable, const float *__restrict__ left_over)
+__global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(Runs z, const unsigned *__restrict__ keys, float *__restrict__ dtable, const float *__restrict__ left_over,
+                                                               const int *__restrict__ list)
 {
-    const int stretch = blockIdx.x, from = stretch * z.run, to = from + z.run;
-    if (to >= z.n) return;
-    const unsigned key = keys[to - 1];
-    if (key >= z.V || key == z.pad || keys[to] != key || (from && keys[from - 1] == key)) return;
     __shared__ float part[kJoinWaves][kCols];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // stretches behind this one whose first position is the token's
-    int count = 0;
-    for (int base = stretch + 1;; base += kJoinWaves * 64) {
-        const int s = base + threadIdx.x;
-        const int mine = __syncthreads_count(s < z.stretches && keys[(size_t)s * z.run] == key);
-        count += mine;
-        if (mine < kJoinWaves * 64) break;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.y * kCols + Row<float, VEC>::column(lane), left = z.E - col;
+    for (int entry = blockIdx.x; entry < list[0]; entry += gridDim.x) {
+        const int stretch = list[1 + entry];
+        const unsigned key = keys[(size_t)(stretch + 1) * z.run];
+        // stretches behind this one whose first position is the token's
+        int count = 0;
+        for (int base = stretch + 1;; base += kJoinWaves * 64) {
+            const int s = base + threadIdx.x;
+            const int mine = __syncthreads_count(s < z.stretches && keys[(size_t)s * z.run] == key);
+            count += mine;
+            if (mine < kJoinWaves * 64) break;
+        }
+        const int each = (count + kJoinWaves - 1) / kJoinWaves, first = wave * each, last = count - first < each ? count : first + each;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (wave == 0) {
+            Row<float, VEC> x;
+            x.load(left_over + ((size_t)stretch * 2 + 1) * z.E + col, left);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = x.v[e];
+        }
+        constexpr int U = 8;
+        for (int base = first; base < last; base += U) {
+            Row<float, VEC> x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u].load(left_over + (size_t)(stretch + 1 + (base + u < last ? base + u : base)) * 2 * z.E + col, base + u < last ? left : 0);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += x[u].v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave][e * 64 + lane] = sum[e];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                for (int w = 1; w < kJoinWaves; ++w) sum[e] += part[w][e * 64 + lane];
+            finish<VEC>(z, dtable + (size_t)key * z.E + col, left, sum);
+        }
+        __syncthreads();
     }
-    const int col = blockIdx.y * kCols + Row<float, VEC>::column(lane), left = z.E - col;
-    const int each = (count + kJoinWaves - 1) / kJoinWaves, first = wave * each, last = count - first < each ? count : first + each;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    if (wave == 0) {
-        Row<float, VEC> x;
-        x.load(left_over + ((size_t)stretch * 2 + 1) * z.E + col, left);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = x.v[e];
-    }
-    constexpr int U = 8;
-    for (int base = first; base < last; base += U) {
-        Row<float, VEC> x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[u].load(left_over + (size_t)(stretch + 1 + (base + u < last ? base + u : base)) * 2 * z.E + col, base + u < last ? left : 0);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += x[u].v[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[wave][e * 64 + lane] = sum[e];
-    __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        for (int w = 1; w < kJoinWaves; ++w) sum[e] += part[w][e * 64 + lane];
-    finish<VEC>(z, dtable + (size_t)key * z.E + col, left, sum);
 }
 
 // Where things lie in the workspace.
 struct Plan {
     bool few;
     int passes, tiles, run, stretches;
-    size_t keys[2], order[2], counts, left_over, bytes;
+    size_t keys[2], order[2], counts, list, left_over, bytes;
 };
 Plan plan_of(int n, int E, int V)
 {
     Plan p{};
-    p.few = n <= kRankMost;
+    p.few = n <= kFew;
     p.tiles = ceil_div(n, kTile);
     while (p.passes < 4 && ((long long)V >> (kBits * p.passes)) > 0) ++p.passes;
-    p.run = n <= kRankMost ? 16 : kMostRun;
+    p.run = n <= kFew ? 8 : kMostRun;
     p.stretches = ceil_div(n, p.run);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -372,6 +426,7 @@ Plan plan_of(int n, int E, int V)
         p.order[k] = take((size_t)n * 4);
     }
     p.counts = p.few ? 0 : take(((size_t)p.tiles + 1) * kDigits * 4);
+    p.list = take(((size_t)p.stretches + 1) * 4);
     p.left_over = take((size_t)p.stretches * 2 * E * 4);
     p.bytes = at;
     return p;
@@ -379,8 +434,8 @@ Plan plan_of(int n, int E, int V)
 int check(int n, int E, int V)
 {
     if (n <= 0 || E <= 0 || V <= 0) return NSK_ERR_BAD_DESC;
-    // (a launch has fewer than 2^32 threads: 512 for 32 positions and 256 columns in the largest)
-    if (ceil_div(E, kCols) > 65535 || ((long long)n + 31) / 32 * ceil_div(E, kCols) > 1LL << 22) return NSK_ERR_UNSUPPORTED;
+    // (a launch has fewer than 2^32 threads: 64 for 32 positions and 256 columns in the largest)
+    if (ceil_div(E, kCols) > 8192 || ((long long)n + 31) / 32 * ceil_div(E, kCols) > 1LL << 25) return NSK_ERR_UNSUPPORTED;
     return NSK_OK;
 }
 
@@ -434,17 +489,22 @@ int nsk_embedding_scaled_bwd(int dtype, int n, int E, int V, const int *tokens, 
     const unsigned filling = (unsigned)((elements + 16383) / 16384 < 1024 ? (elements + 16383) / 16384 : 1024);
     auto keys_at = [&](int k) { return (unsigned *)(ws + p.keys[k]); };
     auto order_at = [&](int k) { return (int *)(ws + p.order[k]); };
-    int last = 0;
+    int last = 0, *list = (int *)(ws + p.list);
     if (p.few) {
         const unsigned ranking = (unsigned)ceil_div(n, 64);
-        hipLaunchKernelGGL(rank_kernel, dim3(ranking + filling), dim3(kRankWaves * 64), 0, st, (const unsigned *)tokens, n, keys_at(0), order_at(0), ranking, dtable, elements);
+        auto rank = [&](auto narrow) {
+            hipLaunchKernelGGL(rank_kernel<decltype(narrow)::value>, dim3(ranking + filling), dim3(kRankWaves * 64), 0, st, (const unsigned *)tokens, n, (unsigned)V, keys_at(0), order_at(0),
+                               ranking, dtable, elements, list);
+        };
+        if (V < 65535) rank(std::true_type{});
+        else rank(std::false_type{});
     } else {
         int *counts = (int *)(ws + p.counts);
         const unsigned *from = (const unsigned *)tokens;
         const int *from_order = nullptr;
         for (int k = 0; k < p.passes; ++k) {
             last = k & 1;
-            hipLaunchKernelGGL(digits_kernel, dim3((unsigned)p.tiles + (k == 0 ? filling : 0)), dim3(kThreads), 0, st, from, n, (unsigned)V, kBits * k, p.tiles, counts, dtable, elements);
+            hipLaunchKernelGGL(digits_kernel, dim3((unsigned)p.tiles + (k == 0 ? filling : 0)), dim3(kThreads), 0, st, from, n, (unsigned)V, kBits * k, p.tiles, counts, dtable, elements, list);
             hipLaunchKernelGGL(places_kernel, dim3(kDigits), dim3(64), 0, st, p.tiles, counts);
             hipLaunchKernelGGL(scatter_kernel, dim3((unsigned)p.tiles), dim3(kThreads), 0, st, from, from_order, n, (unsigned)V, kBits * k, p.tiles, counts, keys_at(last), order_at(last));
             from = keys_at(last);
@@ -455,12 +515,12 @@ int nsk_embedding_scaled_bwd(int dtype, int n, int E, int V, const int *tokens, 
     const int *order = order_at(last);
     const Runs z{n, E, (unsigned)V, pad < 0 ? (unsigned)V : (unsigned)pad, p.run, p.stretches, ceil_div(E, kCols), scale, accumulate};
     float *left_over = (float *)(ws + p.left_over);
-    const dim3 grid((unsigned)(((long long)z.stretches * z.chunks + kWaves - 1) / kWaves)), joins((unsigned)z.stretches, (unsigned)z.chunks);
+    const dim3 grid((unsigned)(((long long)z.stretches * z.chunks + kWaves - 1) / kWaves)), joins((unsigned)(z.stretches < kJoinBlocks ? z.stretches : kJoinBlocks), (unsigned)z.chunks);
     auto launch = [&](auto one, auto vec) {
         typedef decltype(one) T;
         constexpr bool VEC = decltype(vec)::value;
-        hipLaunchKernelGGL((runs_kernel<T, VEC>), grid, dim3(kThreads), 0, st, z, keys, order, (const T *)dout, dtable, left_over);
-        hipLaunchKernelGGL(join_kernel<VEC>, joins, dim3(kJoinWaves * 64), 0, st, z, keys, dtable, left_over);
+        hipLaunchKernelGGL((runs_kernel<T, VEC>), grid, dim3(kThreads), 0, st, z, keys, order, (const T *)dout, dtable, left_over, list);
+        hipLaunchKernelGGL(join_kernel<VEC>, joins, dim3(kJoinWaves * 64), 0, st, z, keys, dtable, left_over, list);
     };
     if (dtype == NSK_BF16) {
         if (E % 4) launch(bf16_t{}, std::false_type{});
