@@ -435,7 +435,8 @@ int check(int n, int E, int V)
 {
     if (n <= 0 || E <= 0 || V <= 0) return NSK_ERR_BAD_DESC;
     // (a launch has fewer than 2^32 threads: 64 for 32 positions and 256 columns in the largest)
-    if (ceil_div(E, kCols) > 8192 || ((long long)n + 31) / 32 * ceil_div(E, kCols) > 1LL << 25) return NSK_ERR_UNSUPPORTED;
+    const long long chunks = ((long long)E + kCols - 1) / kCols;
+    if (chunks > 8192 || ((long long)n + 31) / 32 * chunks > 1LL << 25) return NSK_ERR_UNSUPPORTED;
     return NSK_OK;
 }
 

@@ -1,0 +1,124 @@
+"""Scaled embedding and its gradient by sorted tokens.
+
+Tolerances.  Forward: one product, rounded once: the same bits as torch's product in fp32, rounded.  Gradient: a sum of m rows in stretches: at most m additions, 2^-24 of the partial sums
+each, and one product: |error| <= 2^-24 * (m + 2) * scale * (sum of magnitudes)."""
+import math
+
+import pytest
+import torch
+
+from oracle import learning as O
+from paper_2409_11600_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def tokens_of(n, V, kind, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    if kind == "even":
+        t = torch.randint(0, V, (n,), generator=gen)
+    elif kind == "one":
+        t = torch.full((n,), V - 1)
+    elif kind == "words":               # few are frequent, many rare
+        t = (V ** torch.rand(n, generator=gen) - 1).long()
+    elif kind == "runs":                # as often as the stretches are long, and one more or less
+        t = torch.arange(n) // torch.randint(30, 35, (1,), generator=gen) % V
+    else:                               # some are none
+        t = torch.randint(-3, V + 3, (n,), generator=gen)
+        t[::7], t[1::11] = -2 ** 31, 2 ** 31 - 1
+    return t.to(torch.int32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,E,V", [(1, 1, 1), (50, 256, 300), (3, 8, 5), (77, 33, 10), (1000, 7, 4), (300, 1028, 50), (257, 12, 9)])
+def test_forward(n, E, V, dtype):
+    table = torch.randn(V, E, generator=torch.Generator().manual_seed(1)).to(TYPES[dtype])
+    for pad in (None, V - 1):
+        for kind in ("even", "none"):
+            t = tokens_of(n, V, kind)
+            out = B.embedding_scaled_fwd(t.cuda(), table.cuda(), 2.7, pad=pad)
+            inside = (t >= 0) & (t < V)
+            want = (table[t.clamp(0, V - 1).long()].float() * torch.tensor(2.7)).to(TYPES[dtype])
+            if pad is not None:
+                want[t == pad] = 0
+            assert torch.equal(out.cpu()[inside], want[inside]) and bool(out.cpu()[~inside].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,E,V,kind", [(1, 1, 1, "one"), (2, 4, 70000, "even"), (63, 20, 8, "even"), (64, 8, 3, "none"), (65, 8, 65534, "even"), (65, 8, 65535, "even"), (1000, 7, 50, "words"),
+                                        (9000, 40, 900, "words"), (5000, 260, 2, "even"), (4000, 16, 100, "runs"), (4096, 12, 5, "one"), (16384, 8, 70000, "none"), (16385, 8, 70000, "none"),
+                                        (20000, 12, 600, "words"), (17000, 520, 3, "even"), (40000, 9, 1, "one"), (33000, 4, 100000, "runs"), (50000, 16, 512, "words"), (17001, 8, 300000, "words")])
+def test_gradient(n, E, V, kind, dtype):
+    t, dt = tokens_of(n, V, kind, seed=n), TYPES[dtype]
+    dout = torch.randn(n, E, generator=torch.Generator().manual_seed(2)).to(dt)
+    inside = (t >= 0) & (t < V)
+    for pad in (None, int(t[inside][0]) if bool(inside.any()) else 0):
+        counts = inside if pad is None else inside & (t != pad)
+        at, d = t[counts].long(), dout[counts].double()
+        want = torch.zeros(V, E, dtype=torch.float64).index_add(0, at, d) * 1.5
+        size = torch.zeros(V, E, dtype=torch.float64).index_add(0, at, d.abs()) * 1.5
+        m = torch.zeros(V, dtype=torch.float64).index_add(0, at, torch.ones(len(at), dtype=torch.float64))[:, None]
+        got = B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad)
+        assert bool(((got.double().cpu() - want).abs() <= 2.0 ** -24 * (m + 2) * size).all())
+        old = torch.randn(V, E, generator=torch.Generator().manual_seed(3))
+        added = B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad, dtable=old.cuda(), accumulate=True)
+        assert bool(((added.double().cpu() - want - old.double()).abs() <= 2.0 ** -24 * ((m + 2) * size + (want + old).abs() * 2)).all())
+        assert torch.equal(added.cpu()[m[:, 0] == 0], old[m[:, 0] == 0])           # what does not occur stays
+        assert torch.equal(got, B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad))
+
+
+def test_small_against_the_loop():
+    t, dout = tokens_of(40, 6, "none"), torch.randn(40, 5)
+    want = O.embedding_gradient(t, dout.double(), 6, 0.3, pad=2)
+    assert (B.embedding_scaled_bwd(t.cuda(), dout.cuda(), 6, 0.3, pad=2).double().cpu() - want).abs().max() <= 2.0 ** -24 * 40 * 0.3 * dout.abs().sum(0).max()
+    out, table = B.embedding_scaled_fwd(t.cuda(), dout[:6].cuda(), 0.3, pad=2), dout[:6].double()
+    assert torch.allclose(out.double().cpu(), O.embedding(t, table, 0.3, pad=2), rtol=2.0 ** -23, atol=0, equal_nan=True)
+
+
+def test_as_the_unscaled_one():
+    """Both calls of the framework, where they mean the same: the same rows, and sums within their roundings."""
+    t, table, dout = tokens_of(3000, 200, "words").cuda(), torch.randn(200, 64, device="cuda"), torch.randn(3000, 64, device="cuda")
+    assert torch.equal(B.embedding_scaled_fwd(t, table), B.embedding_fwd(t, table))
+    a, b = B.embedding_scaled_bwd(t, dout, 200), B.embedding_bwd(t, dout, 200)
+    assert (a - b).abs().max() <= 2.0 ** -23 * 3000 * dout.abs().max()
+
+
+def test_room_behind_the_table_stays():
+    buf = torch.full((64,), 3.0, device="cuda")
+    t = torch.tensor([0, 2, 2], dtype=torch.int32, device="cuda")
+    B.embedding_scaled_bwd(t, torch.ones(3, 7, device="cuda"), 3, 2.0, dtable=buf[:21].view(3, 7))
+    assert torch.equal(buf[:21].view(3, 7), torch.tensor([2.0, 0.0, 4.0], device="cuda")[:, None].expand(3, 7)) and bool((buf[21:] == 3).all())
+
+
+@pytest.mark.parametrize("n", [500, 30000])
+def test_captured(n):
+    E, V = 24, 800
+    t, dout, ws = tokens_of(n, V, "words").cuda(), torch.randn(n, E, device="cuda"), B.Workspace()
+    out, grad = B.embedding_scaled_fwd(t, torch.randn(V, E, device="cuda"), 2.0), B.embedding_scaled_bwd(t, dout, V, 2.0, ws=ws)
+    table = torch.randn(V, E, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        B.embedding_scaled_fwd(t, table, 2.0, out=out)
+        B.embedding_scaled_bwd(t, dout, V, 2.0, dtable=grad, ws=ws)
+    for k in ("even", "words", "one", "none"):
+        t.copy_(tokens_of(n, V, k, seed=5).cuda())
+        dout.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, B.embedding_scaled_bwd(t, dout, V, 2.0))
+        assert torch.equal(out.nan_to_num(nan=77), B.embedding_scaled_fwd(t, table, 2.0).nan_to_num(nan=77))
+
+
+def test_beside_each_other():
+    data = [(tokens_of(n, 900, "words", seed=n).cuda(), torch.randn(n, 64, device="cuda")) for n in (12000, 30000)]
+    want = [B.embedding_scaled_bwd(t, d, 900) for t, d in data]
+    torch.cuda.synchronize()
+    streams, spaces, got = [torch.cuda.Stream() for _ in data], [B.Workspace() for _ in data], []
+    for _ in range(6):
+        for s, ws, (t, d) in zip(streams, spaces, data):
+            with torch.cuda.stream(s):
+                got.append(B.embedding_scaled_bwd(t, d, 900, ws=ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 2]) for i, g in enumerate(got))
