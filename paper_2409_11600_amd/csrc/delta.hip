@@ -8,7 +8,9 @@
 //   dV = beta X,  dA = -X U^T,  dP = dO U^T  (where A and P are not zero),  and with E1 = X S^T, E2 = dO S^T, E3 = U G^T:
 //   dQ = exp(c) E2 + (dP L) K,  dK = -beta exp(c) E1 + exp(C - c) E3 + (dA beta L) K + (dA beta L)^T K + (dP L)^T Q,  L_ij = exp(c_i - c_j),
 //   and the gradients of c, of beta and of the lengths of q and k from the row and column sums of the same products.
-// All products are on the fp32 matrix unit: states, gates' gradients and the results of a chunk of 64 dependent steps keep 32 bits.
+// Products keep 32 bits: states, gates' gradients and the results of a chunk of 64 dependent steps.  Those of two float operands are on the fp32 matrix unit.  Keys and queries in bf16 stay what they
+// are (their lengths are factors of rows and columns, applied to the products), and what they are multiplied with goes in three bf16 pieces that hold all of its bits: three products of 16
+// clocks for 32 indices, where the fp32 unit takes eight of 32.
 //
 // Where a product's result is the next one's right operand (S, U, X, G), it stays in its registers: v_mfma_f32_16x16x4_f32 leaves lane l rows 4 (l / 16) + r, r < 4, of column l % 16,
 // and a right operand of 16 rows is read in four steps of which step s takes from lane l one value of column l % 16; which row that is is free as long as the left operand's lane takes the same:
@@ -190,6 +192,17 @@ template <typename T> __device__ __forceinline__ void load_gates(int l, const Si
     p.finish(l, z, bias, h, live, g);
 }
 
+// A row of K or Q in LDS: neighbouring rows four banks apart.
+template <typename T> constexpr int row_of(int DP) { return sizeof(T) == 2 ? DP + 8 : DP + 4; }
+// Lengths of the chunk's rows.  Where T is float, K and Q hold normalised rows, and in_products below leaves the products as they are.
+struct Lengths {
+    float k[kC], q[kC], unit_q[kC];         // 1 / |k|, 1 / |q|, 1 / (sqrt(D) |q|)
+};
+template <typename T> __device__ __forceinline__ f32x4 in_products(int l, f32x4 x, const float *lengths, int row0)
+{
+    if constexpr (sizeof(T) == 2) return x * rows_of(l, lengths, row0);
+    else return x;
+}
 // A row of q or k: THREADS / 64 neighbouring lanes take vectors of 16 bytes in turn.  They stay as they were loaded until they are used, so that nothing waits for them before.
 template <typename T, int DP, int THREADS> struct RowPart {
     typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -244,18 +257,20 @@ template <typename T, int DP, int THREADS> struct RowPart {
         if (LANES == 8) s += lane_xor<4>(s);
         return 1.f / sqrtf(s + kEps);
     }
-    __device__ __forceinline__ void store(int l, float *row, float by) const
+    __device__ __forceinline__ void store(int l, T *row, float by) const
     {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int v = l % LANES + i * LANES;
             if (VECTORS % LANES && v >= VECTORS) continue;
+            if constexpr (sizeof(T) == 2) *(u32x4 *)(row + v * V) = x[i];
+            else
 #pragma unroll
             for (int e = 0; e < V; e += 4) *(f32x4 *)(row + v * V + e) = (f32x4){value(i, e) * by, value(i, e + 1) * by, value(i, e + 2) * by, value(i, e + 3) * by};
         }
     }
 };
-// Normalised keys and queries of a chunk into LDS, [64][DP + 4]; inv_k, inv_q: NULL, or where 1 / |k| and 1 / |q| go.
+// Keys and queries of a chunk into LDS, and their lengths.
 template <typename T, int DP, int THREADS> struct KeyParts {
     typedef RowPart<T, DP, THREADS> Part;
     Part k, q;
@@ -264,18 +279,84 @@ template <typename T, int DP, int THREADS> struct KeyParts {
         k.load(l, wave, row0 + k_at(z, hk), z.gi_t, z.D, live, z.vec);
         q.load(l, wave, row0 + q_at(z, hk), z.gi_t, z.D, live, z.vec);
     }
-    __device__ __forceinline__ void finish(int l, int wave, const Sizes &z, float *K, float *Q, float *inv_k, float *inv_q) const
+    __device__ __forceinline__ void finish(int l, int wave, const Sizes &z, T *K, T *Q, Lengths &lengths) const
     {
         const int r = wave * Part::ROWS + l / Part::LANES;
-        const float ik = k.inverse_length(), iq = q.inverse_length();
-        k.store(l, K + r * (DP + 4), ik);
-        q.store(l, Q + r * (DP + 4), iq / sqrtf((float)z.D));
-        if (inv_k && l % Part::LANES == 0) {
-            inv_k[r] = ik;
-            inv_q[r] = iq;
+        const float ik = k.inverse_length(), iq = q.inverse_length(), unit = iq / sqrtf((float)z.D);
+        k.store(l, K + r * row_of<T>(DP), ik);
+        q.store(l, Q + r * row_of<T>(DP), unit);
+        if (l % Part::LANES == 0) {
+            lengths.k[r] = ik;
+            lengths.q[r] = iq;
+            lengths.unit_q[r] = unit;
         }
     }
 };
+
+// Right operands of products with K and Q: the state's DT tiles of 16 rows, or the chunk's four, as they are in registers or in pieces.  A lane's eight values of 32 rows are those of two tiles
+// one after the other; the left operands below are read in the same order.
+template <typename T, int TILES> struct Operand {
+    f32x4 x[TILES];
+    __device__ __forceinline__ void set(const f32x4 (&v)[TILES])
+    {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) x[i] = v[i];
+    }
+};
+template <int TILES> struct Operand<bf16_t, TILES> {
+    Pieces x[TILES / 2];
+    __device__ __forceinline__ void set(const f32x4 (&v)[TILES])
+    {
+#pragma unroll
+        for (int i = 0; i < TILES / 2; ++i) {
+            const float y[8] = {v[2 * i][0], v[2 * i][1], v[2 * i][2], v[2 * i][3], v[2 * i + 1][0], v[2 * i + 1][1], v[2 * i + 1][2], v[2 * i + 1][3]};
+            x[i] = split3<false>(y);
+        }
+    }
+};
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(bf16x8 a, const Pieces &b, f32x4 c) { return mfma(a, b.h, mfma(a, b.m, mfma(a, b.l, c))); }
+__device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+// Four rows of m from k0 + 4 (l / 16) on, of column row0 + l % 16: a read that turns 4 x 16 elements (each lane gives the address of four of a row).
+__device__ __forceinline__ bf16x4 turned(int l, const bf16_t *m, int ld, int row0, int k0)
+{
+    typedef __attribute__((address_space(3))) bf16x4 *Lds;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)(m + (k0 + 4 * (l >> 4) + ((l & 15) >> 2)) * ld + row0 + 4 * (l & 3)));
+}
+// 16 rows of m from row0 on, times the operand.
+template <int TILES> __device__ __forceinline__ f32x4 times(int l, const float *m, int ld, int row0, const Operand<float, TILES> &o, f32x4 c)
+{
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) c = multiply(frag(l, m, ld, row0, 16 * k), o.x[k], c);
+    return c;
+}
+template <int TILES> __device__ __forceinline__ f32x4 times(int l, const bf16_t *m, int ld, int row0, const Operand<bf16_t, TILES> &o, f32x4 c)
+{
+    const bf16_t *p = m + (row0 + (l & 15)) * ld + 4 * (l >> 4);
+#pragma unroll
+    for (int k = 0; k < TILES / 2; ++k) c = multiply(both(*(const bf16x4 *)(p + 32 * k), *(const bf16x4 *)(p + 32 * k + 16)), o.x[k], c);
+    return c;
+}
+// The same of m transposed: its columns row0.., over the chunk's rows.
+__device__ __forceinline__ f32x4 times_t(int l, const float *m, int ld, int row0, const Operand<float, 4> &o, f32x4 c)
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) c = multiply(frag_t(l, m, ld, row0, 16 * b), o.x[b], c);
+    return c;
+}
+__device__ __forceinline__ f32x4 times_t(int l, const bf16_t *m, int ld, int row0, const Operand<bf16_t, 4> &o, f32x4 c)
+{
+#pragma unroll
+    for (int b = 0; b < 2; ++b) c = multiply(both(turned(l, m, ld, row0, 32 * b), turned(l, m, ld, row0, 32 * b + 16)), o.x[b], c);
+    return c;
+}
+// A right operand of 16 of the chunk's rows on the fp32 unit: normalised keys or queries.
+__device__ __forceinline__ f32x4 rows_t(int l, const float *m, int ld, int row0, int k0, const float *) { return frag_t(l, m, ld, row0, k0); }
+__device__ __forceinline__ f32x4 rows_t(int l, const bf16_t *m, int ld, int row0, int k0, const float *lengths)
+{
+    const bf16x4 x = turned(l, m, ld, row0, k0);
+    return (f32x4){(float)x[0], (float)x[1], (float)x[2], (float)x[3]} * rows_of(l, lengths, k0);
+}
 
 // The tiles of 16 x 16 of A and P that are not zero: 10 each.
 constexpr int kTiles = 10;
@@ -305,12 +386,13 @@ __device__ __forceinline__ void store_tile(int l, float *m, int bi, int bj, f32x
 }
 // -A and P by NW wavefronts, the first TILES tiles of 20, of which the first ten are A's: every NW-th tile from this wavefront's number on.  All of a wavefront's tiles go through the products
 // together: one after the other they would wait for LDS four times each.  Returns the tiles without beta (A) or as they are (P), zeros where a wavefront has one less.
-template <int DP, int NW, int TILES, int EACH = (TILES + NW - 1) / NW>
-__device__ __forceinline__ void make_tiles(int l, int wave, const Gates &g, const float *K, const float *Q, float *A, float *P, f32x4 (&x)[EACH])
+template <typename T, int DP, int NW, int TILES, int EACH = (TILES + NW - 1) / NW>
+__device__ __forceinline__ void make_tiles(int l, int wave, const Gates &g, const Lengths &lengths, const T *K, const T *Q, float *A, float *P, f32x4 (&x)[EACH])
 {
-    constexpr int LD = DP + 4;
+    constexpr int LD = row_of<T>(DP), STEP = sizeof(T) == 2 ? 32 : 16;
+    typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Frag;
     int bi[EACH], bj[EACH];
-    const float *left[EACH];
+    const T *left[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int t = wave + i * NW < TILES ? wave + i * NW : TILES - 1;
@@ -319,17 +401,23 @@ __device__ __forceinline__ void make_tiles(int l, int wave, const Gates &g, cons
         x[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
 #pragma unroll
-    for (int k0 = 0; k0 < DP; k0 += 16) {
-        f32x4 a[EACH], b[EACH];
+    for (int k0 = 0; k0 < DP; k0 += STEP) {
+        const int at = (l & 15) * LD + k0 + STEP / 4 * (l >> 4);
+        Frag a[EACH], b[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            a[i] = frag(l, left[i], LD, 16 * bi[i], k0);
-            b[i] = frag(l, K, LD, 16 * bj[i], k0);
+            a[i] = *(const Frag *)(left[i] + 16 * bi[i] * LD + at);
+            b[i] = *(const Frag *)(K + 16 * bj[i] * LD + at);
         }
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+            for (int i = 0; i < EACH; ++i) x[i] = mfma(a[i], b[i], x[i]);
+        } else {
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) x[i] = mfma(a[i][s], b[i][s], x[i]);
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) x[i] = mfma(a[i][s], b[i][s], x[i]);
+        }
     }
     settle(x);
 #pragma unroll
@@ -337,6 +425,7 @@ __device__ __forceinline__ void make_tiles(int l, int wave, const Gates &g, cons
         const int t = wave + i * NW;
         const bool is_a = t < kTiles;
         x[i] *= decays(l, g, bi[i], bj[i], is_a);
+        if constexpr (sizeof(T) == 2) x[i] *= rows_of(l, is_a ? lengths.k : lengths.unit_q, 16 * bi[i]) * lengths.k[16 * bj[i] + (l & 15)];
         const f32x4 by = -rows_of(l, g.beta, 16 * bi[i]);
         if (t >= TILES) x[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
         else store_tile(l, is_a ? A : P, bi[i], bj[i], is_a ? by * x[i] : x[i]);
@@ -452,33 +541,31 @@ __device__ __forceinline__ f32x4 frag_of(int l, const float *m, int rows, int ro
     return x;
 }
 
-template <int DT> struct Shared {
-    static constexpr int DP = 16 * DT, LD = DP + 4;
-    float K[kC * LD], Q[kC * LD], A[kC * kLA], P[kC * kLA];
+template <typename T, int DT> struct Shared {
+    static constexpr int DP = 16 * DT, LD = row_of<T>(DP);
+    alignas(16) T K[kC * LD];
+    alignas(16) T Q[kC * LD];
+    alignas(16) float A[kC * kLA], P[kC * kLA];
     Gates g;
+    alignas(16) Lengths lengths;
 };
 
 // beta (V - exp(c) K S), in place of V
-template <int DT> __device__ __forceinline__ void below_state(int l, const Shared<DT> &s, const f32x4 (&S)[DT], f32x4 (&X)[4])
+template <typename T, int DT> __device__ __forceinline__ void below_state(int l, const Shared<T, DT> &s, const Operand<T, DT> &S, f32x4 (&X)[4])
 {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < DT; ++k) acc = multiply(frag(l, s.K, s.LD, 16 * b, 16 * k), S[k], acc);
+        const f32x4 acc = in_products<T>(l, times(l, s.K, s.LD, 16 * b, S, (f32x4){0.f, 0.f, 0.f, 0.f}), s.lengths.k, 16 * b);
         X[b] = rows_of(l, s.g.beta, 16 * b) * (X[b] - rows_of(l, s.g.in, 16 * b) * acc);
         fence();
     }
 }
 // exp(c) Q S + P U
-template <int DT> __device__ __forceinline__ void answers(int l, const Shared<DT> &s, const f32x4 (&S)[DT], const f32x4 (&U)[4], f32x4 (&O)[4])
+template <typename T, int DT> __device__ __forceinline__ void answers(int l, const Shared<T, DT> &s, const Operand<T, DT> &S, const f32x4 (&U)[4], f32x4 (&O)[4])
 {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-        O[b] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < DT; ++k) O[b] = multiply(frag(l, s.Q, s.LD, 16 * b, 16 * k), S[k], O[b]);
-        O[b] *= rows_of(l, s.g.in, 16 * b);
+        O[b] = rows_of(l, s.g.in, 16 * b) * in_products<T>(l, times(l, s.Q, s.LD, 16 * b, S, (f32x4){0.f, 0.f, 0.f, 0.f}), s.lengths.unit_q, 16 * b);
 #pragma unroll
         for (int j = 0; j <= b; ++j) O[b] = multiply(frag(l, s.P, kLA, 16 * b, 16 * j), U[j], O[b]);
         fence();
@@ -492,8 +579,9 @@ template <typename T, int DT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
                                                             T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
 {
-    typedef Shared<DT> Lds;
-    constexpr int DP = Lds::DP, LD = Lds::LD;
+    typedef Shared<T, DT> Lds;
+    constexpr int DP = Lds::DP;
+    constexpr int LD = Lds::LD;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Lds &s = *(Lds *)lds;
     const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -526,7 +614,7 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T 
             continue;
         }
         lds_barrier();
-        keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
+        keys.finish(l, wave, z, s.K, s.Q, s.lengths);
         if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
         values_of<T>(v, X);
         if (t0 + kC < len) fetch(c + 1);
@@ -534,26 +622,29 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T 
         lds_barrier();
         {
             f32x4 tiles[(2 * kTiles + NW - 1) / NW];
-            make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+            make_tiles<T, DP, NW, 2 * kTiles>(l, wave, s.g, s.lengths, s.K, s.Q, s.A, s.P, tiles);
         }
         lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
-        below_state<DT>(l, s, S, X);
+        Operand<T, DT> state;
+        state.set(S);
+        below_state(l, s, state, X);
         lds_barrier();
         solve(l, s.A, X);
+        settle(X);
         if (o) {
             f32x4 O[4];
-            answers<DT>(l, s, S, X, O);
+            answers(l, s, state, X, O);
             store_rows(l, z, out, z.o_t, live, rows, col, O);
         }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) X[b] *= rows_of(l, s.g.out, 16 * b);
+        for (int b = 0; b < 4; ++b) X[b] *= in_products<T>(l, rows_of(l, s.g.out, 16 * b), s.lengths.k, 16 * b);
+        Operand<T, 4> written;
+        written.set(X);
         const float all = s.g.all;
 #pragma unroll
         for (int k = 0; k < DT; ++k) {
-            S[k] *= all;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) S[k] = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], S[k]);
+            S[k] = times_t(l, s.K, LD, 16 * k, written, S[k] * all);
             if (k & 1) fence();
         }
         settle(S);
@@ -570,8 +661,9 @@ template <typename T, int DT, int NW, bool BACK>
 __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
                                                                  float *__restrict__ matrices)
 {
-    typedef Shared<DT> Lds;
-    constexpr int DP = Lds::DP, LD = Lds::LD;
+    typedef Shared<T, DT> Lds;
+    constexpr int DP = Lds::DP;
+    constexpr int LD = Lds::LD;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Lds &s = *(Lds *)lds;
     const int c = blockIdx.x / (z.N * z.H), rest = blockIdx.x - c * (z.N * z.H), n = rest / z.H, h = rest - n * z.H, hk = h / (z.H / z.Hk);
@@ -589,13 +681,13 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
     if (BACK) load_rows(l, z, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr, z.o_t, live, unit ? z.Dv : col, raw);
     else load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, unit ? z.Dv : col, raw);
     if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-    keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
+    keys.finish(l, wave, z, s.K, s.Q, s.lengths);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     lds_barrier();
     {
         constexpr int TILES = (BACK ? 2 : 1) * kTiles;
         f32x4 tiles[(TILES + NW - 1) / NW];
-        make_tiles<DP, NW, TILES>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+        make_tiles<T, DP, NW, TILES>(l, wave, s.g, s.lengths, s.K, s.Q, s.A, s.P, tiles);
     }
     lds_barrier();
     if (wave < 4) invert_block(l, s.A, wave);
@@ -607,7 +699,8 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) X[b][r] = s.K[(16 * b + g4 + r) * LD + col];
+            for (int r = 0; r < 4; ++r) X[b][r] = (float)s.K[(16 * b + g4 + r) * LD + col];
+            X[b] = in_products<T>(l, X[b], s.lengths.k, 16 * b);
             X[b] *= BACK ? rows_of(l, s.g.out, 16 * b) : -rows_of(l, s.g.in, 16 * b) * rows_of(l, s.g.beta, 16 * b);
         }
     } else if (!BACK) {
@@ -627,9 +720,12 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const f32x4 in = rows_of(l, s.g.in, 16 * b);
-        if (BACK) V[b] *= in;
-        X[b] *= BACK ? -in * rows_of(l, s.g.beta, 16 * b) : rows_of(l, s.g.out, 16 * b);
+        if (BACK) V[b] *= in_products<T>(l, in, s.lengths.unit_q, 16 * b);
+        X[b] *= in_products<T>(l, BACK ? -in * rows_of(l, s.g.beta, 16 * b) : rows_of(l, s.g.out, 16 * b), s.lengths.k, 16 * b);
     }
+    Operand<T, 4> written, asked;
+    written.set(X);
+    if (BACK) asked.set(V);
     const float all = s.g.all;
     const int width = unit ? z.D : z.Dv;
     float *m = matrices + matrices_at(z, c, n, h) + (unit ? 0 : (size_t)z.D * z.D) + col;
@@ -638,11 +734,8 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
         f32x4 acc;
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[r] = unit && 16 * k + g4 + r == col ? all : 0.f;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (BACK) acc = multiply(frag_t(l, s.Q, LD, 16 * k, 16 * b), V[b], acc);       // (zeros in the unit matrix's columns)
-            acc = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], acc);
-        }
+        if (BACK) acc = times_t(l, s.Q, LD, 16 * k, asked, acc);       // (zeros in the unit matrix's columns)
+        acc = times_t(l, s.K, LD, 16 * k, written, acc);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             if (16 * k + g4 + r < z.D && col < width) m[(size_t)(16 * k + g4 + r) * width] = acc[r];
@@ -734,7 +827,7 @@ template <typename T, int DT, int NW>
 __global__ __launch_bounds__(NW * 64) void delta_out_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ states,
                                                             T *__restrict__ o)
 {
-    typedef Shared<DT> Lds;
+    typedef Shared<T, DT> Lds;
     constexpr int DP = Lds::DP;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Lds &s = *(Lds *)lds;
@@ -751,20 +844,22 @@ __global__ __launch_bounds__(NW * 64) void delta_out_kernel(Sizes z, const T *__
     load_rows(l, z, row0 + v_at(z, h), z.gi_t, live, col, raw);
     load_state(l, z, states + state_at(z, c, n, h), col, S);
     if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
-    keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
+    keys.finish(l, wave, z, s.K, s.Q, s.lengths);
     lds_barrier();
     {
         f32x4 tiles[(2 * kTiles + NW - 1) / NW];
-        make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+        make_tiles<T, DP, NW, 2 * kTiles>(l, wave, s.g, s.lengths, s.K, s.Q, s.A, s.P, tiles);
     }
     lds_barrier();
     if (wave < 4) invert_block(l, s.A, wave);
     values_of<T>(raw, X);
-    below_state<DT>(l, s, S, X);
+    Operand<T, DT> state;
+    state.set(S);
+    below_state(l, s, state, X);
     lds_barrier();
     solve(l, s.A, X);
     f32x4 O[4];
-    answers<DT>(l, s, S, X, O);
+    answers(l, s, state, X, O);
     settle(O);
     store_rows(l, z, out, z.o_t, live, rows, col, O);
 }
@@ -775,8 +870,9 @@ template <typename T, int DT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const T *__restrict__ d_o,
                                                              const float *__restrict__ dh_last, float *__restrict__ dh0, float *__restrict__ ends)
 {
-    typedef Shared<DT> Lds;
-    constexpr int DP = Lds::DP, LD = Lds::LD;
+    typedef Shared<T, DT> Lds;
+    constexpr int DP = Lds::DP;
+    constexpr int LD = Lds::LD;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Lds &s = *(Lds *)lds;
     const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -805,7 +901,7 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T
         store_state(l, z, ends + state_at(z, c, n, h), col, G);
         if (c == 0 && !dh0) break;
         lds_barrier();
-        keys.finish(l, wave, z, s.K, s.Q, nullptr, nullptr);
+        keys.finish(l, wave, z, s.K, s.Q, s.lengths);
         if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
         f32x4 dO[4];
         values_of<T>(raw, dO);
@@ -814,17 +910,16 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T
         lds_barrier();
         {
             f32x4 tiles[(2 * kTiles + NW - 1) / NW];
-            make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tiles);
+            make_tiles<T, DP, NW, 2 * kTiles>(l, wave, s.g, s.lengths, s.K, s.Q, s.A, s.P, tiles);
         }
         lds_barrier();
         if (wave < 4) invert_block(l, s.A, wave);
         f32x4 X[4];
+        Operand<T, DT> behind;
+        behind.set(G);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            X[b] = zero;
-#pragma unroll
-            for (int k = 0; k < DT; ++k) X[b] = multiply(frag(l, s.K, LD, 16 * b, 16 * k), G[k], X[b]);
-            X[b] *= rows_of(l, s.g.out, 16 * b);
+            X[b] = rows_of(l, s.g.out, 16 * b) * in_products<T>(l, times(l, s.K, LD, 16 * b, behind, zero), s.lengths.k, 16 * b);
 #pragma unroll
             for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), dO[i], X[b]);
             fence();
@@ -834,19 +929,17 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const f32x4 in = rows_of(l, s.g.in, 16 * b);
-            dO[b] *= in;
-            X[b] *= -in * rows_of(l, s.g.beta, 16 * b);
+            dO[b] *= in_products<T>(l, in, s.lengths.unit_q, 16 * b);
+            X[b] *= in_products<T>(l, -in * rows_of(l, s.g.beta, 16 * b), s.lengths.k, 16 * b);
         }
+        Operand<T, 4> asked, written;
+        asked.set(dO);
+        written.set(X);
         const float all = s.g.all;
 #pragma unroll
         for (int k = 0; k < DT; ++k) {
-            G[k] *= all;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                G[k] = multiply(frag_t(l, s.Q, LD, 16 * k, 16 * b), dO[b], G[k]);
-                G[k] = multiply(frag_t(l, s.K, LD, 16 * k, 16 * b), X[b], G[k]);
-            }
-            fence();
+            G[k] = times_t(l, s.K, LD, 16 * k, written, times_t(l, s.Q, LD, 16 * k, asked, G[k] * all));
+            if (k & 1) fence();
         }
         settle(G);
     }
@@ -857,7 +950,7 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T
 // their gradients of q and k are summed in registers.  64 columns of the state at a time: four wavefronts make U, the other four X; then all make the products that reach over
 // the columns, each a tile column of dQ and dK and its tiles of dA and dP.
 constexpr int kGradWaves = 8;
-template <int DT> struct GradShared : Shared<DT> {
+template <typename T, int DT> struct GradShared : Shared<T, DT> {
     struct Columns {
         float X[kC * kLA], U[kC * kLA], O[kC * kLA];
     };
@@ -871,14 +964,13 @@ template <int DT> struct GradShared : Shared<DT> {
         Columns v;
         Sums t;
     };
-    float inv_k[kC], inv_q[kC];
     float xr[4][kC];
 };
 template <typename T, int DT>
 __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
                                                                      const float *__restrict__ saved, const T *__restrict__ d_o, const float *__restrict__ ends, T *__restrict__ dgi)
 {
-    typedef GradShared<DT> Lds;
+    typedef GradShared<T, DT> Lds;
     constexpr int DP = Lds::DP, LD = Lds::LD, NW = kGradWaves, RT = 4 * DT / NW, KEEP = (2 * kTiles + NW - 1) / NW;
     static_assert(RT >= 1, "tiles of dQ for every wavefront");
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -908,7 +1000,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
     {
         KeyParts<T, DP, NW * 64> keys;
         keys.load(l, wave, z, row0, hk, live);
-        keys.finish(l, wave, z, s.K, s.Q, s.inv_k, s.inv_q);
+        keys.finish(l, wave, z, s.K, s.Q, s.lengths);
     }
     // this wavefront's tiles of dQ and dK
     const int dt = wave % DT, rt0 = wave / DT * RT;
@@ -933,7 +1025,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
         if (wave == 0) load_gates(l, z, row0, bias, h, live, s.g);
         lds_barrier();
         f32x4 tile[KEEP], acc[KEEP];
-        make_tiles<DP, NW, 2 * kTiles>(l, wave, s.g, s.K, s.Q, s.A, s.P, tile);
+        make_tiles<T, DP, NW, 2 * kTiles>(l, wave, s.g, s.lengths, s.K, s.Q, s.A, s.P, tile);
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) acc[i] = zero;
         lds_barrier();
@@ -947,12 +1039,12 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             const int mine = 16 * (wave & 3) + lc, col = v0 + mine;
             f32x4 R[4], X[4];
             values_of<T>(raw, R);
+            Operand<T, DT> state;
+            state.set(S);
             if (wave < 4) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    X[b] = zero;
-#pragma unroll
-                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(l, s.K, LD, 16 * b, 16 * k), S[k], X[b]);
+                    X[b] = in_products<T>(l, times(l, s.K, LD, 16 * b, state, zero), s.lengths.k, 16 * b);
                     R[b] -= rows_of(l, s.g.in, 16 * b) * X[b];
                     X[b] = rows_of(l, s.g.beta, 16 * b) * R[b];
                     fence();
@@ -960,10 +1052,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             } else {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    X[b] = zero;
-#pragma unroll
-                    for (int k = 0; k < DT; ++k) X[b] = multiply(frag(l, s.K, LD, 16 * b, 16 * k), S[k], X[b]);
-                    X[b] *= rows_of(l, s.g.out, 16 * b);
+                    X[b] = rows_of(l, s.g.out, 16 * b) * in_products<T>(l, times(l, s.K, LD, 16 * b, state, zero), s.lengths.k, 16 * b);
 #pragma unroll
                     for (int i = b; i < 4; ++i) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * i), R[i], X[b]);
                     fence();
@@ -1074,9 +1163,11 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             f32x4 k, q;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                k[r] = s.K[(16 * b + g4 + r) * LD + 16 * dt + lc];
-                q[r] = s.Q[(16 * b + g4 + r) * LD + 16 * dt + lc];
+                k[r] = (float)s.K[(16 * b + g4 + r) * LD + 16 * dt + lc];
+                q[r] = (float)s.Q[(16 * b + g4 + r) * LD + 16 * dt + lc];
             }
+            k = in_products<T>(l, k, s.lengths.k, 16 * b);
+            q = in_products<T>(l, q, s.lengths.unit_q, 16 * b);
             const f32x4 ek = sum_columns(e * k), dot = sum_columns(k1 * k + q1 * q);
             if (lc == 0) {
                 *(f32x4 *)&s.t.ends[dt][16 * b + g4] = ek;
@@ -1098,14 +1189,14 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             anew();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x4 k = frag_t(l, s.K, LD, 16 * dt, 16 * j);
+                const f32x4 k = rows_t(l, s.K, LD, 16 * dt, 16 * j, s.lengths.k);
                 if (j <= b) {
                     dK[i] = multiply(frag(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
                     dQ[i] = multiply(frag(l, s.P, kLA, 16 * b, 16 * j), k, dQ[i]);
                 }
                 if (j >= b) {
                     dK[i] = multiply(frag_t(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
-                    dK[i] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), frag_t(l, s.Q, LD, 16 * dt, 16 * j), dK[i]);
+                    dK[i] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), rows_t(l, s.Q, LD, 16 * dt, 16 * j, s.lengths.unit_q), dK[i]);
                 }
             }
         }
@@ -1157,9 +1248,11 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
         f32x4 k, q;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            k[r] = s.K[(16 * (rt0 + i) + g4 + r) * LD + 16 * dt + lc];
-            q[r] = s.Q[(16 * (rt0 + i) + g4 + r) * LD + 16 * dt + lc];
+            k[r] = (float)s.K[(16 * (rt0 + i) + g4 + r) * LD + 16 * dt + lc];
+            q[r] = (float)s.Q[(16 * (rt0 + i) + g4 + r) * LD + 16 * dt + lc];
         }
+        k = in_products<T>(l, k, s.lengths.k, 16 * (rt0 + i));
+        q = in_products<T>(l, q, s.lengths.unit_q, 16 * (rt0 + i));
         const f32x4 kk = sum_columns(dK[i] * k), qq = sum_columns(dQ[i] * q);
         if (lc == 0) {
             *(f32x4 *)&s.t.ends[dt][16 * (rt0 + i) + g4] = kk;
@@ -1181,8 +1274,9 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             }
             if (row >= rows || d >= z.D) continue;
             T *p = out0 + row * z.gi_t;
-            p[k_at(z, hk) + d] = (T)(row < live ? s.inv_k[row] * (dK[i][r] - s.K[row * LD + d] * kk) : 0.f);
-            p[q_at(z, hk) + d] = (T)(row < live ? s.inv_q[row] * unit * (dQ[i][r] - width * s.Q[row * LD + d] * qq) : 0.f);
+            const float k = (float)s.K[row * LD + d] * (sizeof(T) == 2 ? s.lengths.k[row] : 1.f), q = (float)s.Q[row * LD + d] * (sizeof(T) == 2 ? s.lengths.unit_q[row] : 1.f);
+            p[k_at(z, hk) + d] = (T)(row < live ? s.lengths.k[row] * (dK[i][r] - k * kk) : 0.f);
+            p[q_at(z, hk) + d] = (T)(row < live ? s.lengths.q[row] * unit * (dQ[i][r] - width * q * qq) : 0.f);
         }
 }
 
@@ -1393,7 +1487,7 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
         typedef decltype(one) T;
         return with_sizes(z, [&](auto dt, auto nw) {
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
-            const size_t bytes = sizeof(Shared<DT>);
+            const size_t bytes = sizeof(Shared<T, DT>);
             int allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
             if (allowed == NSK_OK) allowed = allow_lds<delta_matrices_kernel<T, DT, NW, false>>(bytes);
             if (allowed == NSK_OK) allowed = allow_lds<delta_out_kernel<T, DT, NW>>(bytes);
@@ -1433,8 +1527,8 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
         typedef decltype(one) T;
         return with_sizes(z, [&](auto dt, auto nw) {
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
-            const size_t bytes = sizeof(Shared<DT>), grad_bytes = sizeof(GradShared<DT>);
-            static_assert(sizeof(GradShared<DT>) <= 160 * 1024, "what a compute unit has");
+            const size_t bytes = sizeof(Shared<T, DT>), grad_bytes = sizeof(GradShared<T, DT>);
+            static_assert(sizeof(GradShared<T, DT>) <= 160 * 1024, "what a compute unit has");
             int allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
             if (allowed == NSK_OK) allowed = allow_lds<delta_matrices_kernel<T, DT, NW, true>>(bytes);
             if (allowed == NSK_OK) allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);

@@ -86,7 +86,8 @@ struct Pieces {
     bf16x8 h, m, l;
 };
 constexpr float kPieceScale = 16777216.f, kSumScale = kPieceScale * kPieceScale;
-__device__ __forceinline__ Pieces split3(const float (&x)[8])
+// SCALED = false: without the 2^24, where the other operand is bf16 itself and its products need no room; of |x| < 2^-110 the last piece then leaves the range.
+template <bool SCALED = true> __device__ __forceinline__ Pieces split3(const float (&x)[8])
 {
     typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
     struct Quad {
@@ -94,7 +95,7 @@ __device__ __forceinline__ Pieces split3(const float (&x)[8])
     } h, m, l;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float a = x[2 * i] * kPieceScale, b = x[2 * i + 1] * kPieceScale;
+        const float a = SCALED ? x[2 * i] * kPieceScale : x[2 * i], b = SCALED ? x[2 * i + 1] * kPieceScale : x[2 * i + 1];
         bf16x2 p;
         p[0] = (bf16_t)a;
         p[1] = (bf16_t)b;
