@@ -1327,8 +1327,7 @@ def delta_fwd(gi, heads, bias=None, h0=None, lengths=None, o=None, h_last=None, 
     _floats(bias, 2 * H), _floats(h0, N, H, D, Dv)
     ot, on, _ = (0, 0, 1) if o is None else o.stride()
     d, need = _delta_call(T, N, tuple(heads), _dtype_code(gi), gt, gn, ot, on, NSK_PASS_FWD)
-    ws = ws or Workspace(dev)
-    wp, wb = ws.get(need)
+    wp, wb = (ws or Workspace(dev)).get(need) if need else (None, 0)
     _check(lib().nsk_delta_fwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(h0), _rows_ptr(o), _ptr(h_last), _ptr(saved), wp, wb, _stream()),
            "nsk_delta_fwd")
     return o, h_last, saved
@@ -1353,8 +1352,7 @@ def delta_bwd(gi, saved, heads, bias=None, do=None, dh_last=None, lengths=None, 
     gt, gn, _ = strides
     ot, on, _ = (0, 0, 1) if do is None else do.stride()
     d, need = _delta_call(T, N, tuple(heads), _dtype_code(gi), gt, gn, ot, on, NSK_PASS_DGRAD)
-    ws = ws or Workspace(dev)
-    wp, wb = ws.get(need)
+    wp, wb = (ws or Workspace(dev)).get(need) if need else (None, 0)
     _check(lib().nsk_delta_bwd(d, _rows_ptr(gi), _ptr(bias), _lengths_ptr(lengths, N), _ptr(saved), _rows_ptr(do), _ptr(dh_last), dgi.data_ptr(), _ptr(dh0),
                                wp, wb, _stream()), "nsk_delta_bwd")
     return dgi, dh0
@@ -1395,31 +1393,36 @@ def _distill_args(logits, top_index, top_logits, tau, weights):
     N, K = logits.shape
     M = top_index.shape[-1]
     _floats(top_logits, N, M), _floats(weights, N)
-    d, need = _distill_call(N, K, M, _dtype_code(logits), logits.stride(0) if N > 1 else 0, float(tau))
-    return need, (d, _logits_ptr(logits), _ints(top_index, N, M), _ptr(top_logits), _ptr(weights))
+    d, need = _distill_call(N, K, M, _dtype_code(logits), logits.stride(0) if N > 1 else 0, tau)
+    return N, need, (d, _logits_ptr(logits), _ints(top_index, N, M), _ptr(top_logits), _ptr(weights))
 
 
 def distill_fwd(logits, top_index, top_logits, tau=1.0, weights=None, per_row=None, loss=None, saved=None, ws: Optional[Workspace] = None):
     """The loss of logits [N,K] (rows may have room between them) against a teacher's largest: top_index int32 [N,M] (negative: no place), top_logits float
     [N,M]; weights: float [N] or None.  Returns (loss [1], per_row [N], saved [N+1,2]), float; saved is what distill_bwd reads."""
-    N, dev = logits.shape[0], logits.device
-    need, args = _distill_args(logits, top_index, top_logits, tau, weights)
-    _floats(per_row, N), _floats(loss, 1), _floats(saved, N + 1, 2)
+    N, need, args = _distill_args(logits, top_index, top_logits, tau, weights)
+    dev = logits.device
     if per_row is None:
         per_row = torch.empty(N, dtype=torch.float32, device=dev)
+    else:
+        _floats(per_row, N), _ptr(per_row)
     if loss is None:
         loss = torch.empty(1, dtype=torch.float32, device=dev)
+    else:
+        _floats(loss, 1), _ptr(loss)
     if saved is None:
         saved = torch.empty(N + 1, 2, dtype=torch.float32, device=dev)
-    wp, wb = (ws or Workspace(dev)).get(need)
-    _check(lib().nsk_distill_fwd(*args, _ptr(per_row), _ptr(loss), _ptr(saved), wp, wb, _stream()), "nsk_distill_fwd")
+    else:
+        _floats(saved, N + 1, 2), _ptr(saved)
+    wp, wb = (ws or Workspace(dev)).get(need) if need else (None, 0)
+    _check(lib().nsk_distill_fwd(*args, per_row.data_ptr(), loss.data_ptr(), saved.data_ptr(), wp, wb, _stream()), "nsk_distill_fwd")
     return loss, per_row, saved
 
 
 def distill_bwd(logits, top_index, top_logits, saved, tau=1.0, dloss=1.0, weights=None, out=None, accumulate=False):
     """Gradient of the logits, whose rows lie as theirs; out may be logits itself unless it is added to."""
-    _, args = _distill_args(logits, top_index, top_logits, tau, weights)
-    _floats(saved, logits.shape[0] + 1, 2)
+    N, _, args = _distill_args(logits, top_index, top_logits, tau, weights)
+    _floats(saved, N + 1, 2)
     if out is None:
         assert not accumulate
         out = torch.empty_like(logits)

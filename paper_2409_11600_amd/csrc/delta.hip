@@ -652,6 +652,118 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T 
     if (h_last) store_state(l, z, h_last + own, col, S);
 }
 
+// The same where the columns of a head fit four wavefronts and LDS two chunks: four more wavefronts prepare the next chunk (K, Q, A, P, the inverses, none of which needs a state) while the
+// first four go through this one.  Both meet three times a chunk, where the others' stages are about as long.
+template <typename T, int DT> struct Preparing {
+    static constexpr int DP = 16 * DT, WAVES = 4;
+    KeyParts<T, DP, WAVES * 64> keys;
+    GateParts<T> gates;
+    __device__ __forceinline__ void load(int l, int wave, const Sizes &z, const T *row0, int h, int hk, int live)
+    {
+        keys.load(l, wave, z, row0, hk, live);
+        if (wave == 0) gates.load(l, z, row0, h, live);
+    }
+    __device__ __forceinline__ void rows(int l, int wave, const Sizes &z, const float *bias, int h, int live, Shared<T, DT> &s) const
+    {
+        keys.finish(l, wave, z, s.K, s.Q, s.lengths);
+        if (wave == 0) gates.finish(l, z, bias, h, live, s.g);
+    }
+    static __device__ __forceinline__ void tiles(int l, int wave, Shared<T, DT> &s)
+    {
+        f32x4 x[2 * kTiles / WAVES];
+        make_tiles<T, DP, WAVES, 2 * kTiles>(l, wave, s.g, s.lengths, s.K, s.Q, s.A, s.P, x);
+    }
+};
+template <typename T, int DT> constexpr bool kFlows = 2 * sizeof(Shared<T, DT>) <= 160 * 1024;
+constexpr int kFlowThreads = 512;
+// The preparing wavefronts' part, for chunk(i), i = 0, 1, .. count - 1.
+template <typename T, int DT, typename F>
+__device__ __forceinline__ void prepare(const Sizes &z, int wave, const T *rows, const float *bias, int h, int hk, int len, int count, Shared<T, DT> *s, F &&chunk)
+{
+    Preparing<T, DT> p;
+    auto live = [&](int i) { return len - chunk(i) * kC < kC ? len - chunk(i) * kC : kC; };
+    auto row0 = [&](int i) { return rows + chunk(i) * kC * z.gi_t; };
+    if (count > 0) p.load(fresh_lane(), wave, z, row0(0), h, hk, live(0));
+    for (int i = 0; i <= count; ++i) {          // (in step i chunk i is prepared, and the others go through chunk i - 1)
+        const int l = fresh_lane();
+        const bool there = i < count;
+        Shared<T, DT> &to = s[i & 1];
+        if (there) p.rows(l, wave, z, bias, h, live(i), to);
+        if (i + 1 < count) p.load(l, wave, z, row0(i + 1), h, hk, live(i + 1));
+        fence();
+        lds_barrier();
+        if (there) p.tiles(l, wave, to);
+        lds_barrier();
+        if (there) invert_block(l, to.A, wave);
+        lds_barrier();
+    }
+}
+template <typename T, int DT>
+__global__ __launch_bounds__(kFlowThreads, 2) void delta_flow_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
+                                                                     T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
+{
+    typedef Shared<T, DT> Lds;
+    constexpr int LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds *both_s = (Lds *)lds;
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = steps_of(z, lengths, n), used = (len + kC - 1) / kC;
+    const T *rows0 = gi + n * z.gi_n;
+    if (wave >= 4) return prepare<T, DT>(z, wave - 4, rows0, bias, h, hk, len, used, both_s, [](int i) { return i; });
+    int l = fresh_lane();
+    const int col = wave * 16 + (l & 15);
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 S[DT];
+    load_state(l, z, h0 ? h0 + own : nullptr, col, S);
+    Raw v;
+    auto fetch = [&](int c) { load_rows(l, z, rows0 + c * kC * z.gi_t + v_at(z, h), z.gi_t, len - c * kC < kC ? len - c * kC : kC, col, v); };
+    if (used > 0) fetch(0);
+    lds_barrier();
+    lds_barrier();
+    lds_barrier();
+    for (int c = 0; c < used; ++c) {
+        l = fresh_lane();
+        const int t0 = c * kC, live = len - t0 < kC ? len - t0 : kC, rows = z.T - t0 < kC ? z.T - t0 : kC;
+        const Lds &s = both_s[c & 1];
+        if (saved) store_state(l, z, saved + state_at(z, c, n, h), col, S);
+        f32x4 X[4];
+        values_of<T>(v, X);
+        if (c + 1 < used) fetch(c + 1);
+        Operand<T, DT> state;
+        state.set(S);
+        below_state(l, s, state, X);
+        settle(X);
+        lds_barrier();
+        solve(l, s.A, X);
+        settle(X);
+        if (o) {
+            f32x4 O[4];
+            answers(l, s, state, X, O);
+            store_rows(l, z, o + t0 * z.o_t + n * z.o_n + h * z.Dv, z.o_t, live, rows, col, O);
+        }
+        lds_barrier();
+#pragma unroll
+        for (int b = 0; b < 4; ++b) X[b] *= in_products<T>(l, rows_of(l, s.g.out, 16 * b), s.lengths.k, 16 * b);
+        Operand<T, 4> written;
+        written.set(X);
+        const float all = s.g.all;
+#pragma unroll
+        for (int k = 0; k < DT; ++k) {
+            S[k] = times_t(l, s.K, LD, 16 * k, written, S[k] * all);
+            if (k & 1) fence();
+        }
+        settle(S);
+        lds_barrier();
+    }
+    for (int c = used; c < z.chunks; ++c) {
+        const int t0 = c * kC;
+        const f32x4 X[4] = {};
+        if (saved) store_state(l, z, saved + state_at(z, c, n, h), col, S);
+        if (o) store_rows(l, z, o + t0 * z.o_t + n * z.o_n + h * z.Dv, z.o_t, 0, z.T - t0 < kC ? z.T - t0 : kC, col, X);
+    }
+    if (h_last) store_state(l, z, h_last + own, col, S);
+}
+
 // ----------------------------------------------------------------------------- all chunks at once
 // A chunk takes S to M S + B, and the gradient behind it to M^T G + B'.  Where heads are few, the chunks' M and B are made beside each other (the products above for a state of
 // D + Dv columns, the unit matrix and zeros), then a small product a chunk goes through the sequence, and then everything else is done for all chunks beside each other.
@@ -946,6 +1058,81 @@ __global__ __launch_bounds__(NW * 64, 2) void delta_ends_kernel(Sizes z, const T
     if (dh0) store_state(l, z, dh0 + own, col, G);
 }
 
+// The same with the next chunk prepared meanwhile.
+template <typename T, int DT>
+__global__ __launch_bounds__(kFlowThreads, 2) void delta_ends_flow_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths,
+                                                                          const T *__restrict__ d_o, const float *__restrict__ dh_last, float *__restrict__ dh0, float *__restrict__ ends)
+{
+    typedef Shared<T, DT> Lds;
+    constexpr int LD = Lds::LD;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Lds *both_s = (Lds *)lds;
+    const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, hk = h / (z.H / z.Hk), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = steps_of(z, lengths, n), used = (len + kC - 1) / kC, count = dh0 ? used : used - 1;       // the first chunk's product is that of dh0
+    auto chunk = [&](int i) { return used - 1 - i; };
+    if (wave >= 4) return prepare<T, DT>(z, wave - 4, gi + n * z.gi_n, bias, h, hk, len, count, both_s, chunk);
+    int l = fresh_lane();
+    const int col = wave * 16 + (l & 15);
+    const size_t own = state_at(z, 0, n, h);
+    f32x4 G[DT];
+    load_state(l, z, dh_last ? dh_last + own : nullptr, col, G);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    Raw raw;
+    auto fetch = [&](int i) {
+        const int t0 = chunk(i) * kC;
+        load_rows(l, z, d_o ? d_o + t0 * z.o_t + n * z.o_n + h * z.Dv : nullptr, z.o_t, len - t0 < kC ? len - t0 : kC, col, raw);
+    };
+    if (count > 0) fetch(0);
+    if (count >= 0) {
+        lds_barrier();
+        lds_barrier();
+        lds_barrier();
+    }
+    for (int i = 0; i < count; ++i) {
+        l = fresh_lane();
+        const Lds &s = both_s[i & 1];
+        store_state(l, z, ends + state_at(z, chunk(i), n, h), col, G);
+        f32x4 dO[4], X[4];
+        values_of<T>(raw, dO);
+        if (i + 1 < count) fetch(i + 1);
+        Operand<T, DT> behind;
+        behind.set(G);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            X[b] = rows_of(l, s.g.out, 16 * b) * in_products<T>(l, times(l, s.K, LD, 16 * b, behind, zero), s.lengths.k, 16 * b);
+            fence();
+        }
+        settle(X);
+        lds_barrier();
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int j = b; j < 4; ++j) X[b] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), dO[j], X[b]);
+        solve_t(l, s.A, X);
+        settle(X);
+        lds_barrier();
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 in = rows_of(l, s.g.in, 16 * b);
+            dO[b] *= in_products<T>(l, in, s.lengths.unit_q, 16 * b);
+            X[b] *= in_products<T>(l, -in * rows_of(l, s.g.beta, 16 * b), s.lengths.k, 16 * b);
+        }
+        Operand<T, 4> asked, written;
+        asked.set(dO);
+        written.set(X);
+        const float all = s.g.all;
+#pragma unroll
+        for (int k = 0; k < DT; ++k) {
+            G[k] = times_t(l, s.K, LD, 16 * k, written, times_t(l, s.Q, LD, 16 * k, asked, G[k] * all));
+            if (k & 1) fence();
+        }
+        settle(G);
+        lds_barrier();
+    }
+    if (count < used) store_state(l, z, ends + own, col, G);
+    if (dh0) store_state(l, z, dh0 + own, col, G);
+}
+
 // The gradients of a chunk's rows, given the states in front of and the gradients behind it.  A block takes a key head and the heads that share it, one after the other, so that
 // their gradients of q and k are summed in registers.  64 columns of the state at a time: four wavefronts make U, the other four X; then all make the products that reach over
 // the columns, each a tile column of dQ and dK and its tiles of dA and dP.
@@ -1041,7 +1228,11 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             values_of<T>(raw, R);
             Operand<T, DT> state;
             state.set(S);
-            if (wave < 4) {
+            const int blocks = z.Dv - v0 < 64 ? (z.Dv - v0 + 15) / 16 : 4;         // of 16 columns, this time
+            if ((wave & 3) >= blocks) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) X[b] = zero;
+            } else if (wave < 4) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     X[b] = in_products<T>(l, times(l, s.K, LD, 16 * b, state, zero), s.lengths.k, 16 * b);
@@ -1061,7 +1252,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             }
             if (v0 == 0) lds_barrier();         // (the inverses)
             anew();
-            if (wave < 4) {
+            if ((wave & 3) >= blocks) {
+            } else if (wave < 4) {
                 solve(l, s.A, X);
                 settle(X);
             } else {
@@ -1113,12 +1305,14 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
                 tile_at(t < kTiles ? t : t - kTiles, bi, bj);
                 const float *left = t < kTiles ? s.v.X : s.v.O;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[i] = multiply(frag(l, left, kLA, 16 * bi, 16 * k), frag(l, s.v.U, kLA, 16 * bj, 16 * k), acc[i]);
+                for (int k = 0; k < 4; ++k)
+                    if (k < blocks) acc[i] = multiply(frag(l, left, kLA, 16 * bi, 16 * k), frag(l, s.v.U, kLA, 16 * bj, 16 * k), acc[i]);
                 fence();
             }
             anew();
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+                if (k >= blocks) break;
                 if (rt0 == 0) both += (sf[k][0] * gf[k][0] + sf[k][1] * gf[k][1]) + (sf[k][2] * gf[k][2] + sf[k][3] * gf[k][3]);
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
@@ -1488,11 +1682,11 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
         return with_sizes(z, [&](auto dt, auto nw) {
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
             const size_t bytes = sizeof(Shared<T, DT>);
-            int allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
-            if (allowed == NSK_OK) allowed = allow_lds<delta_matrices_kernel<T, DT, NW, false>>(bytes);
-            if (allowed == NSK_OK) allowed = allow_lds<delta_out_kernel<T, DT, NW>>(bytes);
-            if (allowed != NSK_OK) return allowed;
+            int allowed = NSK_OK;
             if (at_once(z)) {
+                allowed = allow_lds<delta_matrices_kernel<T, DT, NW, false>>(bytes);
+                if (allowed == NSK_OK) allowed = allow_lds<delta_out_kernel<T, DT, NW>>(bytes);
+                if (allowed != NSK_OK) return allowed;
                 const unsigned all = (unsigned)(z.chunks * z.N * z.H);
                 hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, false>), dim3(all, (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)), dim3(NW * 64), bytes, st, z,
                                    (const T *)gi, bias, lengths, (const T *)nullptr, matrices);
@@ -1501,8 +1695,16 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
                     hipLaunchKernelGGL((delta_out_kernel<T, DT, NW>), dim3(all, (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, states, (T *)o);
                 return check_launch();
             }
-            hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0, (T *)o,
-                               h_last, saved);
+            if constexpr (kFlows<T, DT> && NW == 4) {
+                allowed = allow_lds<delta_flow_kernel<T, DT>>(2 * bytes);
+                if (allowed != NSK_OK) return allowed;
+                hipLaunchKernelGGL((delta_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths, h0, (T *)o, h_last, saved);
+            } else {
+                allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
+                if (allowed != NSK_OK) return allowed;
+                hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0,
+                                   (T *)o, h_last, saved);
+            }
             return check_launch();
         });
     };
@@ -1529,15 +1731,22 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
             const size_t bytes = sizeof(Shared<T, DT>), grad_bytes = sizeof(GradShared<T, DT>);
             static_assert(sizeof(GradShared<T, DT>) <= 160 * 1024, "what a compute unit has");
-            int allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
-            if (allowed == NSK_OK) allowed = allow_lds<delta_matrices_kernel<T, DT, NW, true>>(bytes);
-            if (allowed == NSK_OK) allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);
+            int allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);
             if (allowed != NSK_OK) return allowed;
             if (at_once(z)) {
+                allowed = allow_lds<delta_matrices_kernel<T, DT, NW, true>>(bytes);
+                if (allowed != NSK_OK) return allowed;
                 hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, true>), dim3((unsigned)(z.chunks * z.N * z.H), (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)),
                                    dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, (const T *)d_o, matrices);
                 scan<DT, true>(z, p, lengths, (char *)workspace, dh_last, ends, dh0, st);
+            } else if constexpr (kFlows<T, DT> && NW == 4) {
+                allowed = allow_lds<delta_ends_flow_kernel<T, DT>>(2 * bytes);
+                if (allowed != NSK_OK) return allowed;
+                hipLaunchKernelGGL((delta_ends_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths, (const T *)d_o, dh_last, dh0,
+                                   ends);
             } else {
+                allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
+                if (allowed != NSK_OK) return allowed;
                 hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,
                                    (const T *)d_o, dh_last, dh0, ends);
             }
