@@ -860,78 +860,111 @@ __global__ __launch_bounds__(NW * 64) void delta_matrices_kernel(Sizes z, const 
 // A chunk takes 2 us, which nothing hides where the blocks are few and the sequence long.  Then it is cut into segments (blockIdx.z): Compose makes the M and B of each, the columns of the
 // unit matrix and of no state; Jump goes from segment to segment; Fill goes through each from the state that enters it.
 enum class Scan { Whole, Compose, Jump, Fill };
+// Where blocks are many, one takes two groups of 16 columns and reads M once for both (T=16384, N=1, 4 heads of 128 x 128, us of Compose / Fill with one group 133 / 69, with two 97 / 56).
+template <Scan MODE> constexpr int kColumnTiles = MODE == Scan::Compose || MODE == Scan::Fill ? 2 : 1;
 template <int DT, bool BACK, Scan MODE>
 __global__ __launch_bounds__(DT * 64) void delta_scan_kernel(Sizes z, const int *__restrict__ lengths, const float *__restrict__ matrices, const float *__restrict__ first,
                                                              float *__restrict__ states, float *__restrict__ last, int segment)
 {
-    constexpr int DP = 16 * DT, LD = DP + 4;
-    __shared__ __attribute__((aligned(16))) float lds[2][16 * LD];
+    constexpr int DP = 16 * DT, LD = DP + 4, CT = kColumnTiles<MODE>;
+    constexpr bool CUT = MODE == Scan::Compose || MODE == Scan::Fill;
+    __shared__ __attribute__((aligned(16))) float lds[2][CT][16 * LD];
     const int n = blockIdx.x / z.H, h = blockIdx.x - n * z.H, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = fresh_lane(), lc = l & 15, g4 = 4 * (l >> 4);
-    const int units = (z.D + 15) / 16, tile = blockIdx.y, len = steps_of(z, lengths, n), used = (len + kC - 1) / kC;
-    const bool vec = z.D % 4 == 0, unit = MODE == Scan::Compose && tile < units;
-    const int col = (MODE == Scan::Compose && !unit ? tile - units : tile) * 16 + lc, row = 16 * wave + g4, width = unit ? z.D : z.Dv;
+    const int units = (z.D + 15) / 16, len = steps_of(z, lengths, n), used = (len + kC - 1) / kC, row = 16 * wave + g4;
+    const bool vec = z.D % 4 == 0;
     // the items of the sequence (chunks, or segments) that this block goes through
-    const int items = MODE == Scan::Jump ? (used + segment - 1) / segment : used, number = (MODE == Scan::Compose || MODE == Scan::Fill) ? blockIdx.z : 0;
-    const int from = number * segment * (MODE == Scan::Compose || MODE == Scan::Fill), to = MODE == Scan::Compose || MODE == Scan::Fill ? (items - from < segment ? items : from + segment) : items;
+    const int items = MODE == Scan::Jump ? (used + segment - 1) / segment : used, number = CUT ? blockIdx.z : 0, from = CUT ? number * segment : 0;
+    const int to = CUT && items - from > segment ? from + segment : items;
     const bool ends = to >= items;
     if (from >= items && (MODE == Scan::Compose || from > 0)) return;
     if (MODE == Scan::Compose && ends) return;          // (nothing comes behind it)
     const size_t own = state_at(z, 0, n, h);
-    f32x4 S;
+    f32x4 S[CT];
     struct Chunk {
-        f32x4 M[DT], B;
+        f32x4 M[DT], B[CT];
     };
     Chunk chunk[2];
-    const unsigned at = col < width ? (unsigned)(row * width + col) * 4 : kNowhere;
-    auto get = [&](const float *p, f32x4 &x) {
-        const __amdgpu_buffer_rsrc_t b = buffer(p, p ? z.D * width * 4 : 0);
+    // each group's columns: of the unit matrix in front (Compose), or of the state
+    bool unit[CT];
+    int col[CT], width[CT];
+    unsigned at[CT];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = value_of<float>(load_raw<float>(b, at + r * width * 4));
+    for (int t = 0; t < CT; ++t) {
+        const int tile = blockIdx.y * CT + t;
+        unit[t] = MODE == Scan::Compose && tile < units;
+        col[t] = (MODE == Scan::Compose && !unit[t] ? tile - units : tile) * 16 + lc;
+        width[t] = unit[t] ? z.D : z.Dv;
+        at[t] = col[t] < width[t] ? (unsigned)(row * width[t] + col[t]) * 4 : kNowhere;
+    }
+    auto get = [&](const float *p, int t, f32x4 &x) {
+        const __amdgpu_buffer_rsrc_t b = buffer(p, p ? z.D * width[t] * 4 : 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = value_of<float>(load_raw<float>(b, at[t] + r * width[t] * 4));
     };
-    auto put = [&](float *p) {
-        const __amdgpu_buffer_rsrc_t b = buffer(p, z.D * width * 4);
+    auto put = [&](float *p, int t) {
+        const __amdgpu_buffer_rsrc_t b = buffer(p, z.D * width[t] * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) store<float>(S[r], b, at + r * width * 4);
+        for (int r = 0; r < 4; ++r) store<float>(S[t][r], b, at[t] + r * width[t] * 4);
+    };
+    auto put_all = [&](float *p) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) put(p, t);
     };
     auto item = [&](int i) { return BACK && MODE != Scan::Jump ? used - 1 - i : i; };
     auto fetch = [&](int i, Chunk &x) {
         const float *m = matrices + matrices_at(z, item(i), n, h);
 #pragma unroll
         for (int k = 0; k < DT; ++k) x.M[k] = frag_of(l, m, z.D, 16 * wave, z.D, 16 * k, vec);
-        get(unit ? nullptr : m + (size_t)z.D * z.D, x.B);
-    };
-    if (MODE == Scan::Compose) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[r] = unit && row + r == col ? 1.f : 0.f;
-    } else {
-        get(MODE == Scan::Fill ? first + state_at(z, number, n, h) : first ? first + own : nullptr, S);
+        for (int t = 0; t < CT; ++t) get(unit[t] ? nullptr : m + (size_t)z.D * z.D, t, x.B[t]);
+    };
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+        if (MODE == Scan::Compose) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = unit[t] && row + r == col[t] ? 1.f : 0.f;
+        } else {
+            get(MODE == Scan::Fill ? first + state_at(z, number, n, h) : first ? first + own : nullptr, t, S[t]);
+        }
     }
     // the last product only if what it makes is wanted
     const int stop = MODE == Scan::Compose || (ends && last) ? to : to - 1;
     auto step = [&](int i, const Chunk &now, Chunk &next) {
-        if (MODE != Scan::Compose) put(states + state_at(z, item(i), n, h));
+        if (MODE != Scan::Compose) put_all(states + state_at(z, item(i), n, h));
         if (i >= stop) return;
         if (i + 1 < stop) fetch(i + 1, next);
-        float *to_lds = lds[i & 1];
-        *(f32x4 *)(to_lds + lc * LD + row) = S;
-        lds_barrier();
-        f32x4 acc[2] = {now.B, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int k = 0; k < DT; ++k) acc[k & 1] = multiply(now.M[k], *(const f32x4 *)(to_lds + lc * LD + 16 * k + g4), acc[k & 1]);
+        for (int t = 0; t < CT; ++t) *(f32x4 *)(lds[i & 1][t] + lc * LD + row) = S[t];
+        lds_barrier();
+        f32x4 acc[2 * CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            acc[2 * t] = now.B[t];
+            acc[2 * t + 1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < DT; ++k)
+#pragma unroll
+            for (int t = 0; t < CT; ++t) acc[2 * t + (k & 1)] = multiply(now.M[k], *(const f32x4 *)(lds[i & 1][t] + lc * LD + 16 * k + g4), acc[2 * t + (k & 1)]);
         settle(acc);
-        S = acc[0] + acc[1];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) S[t] = acc[2 * t] + acc[2 * t + 1];
     };
     if (stop > from) fetch(from, chunk[0]);
     for (int i = from; i < to; i += 2) {
         step(i, chunk[0], chunk[1]);
         if (i + 1 < to) step(i + 1, chunk[1], chunk[0]);
     }
-    if (MODE == Scan::Compose) return put(states + matrices_at(z, number, n, h) + (unit ? 0 : (size_t)z.D * z.D));
-    if (MODE == Scan::Jump && items == 0) put(states + state_at(z, 0, n, h));        // (a sequence of no step: what enters it leaves it)
+    if (MODE == Scan::Compose) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) put(states + matrices_at(z, number, n, h) + (unit[t] ? 0 : (size_t)z.D * z.D), t);
+        return;
+    }
+    if (MODE == Scan::Jump && items == 0) put_all(states + state_at(z, 0, n, h));        // (a sequence of no step: what enters it leaves it)
     if (MODE == Scan::Jump || !ends) return;
     if (!BACK)
-        for (int c = used; c < z.chunks; ++c) put(states + state_at(z, c, n, h));
-    if (last) put(last + own);
+        for (int c = used; c < z.chunks; ++c) put_all(states + state_at(z, c, n, h));
+    if (last) put_all(last + own);
 }
 
 // What the chunks answer, given the states in front of them.
@@ -1377,20 +1410,20 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             if (l == 0) s.t.states[dt] = both;
         }
         lds_barrier();
+        anew();
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int b = rt0 + i;
-            anew();
+        for (int j = 0; j < 4; ++j) {
+            const f32x4 k = rows_t(l, s.K, LD, 16 * dt, 16 * j, s.lengths.k), q = rows_t(l, s.Q, LD, 16 * dt, 16 * j, s.lengths.unit_q);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x4 k = rows_t(l, s.K, LD, 16 * dt, 16 * j, s.lengths.k);
+            for (int i = 0; i < RT; ++i) {
+                const int b = rt0 + i;
                 if (j <= b) {
                     dK[i] = multiply(frag(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
                     dQ[i] = multiply(frag(l, s.P, kLA, 16 * b, 16 * j), k, dQ[i]);
                 }
                 if (j >= b) {
                     dK[i] = multiply(frag_t(l, s.A, kLA, 16 * b, 16 * j), k, dK[i]);
-                    dK[i] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), rows_t(l, s.Q, LD, 16 * dt, 16 * j, s.lengths.unit_q), dK[i]);
+                    dK[i] = multiply(frag_t(l, s.P, kLA, 16 * b, 16 * j), q, dK[i]);
                 }
             }
         }
@@ -1628,10 +1661,10 @@ template <int DT, bool BACK> void scan(const Sizes &z, const Plan &p, const int 
         return;
     }
     float *composed = (float *)(workspace + p.composed), *between = (float *)(workspace + p.between);
-    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Compose>), dim3(heads, both, (unsigned)p.segments), block, 0, st, z, lengths, matrices, (const float *)nullptr, composed,
+    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Compose>), dim3(heads, (both + kColumnTiles<Scan::Compose> - 1) / kColumnTiles<Scan::Compose>, (unsigned)p.segments), block, 0, st, z, lengths, matrices, (const float *)nullptr, composed,
                        (float *)nullptr, p.segment);
     hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Jump>), dim3(heads, columns), block, 0, st, z, lengths, composed, first, between, (float *)nullptr, p.segment);
-    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Fill>), dim3(heads, columns, (unsigned)p.segments), block, 0, st, z, lengths, matrices, between, states, last, p.segment);
+    hipLaunchKernelGGL((delta_scan_kernel<DT, BACK, Scan::Fill>), dim3(heads, (columns + kColumnTiles<Scan::Fill> - 1) / kColumnTiles<Scan::Fill>, (unsigned)p.segments), block, 0, st, z, lengths, matrices, between, states, last, p.segment);
 }
 size_t saved_of(const Sizes &z) { return (size_t)z.chunks * z.N * z.H * z.D * z.Dv * sizeof(float); }
 
