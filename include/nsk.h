@@ -587,9 +587,10 @@ int nsk_embedding_scaled_bwd(int dtype, int n, int E, int V, const int *tokens, 
  *   S' = alpha S_{t-1},  S_t = S' + k^ (beta * (v - S'^T k^))^T,  o_t = S_t^T q^.
  * In later steps S stays, o and the gradients are zero and gi, d_o are not used, whatever they hold.  A length below 0 counts as 0,
  * one above T as T.  States are float throughout.  Steps are taken in chunks of 64: where a value of a step is not finite, so may be what
- * is returned for other steps of its chunk.
+ * is returned for other steps of its chunk.  (|q|^2 and |k|^2 are floats: rows longer than 1.8e19 have no length.)
  * Rows of W (gi, dgi) and H*Dv (o, d_o) elements are contiguous; strides as in nsk_glr_desc_t.  D and Dv are at most 128; multiples of
- * 8 with strides that are multiples of 16 bytes are loaded in vectors. */
+ * 8 with strides that are multiples of 16 bytes are loaded in vectors.  From a step to the next there are fewer than 2^25 elements.
+ * h_last may be the buffer of h0 and dh0 that of dh_last; other buffers do not overlap. */
 #define NSK_DELTA_CHUNK 64
 #define NSK_DELTA_EPS 1e-6f
 typedef struct {
@@ -634,8 +635,8 @@ typedef struct {
 } nsk_distill_desc_t;
 /* Workspace of nsk_distill_fwd; may be 0 (0 also for an invalid descriptor).  Host only. */
 size_t nsk_distill_workspace_bytes(const nsk_distill_desc_t *desc);
-/* per_row: float [N], loss: float [1].  saved: float [N+1][2], for the backward pass: of each row the largest logit / tau and
- * 1 / sum_k exp(logits / tau - it) (0 and 0 where the weight is 0), then sum_n w_n and its reciprocal (0 where it is 0).  Fixed order of summation. */
+/* per_row: float [N], loss: float [1].  saved: float [N+1][2], for the backward pass: of each row the largest logit / tau, rounded, and
+ * 1 / sum_k exp(logits / tau - it) with it as rounded (0 and 0 where the weight is 0), then sum_n w_n and its reciprocal (0 where it is 0).  Fixed order of summation. */
 int nsk_distill_fwd(const nsk_distill_desc_t *desc, const void *logits, const int *top_index, const float *top_logits,
                     const float *weights, float *per_row, float *loss, float *saved, void *workspace, size_t workspace_bytes, void *stream);
 /* dlogits[n][k] (+)= dloss * w_n / sum(w) * tau * (q[k] - sum of p_m over the places with index k), rounded once; columns from K to ld stay.

@@ -1633,7 +1633,14 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
 }
 // The workspace: the states (or gradients) of all chunks; where the chunks are taken all at once their matrices; where the sequence is cut into segments theirs, and the states between them.
 bool at_once(const Sizes &z) { return z.chunks > 2 && (long long)z.N * z.H < 192; }
-int segment_of(const Sizes &z) { return z.chunks >= 48 && (long long)z.N * z.H * ceil_div(z.Dv, 16) <= 256 ? z.chunks > 512 ? 32 : 16 : 0; }
+// (Compose and Fill take a step a chunk of a segment, Jump one a segment: segments about as many as twice their chunks.)
+int segment_of(const Sizes &z)
+{
+    if (z.chunks < 48 || (long long)z.N * z.H * ceil_div(z.Dv, 16) > 256) return 0;
+    int s = 16;
+    while ((long long)z.chunks > 2LL * s * s) s *= 2;
+    return s;
+}
 size_t saved_of(const Sizes &z);
 struct Plan {
     int segment, segments;

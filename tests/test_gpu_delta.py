@@ -265,6 +265,34 @@ def test_same_bits_and_beside_each_other():
         assert all(torch.equal(a, b) for a, b in zip(r, want[i % len(want)]))
 
 
+@pytest.mark.parametrize("T,N,heads", [(150, 2, (2, 1, 32, 32)), (3100, 1, (2, 2, 16, 16)), (70, 100, (2, 2, 16, 16)), (70, 2, (2, 2, 16, 72))])
+def test_states_in_place(T, N, heads):
+    """The last state into the buffer of the first, and the gradient of the first into that of the last: what a sequence in parts does."""
+    c = case(T, N, heads)
+    g = gpu(c)
+    o, last, saved, dgi, dh0 = both(g, heads)
+    h, dh = g["h0"].clone(), g["dh_last"].clone()
+    again, _, _ = B.delta_fwd(g["gi"], heads, g["bias"], h0=h, h_last=h)
+    assert torch.equal(again, o) and torch.equal(h, last)
+    dgi2, _ = B.delta_bwd(g["gi"], saved, heads, g["bias"], do=g["do"], dh_last=dh, dh0=dh)
+    assert torch.equal(dgi2, dgi) and torch.equal(dh, dh0)
+
+
+def test_very_long():
+    """Two million chunks, offsets beyond 2^31 bytes.  Where alpha is 0.3 a step, what was 128 steps ago is 1e-67 of itself: windows of steps say what the outputs are."""
+    T, heads = (1 << 27) + 77, (1, 1, 1, 1)
+    gen = torch.Generator("cuda").manual_seed(5)
+    gi = torch.randn(T, 1, 5, device="cuda", dtype=torch.bfloat16, generator=gen)
+    bias = torch.tensor([-1.0, 0.0], device="cuda")
+    gi[..., 3].clamp_(-1, 0.15)
+    o, last, _ = B.delta_fwd(gi, heads, bias, save=False)
+    for at in (0, 128 * 64, 2048 * 64 - 20, (1 << 25) + 5, 3 * (1 << 25), (1 << 27) - 60, T - 64):
+        begin = max(at - 128, 0)
+        want, S, _ = O.delta(gi[begin:at + 64].double().cpu(), heads, bias.double().cpu())
+        close(o[at:at + 64], want[at - begin:])
+    close(last, S)
+
+
 @pytest.mark.parametrize("T,N,heads", [(150, 2, (2, 1, 32, 32)), (3100, 1, (2, 2, 16, 16)), (70, 100, (2, 2, 16, 16))])
 def test_captured(T, N, heads):
     """Both passes in a graph, replayed with other inputs, eager work between the replays."""

@@ -157,6 +157,13 @@ def test_temperatures(tau):
     assert (out.double().cpu() - grad).abs().max() <= tol * tau / 5
 
 
+@pytest.mark.parametrize("K", [50, 40000])
+def test_large_logits(K):
+    """Far from 0 (3e4 units of tau, where neighbours are 0.002 apart), only the differences count."""
+    buf, index, teacher, _ = case(3, K, 9)
+    check(buf + 20000, index, teacher - 20000, None, K, tau=0.7)
+
+
 def test_captured():
     bufs = [tuple(x.cuda() for x in case(9, 5000, 12, "bf16", seed=s, weights="some")) for s in range(4)]
     z, index, teacher, w = (x.clone() for x in bufs[0])
