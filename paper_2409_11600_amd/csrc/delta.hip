@@ -575,7 +575,6 @@ template <typename T, int DT> __device__ __forceinline__ void answers(int l, con
 // ----------------------------------------------------------------------------- all steps
 // A block takes the columns of a state that its wavefronts hold, 16 each, through all chunks.
 template <typename T, int DT, int NW>
-
 __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
                                                             T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
 {
@@ -1632,7 +1631,15 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
     return NSK_OK;
 }
 // The workspace: the states (or gradients) of all chunks; where the chunks are taken all at once their matrices; where the sequence is cut into segments theirs, and the states between them.
-bool at_once(const Sizes &z) { return z.chunks > 2 && (long long)z.N * z.H < 192; }
+// Few heads: all at once (whose time grows with the heads) rather than a block a head through all chunks (the same time up to 256 heads).  us of all at once / of that, heads of D x D in bf16:
+//   T=2048, D=64: forwards 64 heads 153 / 176, 80 183 / 177, 96 208 / 177; backwards 64 329 / 392, 96 488 / 500, 112 568 / 551;
+//   T=1024, D=128: forwards 64 174 / 198, 80 232 / 197; backwards 64 379 / 398, 80 491 / 463;  T=512, D=32: forwards 96 36 / 45, 128 48 / 46; backwards 128 104 / 119, 192 144 / 151;
+//   T=200, D=64 in fp32: forwards 60 35 / 41, 80 47 / 41; backwards 80 95 / 97, 100 102 / 99.  One or two chunks are not worth the launches.
+bool at_once(const Sizes &z, bool back)
+{
+    const int most = z.D <= 32 ? back ? 160 : 120 : z.D <= 64 ? back ? 104 : 80 : 72;
+    return z.chunks > 2 && (long long)z.N * z.H < most;
+}
 // (Compose and Fill take a step a chunk of a segment, Jump one a segment: segments about as many as twice their chunks.)
 int segment_of(const Sizes &z)
 {
@@ -1646,13 +1653,13 @@ struct Plan {
     int segment, segments;
     size_t matrices, composed, between, bytes;
 };
-Plan plan_of(const Sizes &z, bool states)
+Plan plan_of(const Sizes &z, bool back)
 {
     Plan p{};
-    const bool all = at_once(z);
+    const bool all = at_once(z, back);
     p.segment = all ? segment_of(z) : 0;
     p.segments = p.segment ? ceil_div(z.chunks, p.segment) : 0;
-    p.matrices = states || all ? align_up(saved_of(z)) : 0;
+    p.matrices = back || all ? align_up(saved_of(z)) : 0;
     p.composed = p.matrices + (all ? align_up(matrices_at(z, z.chunks, 0, 0) * sizeof(float)) : 0);
     p.between = p.composed + align_up(matrices_at(z, p.segments, 0, 0) * sizeof(float));
     p.bytes = p.between + align_up(state_at(z, p.segments, 0, 0) * sizeof(float));
@@ -1723,7 +1730,7 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
             const size_t bytes = sizeof(Shared<T, DT>);
             int allowed = NSK_OK;
-            if (at_once(z)) {
+            if (at_once(z, false)) {
                 allowed = allow_lds<delta_matrices_kernel<T, DT, NW, false>>(bytes);
                 if (allowed == NSK_OK) allowed = allow_lds<delta_out_kernel<T, DT, NW>>(bytes);
                 if (allowed != NSK_OK) return allowed;
@@ -1773,7 +1780,7 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             static_assert(sizeof(GradShared<T, DT>) <= 160 * 1024, "what a compute unit has");
             int allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);
             if (allowed != NSK_OK) return allowed;
-            if (at_once(z)) {
+            if (at_once(z, true)) {
                 allowed = allow_lds<delta_matrices_kernel<T, DT, NW, true>>(bytes);
                 if (allowed != NSK_OK) return allowed;
                 hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, true>), dim3((unsigned)(z.chunks * z.N * z.H), (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)),

@@ -191,7 +191,9 @@ __device__ void save_row(const Sizes &z, long long n, Soft q, float *saved)
     }
 }
 
-// A row (or a piece of it) a block.  With several pieces a row, their sums go to `partial` and distill_join_kernel finishes the rows.
+// A row (or a piece of it) a block.  With several pieces a row, their sums go to `partial` and distill_join_kernel finishes the rows.  Bound by memory where rows are many: 10000 x 32768 in
+// bf16 take 117 us, 5.6 TB/s (6.4 with what the last-level cache has kept), the vector unit busy three quarters of the time with an exponential an element; 50 x 1000 take 5.4, a chain of one
+// load of the row, three joins over the block and the logits of the places.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_fwd_kernel(Sizes z, const T *__restrict__ logits, const int *__restrict__ index, const float *__restrict__ t,
                                                                const float *__restrict__ weights, float *__restrict__ per_row, float *__restrict__ saved, float *__restrict__ partial)
@@ -242,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(Sizes z, const T
     finish_row(z, n, q, logits + n * z.ld, at, tr, teacher, by, per_row, part);
 }
 
-// Sums of w_n l_n and of w_n: a block for all rows, or kSums blocks and one that joins what they leave.  In 64 bits, in a fixed order.
+// Sums of w_n l_n and of w_n: a block for all rows, or kSums blocks and one that joins what they leave.  In 64 bits, in a fixed order.  2.5 us for 50 rows, 7.5 for 10000.
 constexpr int kSums = 64, kRowsOfOne = 1 << 16;
 __global__ __launch_bounds__(1024) void distill_loss_kernel(int N, const float *__restrict__ weights, const float *__restrict__ per_row, const double *__restrict__ joined, double *__restrict__ left,
                                                             float *__restrict__ loss, float *__restrict__ saved)
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(int N, const float *
     saved[2 * (long long)N + 1] = total != 0. ? (float)(1. / total) : 0.f;
 }
 
-// A row (or a piece of it) a block.  All columns are written as if the teacher had no places; the columns of its places are then written again, each by one lane
+// A row (or a piece of it) a block.  Bound by memory: 5003 x 50001 in fp32, three quarters of the rows with a weight, 395 us, 4.4 TB/s of reads and writes mixed.  All columns are written as if the teacher had no places; the columns of its places are then written again, each by one lane
 // with the sum of its places' p, from the logit (and the gradient that is added to) read before: so each is rounded once, and a place costs nothing on the way.  Which places share an index
 // a hash table in LDS finds, the memory's passes running beside it; those that do look for each other one by one, so that the sum is in the places' order (comparing all places with all,
 // as at first, took 321 us a call where M = 1024, N = 512, K = 32000, bf16, now 23; M = 64: 18 and 14).
@@ -417,15 +419,17 @@ int check(const nsk_distill_desc_t *desc, Sizes &z)
     while (1 << z.bits < 2 * d.M) ++z.bits;
     return NSK_OK;
 }
-// Few long rows are shared by several blocks.
-void cut(Sizes &z, int least)
+// Few long rows are shared by several blocks.  Forwards that takes a launch more, which only rows of 65536 and more make up for; bf16, us of N x K, one block a row / pieces of 4096 and more:
+// forwards 64 x 8192 9.3 / 12.5, 64 x 32768 10.9 / 12.0, 512 x 32768 14.4 / 18.0 (64 x 131072 13.3, 1 x 131072 11.4 with pieces, where one block alone would need 16 loads one after the other);
+// backwards 8 x 32768 9.7 / 7.3, 64 x 8192 8.2 / 6.6, 256 x 32768 13.7 / 11.5, 512 x 32768 17.7 / 16.7.
+constexpr int kLeast = 4096, kLongForward = 65536;
+void cut(Sizes &z, bool forward)
 {
     int pieces = 1;
-    while (pieces < 64 && (long long)z.N * pieces < 1024 && z.K / (2 * pieces) >= least) pieces *= 2;
+    while ((!forward || z.K >= kLongForward) && pieces < 64 && (long long)z.N * pieces < 1024 && z.K / (2 * pieces) >= kLeast) pieces *= 2;
     z.piece = (ceil_div(z.K, pieces) + 15) / 16 * 16;
     z.pieces = ceil_div(z.K, z.piece);
 }
-constexpr int kLeast = 4096;
 size_t sums_at(const Sizes &z) { return z.pieces > 1 ? align_up((size_t)z.N * z.pieces * 2 * sizeof(float)) : 0; }
 size_t workspace_of(const Sizes &z) { return sums_at(z) + (z.N > kRowsOfOne ? kSums * 2 * sizeof(double) : 0); }
 
@@ -440,7 +444,7 @@ size_t nsk_distill_workspace_bytes(const nsk_distill_desc_t *desc)
 {
     Sizes z;
     if (check(desc, z) != NSK_OK) return 0;
-    cut(z, kLeast);
+    cut(z, true);
     return workspace_of(z);
 }
 
@@ -454,7 +458,7 @@ int nsk_distill_fwd(const nsk_distill_desc_t *desc, const void *logits, const in
     if (unaligned16(logits) || unaligned16(top_index) || unaligned16(top_logits) || unaligned16(weights) || unaligned16(per_row) || unaligned16(loss) || unaligned16(saved) ||
         unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    cut(z, kLeast);
+    cut(z, true);
     if (workspace_of(z) && (!workspace || workspace_bytes < workspace_of(z))) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     float *partial = (float *)workspace;
@@ -486,7 +490,7 @@ int nsk_distill_bwd(const nsk_distill_desc_t *desc, const void *logits, const in
     if (!logits || !top_index || !top_logits || !saved || !dlogits) return NSK_ERR_NULL;
     if (unaligned16(logits) || unaligned16(top_index) || unaligned16(top_logits) || unaligned16(weights) || unaligned16(saved) || unaligned16(dlogits)) return NSK_ERR_ALIGNMENT;
     if (accumulate && logits == dlogits) return NSK_ERR_BAD_DESC;
-    cut(z, kLeast);
+    cut(z, false);
     const dim3 grid((unsigned)z.N, (unsigned)z.pieces);
     const size_t lds = ((size_t)z.M * 4 + ((size_t)1 << z.bits)) * 4;
     hipStream_t st = (hipStream_t)stream;
