@@ -574,7 +574,7 @@ template <typename T, int DT> __device__ __forceinline__ void answers(int l, con
 
 // ----------------------------------------------------------------------------- all steps
 // A block takes the columns of a state that its wavefronts hold, 16 each, through all chunks.  Bound by the chain within a chunk (load, products, inverse, solution, products), 10 to 13 us of it:
-// T=1024, heads of 128 x 128 in bf16, 198 us for 40 of them and for 192 of them; fp32 343.
+// T=1024, heads of 128 x 128 in bf16, 198 us for 40 of them and 229 for 192; fp32 343 for 40.
 template <typename T, int DT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void delta_fwd_kernel(Sizes z, const T *__restrict__ gi, const float *__restrict__ bias, const int *__restrict__ lengths, const float *__restrict__ h0,
                                                             T *__restrict__ o, float *__restrict__ h_last, float *__restrict__ saved)
@@ -713,7 +713,7 @@ __global__ __launch_bounds__(kFlowThreads, 2) void delta_flow_kernel(Sizes z, co
     const T *rows0 = gi + n * z.gi_n;
     if (wave >= 4) return prepare<T, DT>(z, wave - 4, rows0, bias, h, hk, len, used, both_s, [](int i) { return i; });
     int l = fresh_lane();
-    const int col = wave * 16 + (l & 15);
+    const int col = (blockIdx.y * 4 + wave) * 16 + (l & 15);
     const size_t own = state_at(z, 0, n, h);
     f32x4 S[DT];
     load_state(l, z, h0 ? h0 + own : nullptr, col, S);
@@ -1109,7 +1109,7 @@ __global__ __launch_bounds__(kFlowThreads, 2) void delta_ends_flow_kernel(Sizes 
     auto chunk = [&](int i) { return used - 1 - i; };
     if (wave >= 4) return prepare<T, DT>(z, wave - 4, gi + n * z.gi_n, bias, h, hk, len, count, both_s, chunk);
     int l = fresh_lane();
-    const int col = wave * 16 + (l & 15);
+    const int col = (blockIdx.y * 4 + wave) * 16 + (l & 15);
     const size_t own = state_at(z, 0, n, h);
     f32x4 G[DT];
     load_state(l, z, dh_last ? dh_last + own : nullptr, col, G);
@@ -1640,15 +1640,21 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
     return NSK_OK;
 }
 // The workspace: the states (or gradients) of all chunks; where the chunks are taken all at once their matrices; where the sequence is cut into segments theirs, and the states between them.
-// Few heads: all at once (whose time grows with the heads) rather than a block a head through all chunks (the same time up to 256 heads).  us of all at once / of that, heads of D x D in bf16:
-//   T=2048, D=64: forwards 64 heads 153 / 176, 80 183 / 177, 96 208 / 177; backwards 64 329 / 392, 96 488 / 500, 112 568 / 551;
-//   T=1024, D=128: forwards 64 174 / 198, 80 232 / 197; backwards 64 379 / 398, 80 491 / 463;  T=512, D=32: forwards 96 36 / 45, 128 48 / 46; backwards 128 104 / 119, 192 144 / 151;
-//   T=200, D=64 in fp32: forwards 60 35 / 41, 80 47 / 41; backwards 80 95 / 97, 100 102 / 99.  One or two chunks are not worth the launches.
-bool at_once(const Sizes &z, bool back)
+// Few heads: all at once, whose time grows with the heads and their tiles, rather than a block or two a head through all chunks, whose time is the same up to 256 blocks.  us of all at once / of that
+// (heads of D x Dv, bf16; T=1024 if not said):
+//   64 x 64: forwards 56 heads 79 / 91, 68 95 / 91; backwards 80 216 / 228, T=2048 96 488 / 500, 112 568 / 551;  fp32 forwards 68 120 / 142, 80 141 / 144, T=200 60 35 / 41, 80 47 / 41;
+//   64 x 128: forwards 44 80 / 92, 56 92 / 92; backwards 56 222 / 245, 68 280 / 279;  128 x 128: forwards 28 99 / 113, 36 141 / 112; backwards 28 198 / 227, 36 285 / 277;
+//   T=8192, 24 heads forwards 745 / 860, 32 936 / 866;  32 x 32, T=512: forwards 96 36 / 45, 128 48 / 46; backwards 192 144 / 151;
+//   128 x 128 in fp32, where nothing is prepared meanwhile: forwards 56 271 / 343, 72 373 / 346; backwards 72 633 / 650, 100 896 / 780.
+// One or two chunks are not worth the launches.
+bool at_once(const Sizes &z, int dtype, bool back)
 {
-    const int most = z.D <= 32 ? back ? 160 : 120 : z.D <= 64 ? back ? 104 : 80 : 72;
-    return z.chunks > 2 && (long long)z.N * z.H < most;
+    const long long tiles = (long long)z.N * z.H * (ceil_div(z.D, 16) + ceil_div(z.Dv, 16));
+    return z.chunks > 2 && tiles < (z.D <= 64 ? back ? 850 : 540 : dtype == NSK_BF16 ? 540 : 1150);
 }
+// Heads of more than 64 columns take two blocks with preparing wavefronts each, if both fit the chip at once, rather than one of eight wavefronts without (T=1024 forwards, us of 100 heads of
+// 128 x 128 in bf16 119 / 202, of 128 heads of 64 x 128 97 / 155, in fp32 152 / 235).
+bool flows(const Sizes &z) { return z.Dv <= 64 || (long long)z.N * z.H <= 128; }
 // (Compose and Fill take a step a chunk of a segment, Jump one a segment: segments about as many as twice their chunks.)
 int segment_of(const Sizes &z)
 {
@@ -1662,10 +1668,10 @@ struct Plan {
     int segment, segments;
     size_t matrices, composed, between, bytes;
 };
-Plan plan_of(const Sizes &z, bool back)
+Plan plan_of(const Sizes &z, int dtype, bool back)
 {
     Plan p{};
-    const bool all = at_once(z, back);
+    const bool all = at_once(z, dtype, back);
     p.segment = all ? segment_of(z) : 0;
     p.segments = p.segment ? ceil_div(z.chunks, p.segment) : 0;
     p.matrices = back || all ? align_up(saved_of(z)) : 0;
@@ -1717,7 +1723,7 @@ size_t nsk_delta_workspace_bytes(const nsk_delta_desc_t *desc, int pass)
 {
     Sizes z;
     if ((pass != NSK_PASS_FWD && pass != NSK_PASS_DGRAD) || check(desc, z) != NSK_OK) return 0;
-    return plan_of(z, pass == NSK_PASS_DGRAD).bytes;
+    return plan_of(z, desc->dtype, pass == NSK_PASS_DGRAD).bytes;
 }
 
 int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bias, const int *lengths, const float *h0, void *o, float *h_last, float *saved, void *workspace,
@@ -1729,7 +1735,7 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (!gi || (!o && !h_last)) return NSK_ERR_NULL;
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(h0) || unaligned16(o) || unaligned16(h_last) || unaligned16(saved) || unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    const Plan p = plan_of(z, false);
+    const Plan p = plan_of(z, desc->dtype, false);
     if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     float *matrices = (float *)((char *)workspace + p.matrices), *states = saved ? saved : (float *)workspace;
@@ -1739,7 +1745,7 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             constexpr int DT = decltype(dt)::value, NW = decltype(nw)::value;
             const size_t bytes = sizeof(Shared<T, DT>);
             int allowed = NSK_OK;
-            if (at_once(z, false)) {
+            if (at_once(z, desc->dtype, false)) {
                 allowed = allow_lds<delta_matrices_kernel<T, DT, NW, false>>(bytes);
                 if (allowed == NSK_OK) allowed = allow_lds<delta_out_kernel<T, DT, NW>>(bytes);
                 if (allowed != NSK_OK) return allowed;
@@ -1751,16 +1757,18 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
                     hipLaunchKernelGGL((delta_out_kernel<T, DT, NW>), dim3(all, (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, states, (T *)o);
                 return check_launch();
             }
-            if constexpr (kFlows<T, DT> && NW == 4) {
-                allowed = allow_lds<delta_flow_kernel<T, DT>>(2 * bytes);
-                if (allowed != NSK_OK) return allowed;
-                hipLaunchKernelGGL((delta_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths, h0, (T *)o, h_last, saved);
-            } else {
-                allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
-                if (allowed != NSK_OK) return allowed;
-                hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0,
-                                   (T *)o, h_last, saved);
-            }
+            if constexpr (kFlows<T, DT>)
+                if (flows(z)) {
+                    allowed = allow_lds<delta_flow_kernel<T, DT>>(2 * bytes);
+                    if (allowed != NSK_OK) return allowed;
+                    hipLaunchKernelGGL((delta_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 64)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths,
+                                       h0, (T *)o, h_last, saved);
+                    return check_launch();
+                }
+            allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
+            if (allowed != NSK_OK) return allowed;
+            hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0,
+                               (T *)o, h_last, saved);
             return check_launch();
         });
     };
@@ -1777,7 +1785,7 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
     if (unaligned16(gi) || unaligned16(bias) || unaligned16(lengths) || unaligned16(saved) || unaligned16(d_o) || unaligned16(dh_last) || unaligned16(dgi) || unaligned16(dh0) ||
         unaligned16(workspace))
         return NSK_ERR_ALIGNMENT;
-    const Plan p = plan_of(z, true);
+    const Plan p = plan_of(z, desc->dtype, true);
     if (!workspace || workspace_bytes < p.bytes) return NSK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     float *ends = (float *)workspace, *matrices = (float *)((char *)workspace + p.matrices);
@@ -1789,17 +1797,19 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
             static_assert(sizeof(GradShared<T, DT>) <= 160 * 1024, "what a compute unit has");
             int allowed = allow_lds<delta_grad_kernel<T, DT>>(grad_bytes);
             if (allowed != NSK_OK) return allowed;
-            if (at_once(z, true)) {
+            if (at_once(z, desc->dtype, true)) {
                 allowed = allow_lds<delta_matrices_kernel<T, DT, NW, true>>(bytes);
                 if (allowed != NSK_OK) return allowed;
                 hipLaunchKernelGGL((delta_matrices_kernel<T, DT, NW, true>), dim3((unsigned)(z.chunks * z.N * z.H), (unsigned)ceil_div(ceil_div(z.D, 16) + ceil_div(z.Dv, 16), NW)),
                                    dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, (const T *)d_o, matrices);
                 scan<DT, true>(z, p, lengths, (char *)workspace, dh_last, ends, dh0, st);
-            } else if constexpr (kFlows<T, DT> && NW == 4) {
-                allowed = allow_lds<delta_ends_flow_kernel<T, DT>>(2 * bytes);
-                if (allowed != NSK_OK) return allowed;
-                hipLaunchKernelGGL((delta_ends_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths, (const T *)d_o, dh_last, dh0,
-                                   ends);
+            } else if (kFlows<T, DT> && flows(z)) {
+                if constexpr (kFlows<T, DT>) {
+                    allowed = allow_lds<delta_ends_flow_kernel<T, DT>>(2 * bytes);
+                    if (allowed != NSK_OK) return allowed;
+                    hipLaunchKernelGGL((delta_ends_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 64)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths,
+                                       (const T *)d_o, dh_last, dh0, ends);
+                }
             } else {
                 allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
                 if (allowed != NSK_OK) return allowed;

@@ -100,9 +100,10 @@ def test_sizes(T, N, heads, dtype):
     check(case(T, N, heads, dtype, seed=T), heads)
 
 
-# many heads: a block takes all chunks of one; few heads and many chunks: cut into segments, the last of one chunk
+# many heads: a block takes all chunks of one, or two do, or eight wavefronts; few heads and many chunks: cut into segments, the last of one chunk
 @pytest.mark.parametrize("T,N,heads,dtype", [(140, 66, (3, 1, 20, 36), "f32"), (135, 50, (4, 4, 32, 48), "bf16"), (70, 100, (2, 2, 72, 80), "f32"), (3137, 1, (2, 1, 24, 40), "f32"),
-                                             (3100, 2, (1, 1, 16, 8), "bf16")])
+                                             (3100, 2, (1, 1, 16, 8), "bf16"), (330, 40, (3, 1, 64, 100), "bf16"), (200, 60, (2, 2, 40, 128), "f32"), (150, 70, (2, 1, 24, 72), "bf16"),
+                                             (200, 36, (2, 2, 100, 120), "bf16")])
 def test_ways_of_going_through(T, N, heads, dtype):
     lengths = [(37 * n + T // 2) % (T + 1) for n in range(N)]
     lengths[0] = T
