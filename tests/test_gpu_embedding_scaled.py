@@ -68,6 +68,18 @@ def test_gradient(n, E, V, kind, dtype):
         assert torch.equal(got, B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad))
 
 
+@pytest.mark.parametrize("n,E,V,pad", [(3, 1, 5000000, None), (300, 2052, 40, 7), (1000, 1030, 333, 0), (16384, 20, 3000, 2999), (20000, 20, 3000, 5), (1, 8, 1, 0)])
+def test_every_row_is_written(n, E, V, pad):
+    """Whatever the table held: zeros where a token does not occur."""
+    t = tokens_of(n, V, "words", seed=n)
+    dout = torch.randn(n, E, generator=torch.Generator().manual_seed(2))
+    table = torch.full((V, E), math.nan, device="cuda")
+    got = B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.0, pad=pad, dtable=table).cpu()
+    counts = (t >= 0) & (t < V) & (t != (-1 if pad is None else pad))
+    occurs = torch.zeros(V, dtype=torch.bool).index_fill(0, t[counts].long(), True)
+    assert not got[~occurs].any() and bool(torch.isfinite(got).all()) and bool(got[occurs].any(1).all())
+
+
 def test_small_against_the_loop():
     t, dout = tokens_of(40, 6, "none"), torch.randn(40, 5)
     want = O.embedding_gradient(t, dout.double(), 6, 0.3, pad=2)
