@@ -1644,13 +1644,13 @@ int check(const nsk_delta_desc_t *desc, Sizes &z)
 // (heads of D x Dv, bf16; T=1024 if not said):
 //   64 x 64: forwards 56 heads 79 / 91, 68 95 / 91; backwards 80 216 / 228, T=2048 96 488 / 500, 112 568 / 551;  fp32 forwards 68 120 / 142, 80 141 / 144, T=200 60 35 / 41, 80 47 / 41;
 //   64 x 128: forwards 44 80 / 92, 56 92 / 92; backwards 56 222 / 245, 68 280 / 279;  128 x 128: forwards 28 99 / 113, 36 141 / 112; backwards 28 198 / 227, 36 285 / 277;
-//   T=8192, 24 heads forwards 745 / 860, 32 936 / 866;  32 x 32, T=512: forwards 96 36 / 45, 128 48 / 46; backwards 192 144 / 151;
+//   T=8192, 24 heads forwards 745 / 860, 32 936 / 866;  32 x 32, T=512: forwards 96 36 / 45, 128 48 / 46; backwards 192 144 / 151;  16 x 16: forwards 128 75 / 84, 200 101 / 84;
 //   128 x 128 in fp32, where nothing is prepared meanwhile: forwards 56 271 / 343, 72 373 / 346; backwards 72 633 / 650, 100 896 / 780.
 // One or two chunks are not worth the launches.
 bool at_once(const Sizes &z, int dtype, bool back)
 {
-    const long long tiles = (long long)z.N * z.H * (ceil_div(z.D, 16) + ceil_div(z.Dv, 16));
-    return z.chunks > 2 && tiles < (z.D <= 64 ? back ? 850 : 540 : dtype == NSK_BF16 ? 540 : 1150);
+    const int tiles = ceil_div(z.D, 16) + ceil_div(z.Dv, 16);
+    return z.chunks > 2 && (long long)z.N * z.H * (tiles < 4 ? 4 : tiles) < (z.D <= 64 ? back ? 850 : 540 : dtype == NSK_BF16 ? 540 : 1150);
 }
 // Heads of more than 64 columns take two blocks with preparing wavefronts each, if both fit the chip at once, rather than one of eight wavefronts without (T=1024 forwards, us of 100 heads of
 // 128 x 128 in bf16 119 / 202, of 128 heads of 64 x 128 97 / 155, in fp32 152 / 235).
