@@ -87,7 +87,7 @@ template <typename T> __device__ __forceinline__ Vec<T> load_vec(const T *p)
 template <typename T> __device__ __forceinline__ void store_vec(T *p, const Vec<T> &v)
 {
     typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-    *(u32x4 *)p = __builtin_bit_cast(u32x4, v);
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4 *)p);
 }
 
 // (maximum, sum) over n logits by the whole block.  Each lane keeps its own pair; the sum is rescaled once a group of vectors.
@@ -290,7 +290,8 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(int N, const float *
     saved[2 * (long long)N + 1] = total != 0. ? (float)(1. / total) : 0.f;
 }
 
-// A row (or a piece of it) a block.  Bound by memory: 5003 x 50001 in fp32, three quarters of the rows with a weight, 395 us, 4.4 TB/s of reads and writes mixed.  All columns are written as if the teacher had no places; the columns of its places are then written again, each by one lane
+// A row (or a piece of it) a block.  Bound by memory: 5003 x 50001 in fp32, three quarters of the rows with a weight, 395 us, 4.4 TB/s of reads and writes mixed (four vectors at a
+// time and stores that are not kept in the caches: 5000 x 50000 in fp32, all rows, 438 us, 4.6 TB/s; two at a time 444, kept 470, both 482).  All columns are written as if the teacher had no places; the columns of its places are then written again, each by one lane
 // with the sum of its places' p, from the logit (and the gradient that is added to) read before: so each is rounded once, and a place costs nothing on the way.  Which places share an index
 // a hash table in LDS finds, the memory's passes running beside it; those that do look for each other one by one, so that the sum is in the places' order (comparing all places with all,
 // as at first, took 321 us a call where M = 1024, N = 512, K = 32000, bf16, now 23; M = 64: 18 and 14).
@@ -299,7 +300,7 @@ template <typename T, bool ADD>
 __global__ __launch_bounds__(kThreads) void distill_bwd_kernel(Sizes z, const T *logits, const int *__restrict__ index, const float *__restrict__ t, const float *__restrict__ weights,
                                                                const float *__restrict__ saved, float dloss, T *dlogits)
 {
-    constexpr int V = Span<T>::V, U = 2;
+    constexpr int V = Span<T>::V, U = 4;
     extern __shared__ float lds[];
     __shared__ float part[2][kThreads / 64];
     float *p_at = lds, *z_at = lds + z.M, *old_at = lds + 2 * z.M;
