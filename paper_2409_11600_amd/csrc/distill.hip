@@ -290,7 +290,7 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(int N, const float *
     saved[2 * (long long)N + 1] = total != 0. ? (float)(1. / total) : 0.f;
 }
 
-// A row (or a piece of it) a block.  Bound by memory: 5003 x 50001 in fp32, three quarters of the rows with a weight, 395 us, 4.4 TB/s of reads and writes mixed (four vectors at a
+// A row (or a piece of it) a block.  Bound by memory: 5003 x 50001 in fp32, seven tenths of the rows with a weight, 395 us, 4.4 TB/s of reads and writes mixed (four vectors at a
 // time and stores that are not kept in the caches: 5000 x 50000 in fp32, all rows, 438 us, 4.6 TB/s; two at a time 444, kept 470, both 482).  All columns are written as if the teacher had no places; the columns of its places are then written again, each by one lane
 // with the sum of its places' p, from the logit (and the gradient that is added to) read before: so each is rounded once, and a place costs nothing on the way.  Which places share an index
 // a hash table in LDS finds, the memory's passes running beside it; those that do look for each other one by one, so that the sum is in the places' order (comparing all places with all,
