@@ -7,7 +7,9 @@
 //   dU = P^T dO + exp(C - c) K G,  (1 + A)^T X = dU,  G <- exp(C) G + (exp(c) Q)^T dO - (beta exp(c) K)^T X,
 //   dV = beta X,  dA = -X U^T,  dP = dO U^T  (where A and P are not zero),  and with E1 = X S^T, E2 = dO S^T, E3 = U G^T:
 //   dQ = exp(c) E2 + (dP L) K,  dK = -beta exp(c) E1 + exp(C - c) E3 + (dA beta L) K + (dA beta L)^T K + (dP L)^T Q,  L_ij = exp(c_i - c_j),
-//   and the gradients of c, of beta and of the lengths of q and k from the row and column sums of the same products.
+//   and the gradients of beta and of the lengths of q and k from the row sums of the same products.  That of log alpha_t is the sum of what the gate t lies in: of row i's products with exp(c_i)
+//   from i = t on, of row j's with exp(C - c_j) in front of t, of dA_ij A_ij + dP_ij P_ij over the pairs j < t <= i, and of exp(C) S G.  Only such terms are added up: they all hold alpha_t, so
+//   that the sum keeps its bits where the gate is nearly closed (as the sum from t on of the gradients of c, most of which cancels there, it had no right digit left at alpha = 1e-7).
 // Products keep 32 bits: states, gates' gradients and the results of a chunk of 64 dependent steps.  Those of two float operands are on the fp32 matrix unit.  Keys and queries in bf16 stay what they
 // are (their lengths are factors of rows and columns, applied to the products), and what they are multiplied with goes in three bf16 pieces that hold all of its bits: three products of 16
 // clocks for 32 indices, where the fp32 unit takes eight of 32.
@@ -103,6 +105,13 @@ __device__ __forceinline__ f32x4 sum_columns(f32x4 v)
     return v;
 }
 
+// The sum of a tile's columns up to this lane's: rows of 16 lanes moved by 1, 2, 4 and 8.
+template <int BY> __device__ __forceinline__ float add_moved(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x110 + BY, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum_up_to_column(float v) { return add_moved<8>(add_moved<4>(add_moved<2>(add_moved<1>(v)))); }
+
 // ----------------------------------------------------------------------------- memory
 // Rows are reached through buffer descriptors: what lies at or behind `bytes` reads as zero and is not written, and so is a lane's offset of kNowhere plus anything below 2^31.  An access is
 // a lane's offset plus a uniform one: one instruction, where 64-bit addresses and conditions took six.
@@ -131,20 +140,24 @@ struct alignas(16) Gates {
 // By one wavefront, a step a lane.  Steps from `live` on leave the state as it is.
 __device__ __forceinline__ float exp_of(double c) { return __builtin_amdgcn_exp2f((float)c); }
 // c plus the sums of the lanes in front: within 16 lanes, then over the rows of 16.
-template <int CTRL, int ROWS> __device__ __forceinline__ double add_moved(double c)
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ double moved(double c)
 {
     const unsigned long long u = __builtin_bit_cast(unsigned long long, c);
     const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, true), hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, true);
-    return c + __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+__device__ __forceinline__ double sums_in_row(double c)
+{
+    c += moved<0x111>(c);       // a row moved by 1, 2, 4 and 8 lanes
+    c += moved<0x112>(c);
+    c += moved<0x114>(c);
+    return c + moved<0x118>(c);
 }
 __device__ __forceinline__ double sums_up_to(double c)
 {
-    c = add_moved<0x111, 0xf>(c);       // a row moved by 1, 2, 4 and 8 lanes
-    c = add_moved<0x112, 0xf>(c);
-    c = add_moved<0x114, 0xf>(c);
-    c = add_moved<0x118, 0xf>(c);
-    c = add_moved<0x142, 0xa>(c);       // the last lane of a row to the next one (rows 1 and 3), then of the second to the last two
-    return add_moved<0x143, 0xc>(c);
+    c = sums_in_row(c);
+    c += moved<0x142, 0xa>(c);       // the last lane of a row to the next one (rows 1 and 3), then of the second to the last two
+    return c + moved<0x143, 0xc>(c);
 }
 template <typename T> struct GateParts {
     unsigned a, b;
@@ -1183,7 +1196,7 @@ template <typename T, int DT> struct GradShared : Shared<T, DT> {
     };
     // (after the columns)
     struct Sums {
-        float row_a[4][kC], col_a[4][kC], row_p[4][kC], col_p[4][kC];       // of the tiles, by their other index
+        float row_a[4][kC], col_a[4][kC], row_p[4][kC], col_p[4][kC];       // of the tiles, by their other index; col of a tile on the diagonal: what its steps' gates lie in
         float dots[DT][kC], ends[DT][kC];
         float states[DT];
     };
@@ -1369,7 +1382,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             settle(E3);
             lds_barrier();
         }
-        // dA and dP, times L, in the place of A and P; the sums of dA A and dP P over rows and columns
+        // dA and dP, times L, in the place of A and P; the sums of dA A and dP P over rows and columns, and on the diagonal, for each step t of the tile, over its pairs j < t <= i
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
             const int t = wave + i * NW;
@@ -1380,10 +1393,18 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
             tile_at(is_a ? t : t - kTiles, bi, bj);
             const f32x4 beta = rows_of(l, s.g.beta, 16 * bi), d = is_a ? -acc[i] : acc[i], L = decays(l, s.g, bi, bj, is_a);
             const f32x4 by_row = d * tile[i], by_col = is_a ? beta * by_row : by_row;
-            float sum = (by_col[0] + by_col[1]) + (by_col[2] + by_col[3]);
+            const bool diagonal = bi == bj;
+            f32x4 part = by_col;
+            if (diagonal)               // (columns up to lc = t - 1 of the rows from t on)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float up = sum_up_to_column(by_col[r]);
+                    part[r] = g4 + r > lc ? up : 0.f;
+                }
+            float sum = (part[0] + part[1]) + (part[2] + part[3]);
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            if (l < 16) (is_a ? s.t.col_a : s.t.col_p)[bi][16 * bj + l] = sum;
+            if (l < 16) (is_a ? s.t.col_a : s.t.col_p)[bi][16 * bj + (diagonal ? (l + 1) & 15 : l)] = sum;       // (nothing comes in front of the tile's first step: the last lane's sum is 0)
             const f32x4 row = sum_columns(by_row);
             if (lc == 0) *(f32x4 *)&(is_a ? s.t.row_a : s.t.row_p)[bj][16 * bi + g4] = row;
             store_tile(l, is_a ? s.A : s.P, bi, bj, is_a ? beta * d * L : d * L);
@@ -1438,35 +1459,43 @@ __global__ __launch_bounds__(kGradWaves * 64) void delta_grad_kernel(Sizes z, co
         settle(dK);
         if (wave == NW - 1) {           // the gates, a step a lane
             const int b = l >> 4;
-            double dc = 0., e = 0., both_all = 0.;
+            double dots = 0., ends = 0., both_all = 0.;
 #pragma unroll
             for (int k = 0; k < DT; ++k) {
-                e += (double)s.t.ends[k][l];
-                dc += (double)s.t.dots[k][l];
+                ends += (double)s.t.ends[k][l];
+                dots += (double)s.t.dots[k][l];
                 both_all += (double)s.t.states[k];
             }
-            dc -= e;
-            float ra = 0.f, xr = (s.xr[0][l] + s.xr[1][l]) + (s.xr[2][l] + s.xr[3][l]);
-            double p = 0.;
+            const float beta = s.g.beta[l], xr = (s.xr[0][l] + s.xr[1][l]) + (s.xr[2][l] + s.xr[3][l]);
+            // the tiles beside the diagonal: this step's row of them, its column, and those with a block between, which hold all gates of that block: tiles (2, 0) and (3, 0) by
+            // their columns in the first block's lanes, (3, 0) and (3, 1) by their rows in the last one's
+            float ra = 0.f;
+            double by_rows = 0., by_cols = 0., far = 0.;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (k <= b) {
-                    ra += s.t.row_a[k][l];
-                    p += (double)s.t.row_p[k][l];
+                if (k <= b) ra += s.t.row_a[k][l];
+                if (k < b) {
+                    const double x = (double)beta * s.t.row_a[k][l] + (double)s.t.row_p[k][l];
+                    by_rows += x;
+                    if (b == 3 && k < 2) far += x;
                 }
-                if (k >= b) p -= (double)s.t.col_a[k][l] + (double)s.t.col_p[k][l];
+                if (k > b) {
+                    const double x = (double)s.t.col_a[k][l] + (double)s.t.col_p[k][l];
+                    by_cols += x;
+                    if (b == 0 && k > 1) far += x;
+                }
             }
-            const float beta = s.g.beta[l];
-            dc += (double)beta * ra + p;
-            // of log alpha: all c from this step on, and C
-            double up = dc, end = e;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const double x = __shfl_down(up, o, 64);
-                if (l + o < 64) up += x;
-                end += __shfl_xor(end, o, 64);
-            }
-            up += end + (double)s.g.all * both_all;
+            far += moved<0x121>(far);       // (a row turned by 1, 2, 4 and 8 lanes)
+            far += moved<0x122>(far);
+            far += moved<0x124>(far);
+            far += moved<0x128>(far);
+            far = __shfl_xor(far, 16, 64);
+            double up = (double)s.t.col_a[b][l] + (double)s.t.col_p[b][l] + (double)s.g.all * both_all;
+            if (b == 1 || b == 2) up += far;
+            // rows from this step on, in their block and (dots) behind it: sums over the lanes turned round; rows and columns in front of it
+            const double from = sums_up_to(__shfl(dots, 63 - l, 64)) + sums_in_row(__shfl(by_rows, 63 - l, 64));
+            const double before = __shfl_up(ends, 1, 64);
+            up += __shfl(from, 63 - l, 64) + (sums_up_to(l ? before : 0.) + sums_in_row(moved<0x111>(by_cols)));
             if (l < rows) {
                 T *q = out0 + l * z.gi_t;
                 q[a_at(z, h)] = (T)(l < live ? (float)up * s.g.rest_a[l] : 0.f);

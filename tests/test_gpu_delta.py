@@ -329,3 +329,37 @@ def test_gradients_of_shared_heads_add_up():
     close(dgi[..., 32:], dgi3[..., 96:].double().cpu()), close(dh0, dh03.double().cpu())
     close(dgi[..., :16], dgi3[..., :48].double().cpu().reshape(T, N, 3, 16).sum(2))
     close(dgi[..., 16:32], dgi3[..., 48:96].double().cpu().reshape(T, N, 3, 16).sum(2))
+
+
+def by_head(x, heads):
+    """(name, head, columns) of a row's parts, each head by itself: a head's queries, keys, values and gates."""
+    H, Hk, D, Dv = heads
+    for name, part, count in zip("qkvab", x.split([Hk * D, Hk * D, H * Dv, H, H], -1), (Hk, Hk, H, H, H)):
+        for h, y in enumerate(part.unflatten(-1, (count, -1)).unbind(-2)):
+            yield f"d{name} of head {h}", y
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,heads", [(200, (6, 6, 32, 24)), (130, (6, 3, 72, 80)), (64, (6, 2, 16, 40)), (777, (6, 6, 8, 16))])
+def test_heads_that_forget(T, heads, dtype):
+    """Each head forgets at another rate, from half a step's memory to a millionth: each head's gradients by themselves, down to a gate's, of which next to nothing is left."""
+    c = case(T, 2, heads, dtype, lengths=[T, T - 7], seed=3)
+    c["bias"][:6] = torch.tensor([1.0, -3.0, -6.0, -9.0, -12.0, -16.0])
+    want, got, slack = wanted(c, heads)[3], both(gpu(c), heads)[3], along(c, heads)
+    for (name, a), (_, b), (_, more) in zip(by_head(got, heads), by_head(want, heads), by_head(slack, heads)):
+        close(a, b, name, more)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_single_gates_that_close(dtype):
+    """Single gates close among open ones, at the ends of chunks, of tiles and inside: their gradients by themselves, 1e-5 and less of the open ones'."""
+    T, N, heads = 260, 2, (4, 4, 32, 48)
+    c = case(T, N, heads, dtype, seed=4)
+    c["bias"][:4] = 2.0
+    at = [1, 15, 16, 40, 63, 64, 65, 100, 127, 128, 150, 176, 192, 205, 255, 259]
+    a = c["gi"][..., -8:-4]
+    a[at] = torch.tensor([-10.0, -14.0, -18.0, -22.0]).to(a.dtype)
+    want, got = wanted(c, heads)[3], both(gpu(c), heads)[3]
+    for (name, x), (_, y) in zip(by_head(got, heads), by_head(want, heads)):
+        if name.startswith("da"):
+            close(x[at], y[at], name + ", closed"), close(x, y, name)
