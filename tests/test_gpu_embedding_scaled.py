@@ -134,3 +134,73 @@ def test_beside_each_other():
                 got.append(B.embedding_scaled_bwd(t, d, 900, ws=ws))
     torch.cuda.synchronize()
     assert all(torch.equal(g, want[i % 2]) for i, g in enumerate(got))
+
+
+def counted_tokens(n, counts, gen):
+    """Token v occurs counts[v % len(counts)] times, positions in any order: (tokens, how many tokens)."""
+    times = torch.tensor(counts).repeat(n // sum(counts) + 1)
+    t = torch.arange(len(times)).repeat_interleave(times)[:n]
+    return t[torch.randperm(n, generator=gen)].to(torch.int32), int(t[-1]) + 1
+
+
+# above 65536 positions a wavefront takes 32 of them in order, and a stretch and the next fill its lanes: tokens that occur as often as that, twice and three times as often, one more and one less,
+# so that they begin and end at every place of a stretch; one token for all, for half of them, and few; tokens that are none; both sides of 65536
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,E,kind", [(65536, 8, "counts"), (65537, 8, "counts"), (66001, 260, "counts"), (70001, 7, "counts"), (65568, 12, "pairs"), (65599, 4, "whole"), (70000, 20, "one"), (90000, 9, "half"),
+                                      (131072, 12, "words"), (100003, 4, "none"), (200000, 4, "even")])
+def test_gradient_of_many_positions(n, E, kind, dtype):
+    gen = torch.Generator().manual_seed(n)
+    if kind in ("counts", "pairs", "whole"):
+        counts = {"counts": [31, 1, 32, 33, 63, 64, 65, 2, 95, 96, 97, 30, 129, 34], "pairs": [16], "whole": [32, 64, 96, 32]}[kind]
+        t, V = counted_tokens(n, counts, gen)
+    elif kind == "half":
+        V = 5000
+        t = torch.where(torch.rand(n, generator=gen) < 0.5, torch.full((n,), 4321), torch.randint(0, V, (n,), generator=gen)).to(torch.int32)
+    else:
+        V = 70001
+        t = tokens_of(n, V, kind, seed=n)
+    dout = torch.randn(n, E, generator=gen).to(TYPES[dtype])
+    inside = (t >= 0) & (t < V)
+    for pad in (None, int(t[inside][0])):
+        counts = inside if pad is None else inside & (t != pad)
+        at, d = t[counts].long(), dout[counts].double()
+        want = torch.zeros(V, E, dtype=torch.float64).index_add(0, at, d) * 1.5
+        size = torch.zeros(V, E, dtype=torch.float64).index_add(0, at, d.abs()) * 1.5
+        m = torch.zeros(V, dtype=torch.float64).index_add(0, at, torch.ones(len(at), dtype=torch.float64))[:, None]
+        got = B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad, dtable=torch.full((V, E), math.nan, device="cuda"))
+        assert bool(((got.double().cpu() - want).abs() <= 2.0 ** -24 * (m + 2) * size).all())
+        old = torch.randn(V, E, generator=gen)
+        added = B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad, dtable=old.cuda(), accumulate=True)
+        assert bool(((added.double().cpu() - want - old.double()).abs() <= 2.0 ** -24 * ((m + 2) * size + (want + old).abs() * 2)).all())
+        assert torch.equal(added.cpu()[m[:, 0] == 0], old[m[:, 0] == 0])
+        assert torch.equal(got, B.embedding_scaled_bwd(t.cuda(), dout.cuda(), V, 1.5, pad=pad))
+
+
+@pytest.mark.parametrize("n", [70000])
+def test_many_positions_captured_and_beside_each_other(n):
+    E, V, gen = 24, 800, torch.Generator().manual_seed(n)
+    t, dout, ws = tokens_of(n, V, "words").cuda(), torch.randn(n, E, device="cuda"), B.Workspace()
+    grad = B.embedding_scaled_bwd(t, dout, V, 2.0, ws=ws)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        B.embedding_scaled_bwd(t, dout, V, 2.0, dtable=grad, ws=ws)
+    others = [counted_tokens(n, [32, 64, 1, 300], gen)[0] % V, tokens_of(n, V, "one"), tokens_of(n, V, "none")]
+    spaces = [B.Workspace() for _ in others]
+    for k in others:
+        t.copy_(k.cuda())
+        dout.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, B.embedding_scaled_bwd(t, dout, V, 2.0))
+    want = [B.embedding_scaled_bwd(k.cuda(), dout, V) for k in others]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in others], []
+    others = [k.cuda() for k in others]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, w, k in zip(streams, spaces, others):
+            with torch.cuda.stream(s):
+                got.append(B.embedding_scaled_bwd(k, dout, V, ws=w))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % len(want)]) for i, g in enumerate(got))
