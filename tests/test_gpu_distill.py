@@ -183,3 +183,65 @@ def test_captured():
         want = B.distill_fwd(*other[:3], weights=other[3])
         assert all(torch.equal(a, b) for a, b in zip((loss, rows, saved), want))
         assert torch.equal(out, B.distill_bwd(*other[:3], want[2], weights=other[3]))
+
+
+# rows of 65536 columns and more are shared by several blocks forwards, whose parts another launch joins: every way of leaving rows out, odd widths and rows with room between, few rows and many
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,ld,how", [(3, 65535, 20, None, "plain"), (3, 65536, 20, None, "accumulate"), (9, 70001, 33, 70008, "in place"), (5, 66001, 1, 66001, "plain"), (70, 65552, 7, None, "in place")])
+@pytest.mark.parametrize("weights", ["some", "none of them", None])
+def test_long_rows(N, K, M, ld, how, weights, dtype):
+    buf, index, teacher, w = case(N, K, M, dtype, seed=K + N, ld=ld, weights=weights, gone=True)
+    check(buf, index, teacher, w, K, accumulate=how == "accumulate", in_place=how == "in place")
+
+
+def test_long_rows_far_from_zero():
+    buf, index, teacher, _ = case(3, 80000, 9)
+    check(buf + 20000, index, teacher - 20000, None, 80000, tau=0.7)
+
+
+@pytest.mark.parametrize("K", [65536, 100001])
+def test_long_rows_that_are_left_out(K):
+    """Rows without weight are not read, rows without a place have nothing, whatever they hold; masked words, a part of a row that is all masked, wrong indices and NaN stay in their rows."""
+    buf, index, teacher, _ = case(8, K, 5)
+    index[:] = torch.arange(5, dtype=torch.int32) * (K // 6)
+    w = torch.tensor([1.0, 0.0, 2.0, 0.5, 1.0, 3.0, 0.0, 1.5])
+    want = check(buf, index, teacher, w, K)
+    buf[1], teacher[6], index[6, 0], buf[6, 5] = math.nan, math.inf, K + 7, -math.inf
+    per_row, saved = B.distill_fwd(buf.cuda(), index.cuda(), teacher.cuda(), tau=1.5, weights=w.cuda())[1:]
+    assert bool(torch.isfinite(per_row).all()) and not per_row[[1, 6]].any() and not saved[[1, 6]].any()
+    assert torch.equal(B.distill_bwd(buf.cuda(), index.cuda(), teacher.cuda(), saved, tau=1.5, dloss=0.7, weights=w.cuda()), want)
+    buf[0, K // 2 + 1:] = -math.inf         # (the places of the first half alone count)
+    index[0, 3:] = -1
+    index[2] = -1
+    buf[2, 0] = math.nan
+    index[3, 2] = K
+    buf[4, K - 1] = math.nan
+    buf[5] = -math.inf
+    loss, per_row, saved = B.distill_fwd(buf.cuda(), index.cuda(), teacher.cuda(), tau=1.5, weights=w.cuda())
+    rows = O.distill_rows(buf[[0, 7]].double(), index[[0, 7]], teacher[[0, 7]].double(), 1.5)
+    assert (per_row[[0, 7]].double().cpu() - rows).abs().max() <= LOSS * 30
+    assert per_row[2] == 0 and bool(per_row[3:6].isnan().all()) and bool(loss.isnan().all())
+    out = B.distill_bwd(buf.cuda(), index.cuda(), teacher.cuda(), saved, tau=1.5, dloss=0.7, weights=w.cuda())
+    assert not out[[1, 2, 6]].any() and not out[0, K // 2 + 1:].any() and bool(out[3:6].isnan().all()) and bool(torch.isfinite(out[[0, 7]]).all())
+    assert torch.equal(out[7], want[7])
+
+
+def test_long_rows_captured():
+    bufs = [tuple(x.cuda() for x in case(9, 70000, 12, "bf16", seed=s, weights="some")) for s in range(3)]
+    z, index, teacher, w = (x.clone() for x in bufs[0])
+    ws = B.Workspace()
+    loss, rows, saved = B.distill_fwd(z, index, teacher, weights=w, ws=ws)
+    out = torch.empty_like(z)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        B.distill_fwd(z, index, teacher, weights=w, per_row=rows, loss=loss, saved=saved, ws=ws)
+        B.distill_bwd(z, index, teacher, saved, weights=w, out=out)
+    for other in bufs:
+        for a, b in zip((z, index, teacher, w), other):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = B.distill_fwd(*other[:3], weights=other[3])
+        assert all(torch.equal(a, b) for a, b in zip((loss, rows, saved), want))
+        assert torch.equal(out, B.distill_bwd(*other[:3], want[2], weights=other[3]))
