@@ -363,3 +363,64 @@ def test_single_gates_that_close(dtype):
     for (name, x), (_, y) in zip(by_head(got, heads), by_head(want, heads)):
         if name.startswith("da"):
             close(x[at], y[at], name + ", closed"), close(x, y, name)
+
+
+def of_sequences(c, ns):
+    """The case of some of the sequences alone."""
+    return {k: v if v is None or k == "bias" else v[:, ns] if k in ("gi", "do") else v[ns] for k, v in c.items()}
+
+
+def check_some(c, heads, ns, slack=True):
+    """check() of some of the sequences, which do not know of each other, and that the others' outputs are numbers."""
+    got, part = both(gpu(c), heads), of_sequences(c, ns)
+    assert all(bool(torch.isfinite(x).all()) for x in got)
+    want, more = wanted(part, heads), along(part, heads) if slack else torch.zeros(part["gi"].shape)
+    o, last, saved, dgi, dh0 = got
+    for name, a, b in zip(("o", "h_last", "saved", "dh0"), (o[:, ns], last[ns], saved[:, ns], dh0[ns]), (*want[:3], want[4])):
+        close(a, b, name)
+    for (name, a), (_, b), (_, c) in zip(by_head(dgi[:, ns], heads), by_head(want[3], heads), by_head(more, heads)):
+        close(a, b, name, c)
+
+
+# more than 128 heads of more than 64 columns: eight wavefronts a head, of each type and each number of a head's tiles; just 128: two blocks a head
+@pytest.mark.parametrize("T,N,heads,dtype", [(200, 65, (2, 1, 64, 72), "bf16"), (140, 43, (3, 1, 40, 128), "bf16"), (195, 65, (2, 2, 128, 128), "bf16"), (200, 33, (4, 2, 72, 100), "bf16"),
+                                             (200, 129, (1, 1, 24, 72), "bf16"), (200, 43, (3, 1, 24, 72), "f32"), (140, 129, (1, 1, 32, 128), "f32"), (200, 65, (2, 1, 64, 100), "f32"),
+                                             (195, 33, (4, 2, 128, 128), "f32"), (195, 64, (2, 2, 128, 128), "bf16"), (200, 32, (4, 2, 64, 100), "f32"), (200, 43, (3, 3, 128, 64), "f32"),
+                                             (140, 65, (2, 1, 72, 40), "f32")])
+def test_many_wide_heads(T, N, heads, dtype):
+    lengths = [(37 * n + T // 2) % (T + 1) for n in range(N)]
+    lengths[1], lengths[2], lengths[N - 1] = 0, 64, T
+    check_some(case(T, N, heads, dtype, lengths=lengths, seed=T + N), heads, [0, 1, 2, N - 1])
+
+
+# few heads and 48 chunks and more: cut into segments, all widths of a head's tiles, sequences that end in different segments, on their borders and before the first
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,heads,lengths", [(3100, (2, 1, 64, 72), [3100, 1024]), (3201, (1, 1, 100, 128), [2047, 3201]), (3073, (2, 1, 128, 128), [3073, 40]), (3072, (1, 1, 72, 16), [0, 3072]),
+                                             (3300, (2, 2, 48, 64), [1025, 3299])])
+def test_segments(T, heads, lengths, dtype):
+    check_some(case(T, 2, heads, dtype, lengths=lengths, seed=T), heads, [0, 1], slack=False)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows and their gradients of 5.4 GB, outputs of 4.3 GB, whose elements' numbers pass 2^31: windows of steps say what both passes give, as in test_very_long."""
+    T, heads = (1 << 27) + 77, (1, 1, 1, 16)
+    gen = torch.Generator("cuda").manual_seed(6)
+    gi = torch.randn(T, 1, 20, device="cuda", dtype=torch.bfloat16, generator=gen)
+    do = torch.randn(T, 1, 16, device="cuda", dtype=torch.bfloat16, generator=gen)
+    bias = torch.tensor([-1.0, 0.0], device="cuda")
+    gi[..., 18].clamp_(-1, 0.15)
+    # (a key of one element is 1 or -1 but for what EPS leaves of it; where it is small its gradient is large beyond measure)
+    gi[..., :2] = torch.where(gi[..., :2] < 0, gi[..., :2] - 1, gi[..., :2] + 1)
+    o, last, saved = B.delta_fwd(gi, heads, bias)
+    dgi, dh0 = B.delta_bwd(gi, saved, heads, bias, do=do)
+    assert gi.numel() > 1 << 31 and o.numel() > 1 << 31 and dgi.stride() == gi.stride()
+    for at in (0, 2048 * 64 - 20, (1 << 25) + 5, 107374182 - 30, (1 << 26) + 5, 3 * (1 << 25), (1 << 27) - 30, T - 64):
+        begin, end = max(at - 128, 0), min(at + 64 + 128, T)
+        part = {"gi": gi[begin:end].cpu(), "do": do[begin:end].cpu(), "bias": bias.cpu(), "h0": None, "lengths": None}
+        want, slack = wanted(part, heads), along(part, heads)
+        here = slice(at - begin, at - begin + 64)
+        close(o[at:at + 64], want[0][here], f"o at {at}")
+        for (name, a), (_, b), (_, more) in zip(by_head(dgi[at:at + 64], heads), by_head(want[3][here], heads), by_head(slack[here], heads)):
+            close(a, b, f"{name} at {at}", more)
+    close(last, want[1], "last")
+    assert bool(torch.isfinite(dh0).all())
