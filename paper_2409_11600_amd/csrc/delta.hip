@@ -1684,6 +1684,8 @@ bool at_once(const Sizes &z, int dtype, bool back)
 // Heads of more than 64 columns take two blocks with preparing wavefronts each, if both fit the chip at once, rather than one of eight wavefronts without (T=1024 forwards, us of 100 heads of
 // 128 x 128 in bf16 119 / 202, of 128 heads of 64 x 128 97 / 155, in fp32 152 / 235).
 bool flows(const Sizes &z) { return z.Dv <= 64 || (long long)z.N * z.H <= 128; }
+// What goes without them: eight wavefronts of many such heads, and heads of which LDS does not hold two chunks.
+template <typename T, int DT, int NW> constexpr bool kAlone = NW == 8 || !kFlows<T, DT>;
 // (Compose and Fill take a step a chunk of a segment, Jump one a segment: segments about as many as twice their chunks.)
 int segment_of(const Sizes &z)
 {
@@ -1786,18 +1788,19 @@ int nsk_delta_fwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
                     hipLaunchKernelGGL((delta_out_kernel<T, DT, NW>), dim3(all, (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, states, (T *)o);
                 return check_launch();
             }
-            if constexpr (kFlows<T, DT>)
-                if (flows(z)) {
+            if (kFlows<T, DT> && flows(z)) {
+                if constexpr (kFlows<T, DT>) {
                     allowed = allow_lds<delta_flow_kernel<T, DT>>(2 * bytes);
                     if (allowed != NSK_OK) return allowed;
                     hipLaunchKernelGGL((delta_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 64)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths,
                                        h0, (T *)o, h_last, saved);
-                    return check_launch();
                 }
-            allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
-            if (allowed != NSK_OK) return allowed;
-            hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0,
-                               (T *)o, h_last, saved);
+            } else if constexpr (kAlone<T, DT, NW>) {
+                allowed = allow_lds<delta_fwd_kernel<T, DT, NW>>(bytes);
+                if (allowed != NSK_OK) return allowed;
+                hipLaunchKernelGGL((delta_fwd_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths, h0,
+                                   (T *)o, h_last, saved);
+            }
             return check_launch();
         });
     };
@@ -1839,7 +1842,7 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
                     hipLaunchKernelGGL((delta_ends_flow_kernel<T, DT>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 64)), dim3(kFlowThreads), 2 * bytes, st, z, (const T *)gi, bias, lengths,
                                        (const T *)d_o, dh_last, dh0, ends);
                 }
-            } else {
+            } else if constexpr (kAlone<T, DT, NW>) {
                 allowed = allow_lds<delta_ends_kernel<T, DT, NW>>(bytes);
                 if (allowed != NSK_OK) return allowed;
                 hipLaunchKernelGGL((delta_ends_kernel<T, DT, NW>), dim3((unsigned)(z.N * z.H), (unsigned)ceil_div(z.Dv, 16 * NW)), dim3(NW * 64), bytes, st, z, (const T *)gi, bias, lengths,

@@ -95,3 +95,12 @@ def test_no_early_reads(tmp_path):
         assert sum(any(line.startswith(kind) for line in code) for code in functions.values()) > 20
     for name, code in functions.items():
         assert not early_reads(code), name
+
+
+@pytest.mark.skipif(shutil.which("nm") is None or not os.path.exists(build.LIB), reason="no symbols to read")
+def test_every_chain_kernel_is_reached():
+    """A head's chain of chunks without preparing wavefronts: four columns' wavefronts only where LDS does not hold two chunks (fp32 keys of more than 64), eight for all."""
+    names = subprocess.run(["nm", build.LIB], check=True, capture_output=True, text=True).stdout
+    for kernel in ("delta_fwd_kernel", "delta_ends_kernel"):
+        found = {m.groups() for m in re.finditer(r"__device_stub__" + kernel + r"I(f|DF16b)Li(\d)ELi(\d)E", names)}
+        assert found == {(t, d, "8") for t in ("f", "DF16b") for d in "248"} | {("f", "8", "4")}, kernel
