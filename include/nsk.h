@@ -619,7 +619,7 @@ int nsk_delta_bwd(const nsk_delta_desc_t *desc, const void *gi, const float *bia
 int nsk_delta_step(int dtype, int N, int H, int Hk, int D, int Dv, int S, const void *gi, const float *bias, const int *slots,
                    float *state, void *o, void *stream);
 
-/* Distillation: cross entropy against the M largest logits of a teacher.  Per row n, with p = softmax(top_logits[n] / tau) over the places whose
+/* Distillation: the divergence (relative entropy) of a row's distribution from that of a teacher's M largest logits.  Per row n, with p = softmax(top_logits[n] / tau) over the places whose
  * index is not negative and q = softmax(logits[n] / tau) over all K:
  *   per_row[n] = tau^2 * sum_m p_m * (log p_m - log q[top_index[n][m]]),   loss[0] = sum_n w_n * per_row[n] / sum_n w_n.
  * weights: float [N], not negative, or NULL: ones.  A row of weight 0 is not read, and one without a place has loss and gradient 0 whatever

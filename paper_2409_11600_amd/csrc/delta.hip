@@ -9,7 +9,8 @@
 //   dQ = exp(c) E2 + (dP L) K,  dK = -beta exp(c) E1 + exp(C - c) E3 + (dA beta L) K + (dA beta L)^T K + (dP L)^T Q,  L_ij = exp(c_i - c_j),
 //   and the gradients of beta and of the lengths of q and k from the row sums of the same products.  That of log alpha_t is the sum of what the gate t lies in: of row i's products with exp(c_i)
 //   from i = t on, of row j's with exp(C - c_j) in front of t, of dA_ij A_ij + dP_ij P_ij over the pairs j < t <= i, and of exp(C) S G.  Only such terms are added up: they all hold alpha_t, so
-//   that the sum keeps its bits where the gate is nearly closed (as the sum from t on of the gradients of c, most of which cancels there, it had no right digit left at alpha = 1e-7).
+//   that the sum keeps its bits where the gate is nearly closed (heads of 32 x 24 in fp32, T=200, relative 2-norms: 3e-7 at alpha = 1e-4, 7e-7 at 1e-7; as the sum from t on of the gradients of c,
+//   most of which cancels there, 4e-4 and 0.3).
 // Products keep 32 bits: states, gates' gradients and the results of a chunk of 64 dependent steps.  Those of two float operands are on the fp32 matrix unit.  Keys and queries in bf16 stay what they
 // are (their lengths are factors of rows and columns, applied to the products), and what they are multiplied with goes in three bf16 pieces that hold all of its bits: three products of 16
 // clocks for 32 indices, where the fp32 unit takes eight of 32.
@@ -83,8 +84,8 @@ __device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c)
 }
 // Nothing is moved across: the fragments of one row of tiles are in flight at a time, not those of a whole product, for which there are not enough registers.
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
-// Sums that are read behind a branch or in a loop's next round.  A matrix instruction's result may be read 11 wait states after it at the earliest; within a block of instructions the
-// compiler sees to that, but where a branch ended with one and a block of a jump alone lay between, it left no wait, and what was read was the sum before the last products.
+// Sums that are read behind a branch or in a loop's next round.  A result of v_mfma_f32_16x16x4_f32 may be read ten wait states after it at the earliest, one of v_mfma_f32_16x16x32_bf16 eight;
+// within a block of instructions the compiler sees to that, but where a branch ended with one and a block of a jump alone lay between, it left no wait, and what was read was the sum before the last products.
 template <int N> __device__ __forceinline__ void settle(f32x4 (&x)[N])
 {
     fence();
@@ -1686,7 +1687,7 @@ bool at_once(const Sizes &z, int dtype, bool back)
 bool flows(const Sizes &z) { return z.Dv <= 64 || (long long)z.N * z.H <= 128; }
 // What goes without them: eight wavefronts of many such heads, and heads of which LDS does not hold two chunks.
 template <typename T, int DT, int NW> constexpr bool kAlone = NW == 8 || !kFlows<T, DT>;
-// (Compose and Fill take a step a chunk of a segment, Jump one a segment: segments about as many as twice their chunks.)
+// (Compose and Fill take a step a chunk of a segment, Jump one a segment: of 16 chunks and more, so many that the segments are twice as many at most: 48 chunks are 3 of 16, 256 16 of 16, 1024 32 of 32.)
 int segment_of(const Sizes &z)
 {
     if (z.chunks < 48 || (long long)z.N * z.H * ceil_div(z.Dv, 16) > 256) return 0;
