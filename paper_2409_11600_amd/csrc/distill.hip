@@ -319,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void distill_bwd_kernel(Sizes z, const T 
         const float *tr = t + n * z.M;
         teacher = teacher_of(z, at, tr, by, part);
         none = !teacher.any;
-        c = dloss * w * saved[2 * (long long)z.N + 1] * z.tau;
+        c = dloss * (w * saved[2 * (long long)z.N + 1]) * z.tau;         // (the row's share first: it is at most 1, where a weight and dloss may leave the range together)
         if (teacher.bad) c = NAN;
         if (!none) {
             for (int i = threadIdx.x; i < 1 << z.bits; i += kThreads) table[i] = -1;

@@ -245,3 +245,15 @@ def test_long_rows_captured():
         want = B.distill_fwd(*other[:3], weights=other[3])
         assert all(torch.equal(a, b) for a, b in zip((loss, rows, saved), want))
         assert torch.equal(out, B.distill_bwd(*other[:3], want[2], weights=other[3]))
+
+
+@pytest.mark.parametrize("by,dloss", [(2.0 ** 100, 2.0 ** 30), (2.0 ** -100, 2.0 ** -40)])
+def test_only_shares_of_the_weights_count(by, dloss):
+    """Weights that are all larger or smaller by a power of two, with a factor of the loss that together with them leaves the range of a float: the same bits."""
+    buf, index, teacher, w = (x.cuda() for x in case(6, 500, 7, weights="some", seed=2))
+    assert bool(w.any())
+    (loss, rows, saved), (loss2, rows2, saved2) = (B.distill_fwd(buf, index, teacher, weights=x) for x in (w, w * by))
+    assert torch.equal(loss, loss2) and torch.equal(rows, rows2)
+    want = B.distill_bwd(buf, index, teacher, saved, weights=w, dloss=dloss)
+    assert bool(torch.isfinite(want).all()) and bool(want.any())
+    assert torch.equal(B.distill_bwd(buf, index, teacher, saved2, weights=w * by, dloss=dloss), want)
