@@ -625,8 +625,8 @@ int nsk_delta_step(int dtype, int N, int H, int Hk, int D, int Dv, int S, const 
  * weights: float [N], not negative, or NULL: ones.  A row of weight 0 is not read, and one without a place has loss and gradient 0 whatever
  * its logits hold; where all weights are 0 the loss is 0.  The tau^2 keeps gradients of different temperatures alike.  top_index: int [N,M], the same index may
  * occur several times (its places add up), one of K or more makes the row NaN; top_logits: float [N,M].  M is at most NSK_DISTILL_MOST.
- * logits / tau and the sum of the weights, if it is not 0, and its
- * reciprocal are within a float's (normal) range.  Row n of the logits begins at n * ld (0: dense).  A logit may be -infinity (q is 0 there; the loss is infinite where p is not). */
+ * A row's largest logit / tau and, where it is not 0, the sum of the weights and its reciprocal lie in the range of normal floats (words may be masked by the type's lowest value as
+ * well as by -infinity).  Row n of the logits begins at n * ld (0: dense).  A logit may be -infinity (q is 0 there; the loss is infinite where p is not). */
 #define NSK_DISTILL_MOST 1024
 typedef struct {
     int N, K, M;

@@ -257,3 +257,16 @@ def test_only_shares_of_the_weights_count(by, dloss):
     want = B.distill_bwd(buf, index, teacher, saved, weights=w, dloss=dloss)
     assert bool(torch.isfinite(want).all()) and bool(want.any())
     assert torch.equal(B.distill_bwd(buf, index, teacher, saved2, weights=w * by, dloss=dloss), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tau", [0.5, 2.0])
+@pytest.mark.parametrize("K", [901, 70000])
+def test_words_masked_by_the_lowest_value(K, tau, dtype):
+    """Their share is 0, also where the value / tau is out of range; whole lanes' and blocks' parts of a row may be masked."""
+    buf, index, teacher, _ = case(3, K, 9, dtype, seed=K)
+    buf[:, ::3] = torch.finfo(TYPES[dtype]).min
+    buf[1, K // 3:] = torch.finfo(TYPES[dtype]).min
+    index = index % (K // 3) // 3 * 3 + 1
+    out = check(buf, index, teacher, None, K, tau=tau)
+    assert not out[:, ::3].any() and not out[1, K // 3:].any()
